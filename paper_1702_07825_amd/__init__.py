@@ -24,7 +24,9 @@ WN_NONLIN_EXACT, WN_NONLIN_PAPER = 0, 1
 A_CLASSES = 256
 EXPORTED = ("wn_create", "wn_workspace_bytes", "wn_generate", "wn_generate_sampled", "wn_teacher_force", "wn_status",
             "wn_abort", "wn_kernel_variant", "wn_launch_info", "wn_destroy", "wn_error_string", "wn_last_error",
-            "wn_cond_create", "wn_cond_workspace_bytes", "wn_condition", "wn_condition_static", "wn_cond_destroy")
+            "wn_cond_create", "wn_cond_workspace_bytes", "wn_condition", "wn_condition_static", "wn_cond_destroy",
+            "wn_loss", "wn_loss_workspace_bytes", "wn_loss_backward", "wn_loss_backward_workspace_bytes",
+            "wn_embed", "wn_embed_backward", "wn_embed_backward_workspace_bytes", "wn_clip", "wn_clip_workspace_bytes")
 # WN_COND_SCRATCH_BYTES of include/wn_cond.h: the largest scratch wn_condition_static takes
 COND_SCRATCH_BYTES = 64 << 20
 # wn_sample_mode_t: how a step's distribution becomes its sample
@@ -57,6 +59,10 @@ class CondConfig(ctypes.Structure):
 
 class CondWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.POINTER(ctypes.c_float)) for n in ("w1", "b1", "w2", "b2")]
+
+
+class ClipArray(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 WEIGHT_FIELDS = ("embed", "b_embed", "w_prev", "w_cur", "b_gate", "w_res", "b_res", "w_skip", "b_skip",
@@ -95,6 +101,25 @@ def load_library(path: str = LIB_PATH):
         L.wn_condition_static.argtypes = [vp, i32, i32, vp, i32, vp, vp]
         L.wn_cond_destroy.restype = None
         L.wn_cond_destroy.argtypes = [vp]
+        f32 = ctypes.c_float
+        L.wn_loss.restype = ctypes.c_int
+        L.wn_loss.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.wn_loss_workspace_bytes.restype = sz
+        L.wn_loss_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.wn_loss_backward.restype = ctypes.c_int
+        L.wn_loss_backward.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.wn_loss_backward_workspace_bytes.restype = sz
+        L.wn_loss_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.wn_embed.restype = ctypes.c_int
+        L.wn_embed.argtypes = [i32, i32, i32, i32, vp, vp, f32, vp, vp]
+        L.wn_embed_backward.restype = ctypes.c_int
+        L.wn_embed_backward.argtypes = [i32, i32, i32, i32, vp, vp, f32, vp, vp, sz, vp]
+        L.wn_embed_backward_workspace_bytes.restype = sz
+        L.wn_embed_backward_workspace_bytes.argtypes = [i32, i32, i32]
+        L.wn_clip.restype = ctypes.c_int
+        L.wn_clip.argtypes = [i32, ctypes.POINTER(ClipArray), f32, vp, vp, sz, vp]
+        L.wn_clip_workspace_bytes.restype = sz
+        L.wn_clip_workspace_bytes.argtypes = []
         L.wn_teacher_force.restype = ctypes.c_int
         L.wn_teacher_force.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, vp]
         L.wn_status.restype = ctypes.c_int
@@ -310,3 +335,156 @@ class Conditioner:
         _check(self._lib.wn_condition_static(self._h, B, Tf, fp, int(T), cp, _stream_handle(stream)),
                "wn_condition_static")
         return cond
+
+
+# ------------------------------------------------------------------------------------------------
+# The operators at the ends of a training step (include/wn_train.h).  Matrices are float32 or
+# bfloat16, dense; a row whose target or token lies outside the classes (-1, say) is padding.
+# ``stream`` is a torch stream of the tensors' device (default: the current one there); tensors made
+# here (outputs, workspaces) belong to that stream.
+# ------------------------------------------------------------------------------------------------
+def _train_dtype(t, name):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    return WN_F32 if t.dtype == torch.float32 else WN_BF16
+
+
+class _On:
+    """The stream of a call and the allocations made for it."""
+
+    def __init__(self, t, stream):
+        import torch
+        if t.device.type != "cuda":
+            raise ValueError("tensors must be on a GPU device")
+        self.device = t.device
+        self.stream = torch.cuda.current_stream(t.device) if stream is None else stream
+        if self.stream.device != t.device:
+            raise ValueError("stream is of %s, the tensors are on %s" % (self.stream.device, t.device))
+        self.handle = self.stream.cuda_stream
+
+    def empty(self, shape, dtype):
+        import torch
+        if self.stream == torch.cuda.current_stream(self.device):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def out(self, t, shape, dtype, name):
+        t = self.empty(shape, dtype) if t is None else t
+        return t, self.ptr(t, dtype, shape, name)
+
+    def ptr(self, t, dtype, shape, name):
+        p = _dev_ptr(t, dtype, shape, name)
+        if t.device != self.device:
+            raise ValueError("%s is on %s, not on %s" % (name, t.device, self.device))
+        return p
+
+    def workspace(self, t, nbytes):
+        import torch
+        if t is None:
+            t = self.empty(max(nbytes, 1), torch.uint8)
+        return t, t.data_ptr(), t.numel() * t.element_size()
+
+
+def _matrix(t, name):
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions, got %s" % (name, tuple(t.shape)))
+    return int(t.shape[0]), int(t.shape[1])
+
+
+def head_loss(x, w, y, b=None, loss=None, lse=None, workspace=None, stream=None):
+    """wn_loss: x [N, D], w [V, D], y int32 [N], b float32 [V] or None -> (loss, lse), float32 [N]."""
+    import torch
+    dt, lib = _train_dtype(x, "x"), load_library()
+    (N, D), (V, _) = _matrix(x, "x"), _matrix(w, "w")
+    on = _On(x, stream)
+    xp, wp = on.ptr(x, x.dtype, (N, D), "x"), on.ptr(w, x.dtype, (V, D), "w")
+    yp = on.ptr(y, torch.int32, (N,), "y")
+    bp = None if b is None else on.ptr(b, torch.float32, (V,), "b")
+    loss, lp = on.out(loss, (N,), torch.float32, "loss")
+    lse, sp = on.out(lse, (N,), torch.float32, "lse")
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_loss_workspace_bytes(dt, N, D, V))
+    _check(lib.wn_loss(dt, N, D, V, xp, wp, bp, yp, lp, sp, wsp, wsn, on.handle), "wn_loss")
+    return loss, lse
+
+
+def head_loss_backward(x, w, y, lse, grad, b=None, need=("dx", "dw", "db"), dx=None, dw=None, db=None, workspace=None,
+                       stream=None):
+    """wn_loss_backward: gradients of (grad * loss).sum() for ``need`` of x, w and b -> (dx, dw, db), None
+    where not needed.  lse: of head_loss on the same x, w, y and b; grad float32 [N]."""
+    import torch
+    dt, lib = _train_dtype(x, "x"), load_library()
+    (N, D), (V, _) = _matrix(x, "x"), _matrix(w, "w")
+    if not need or any(k not in ("dx", "dw", "db") for k in need):
+        raise ValueError("need must name some of dx, dw, db, got %r" % (need,))
+    on = _On(x, stream)
+    xp, wp = on.ptr(x, x.dtype, (N, D), "x"), on.ptr(w, x.dtype, (V, D), "w")
+    yp, sp = on.ptr(y, torch.int32, (N,), "y"), on.ptr(lse, torch.float32, (N,), "lse")
+    gp = on.ptr(grad, torch.float32, (N,), "grad")
+    bp = None if b is None else on.ptr(b, torch.float32, (V,), "b")
+    dx, dxp = on.out(dx, (N, D), x.dtype, "dx") if "dx" in need else (None, None)
+    dw, dwp = on.out(dw, (V, D), x.dtype, "dw") if "dw" in need else (None, None)
+    db, dbp = on.out(db, (V,), torch.float32, "db") if "db" in need else (None, None)
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_loss_backward_workspace_bytes(dt, N, D, V))
+    _check(lib.wn_loss_backward(dt, N, D, V, xp, wp, bp, yp, sp, gp, dxp, dwp, dbp, wsp, wsn, on.handle),
+           "wn_loss_backward")
+    return dx, dw, db
+
+
+def embed(table, tokens, scale: float = 1.0, out=None, stream=None):
+    """wn_embed: table [V, D], tokens int32 of any shape -> scale * table[tokens], zeros for tokens outside 0..V-1."""
+    import torch
+    dt, lib = _train_dtype(table, "table"), load_library()
+    V, D = _matrix(table, "table")
+    on = _On(table, stream)
+    shape = tuple(tokens.shape)
+    N = int(tokens.numel())
+    tp, kp = on.ptr(table, table.dtype, (V, D), "table"), on.ptr(tokens, torch.int32, shape, "tokens")
+    out, op = on.out(out, shape + (D,), table.dtype, "out")
+    _check(lib.wn_embed(dt, N, D, V, tp, kp, float(scale), op, on.handle), "wn_embed")
+    return out
+
+
+def embed_backward(dout, tokens, V: int, scale: float = 1.0, dtable=None, workspace=None, stream=None):
+    """wn_embed_backward: dout (the shape of tokens, then D) -> dtable [V, D], the gradient of embed's table."""
+    import torch
+    dt, lib = _train_dtype(dout, "dout"), load_library()
+    if dout.dim() < 1:
+        raise ValueError("dout must have a dimension of the table's columns")
+    shape, D, V = tuple(tokens.shape), int(dout.shape[-1]), int(V)
+    N = int(tokens.numel())
+    on = _On(dout, stream)
+    dp, kp = on.ptr(dout, dout.dtype, shape + (D,), "dout"), on.ptr(tokens, torch.int32, shape, "tokens")
+    dtable, tp = on.out(dtable, (V, D), dout.dtype, "dtable")
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_embed_backward_workspace_bytes(N, D, V))
+    _check(lib.wn_embed_backward(dt, N, D, V, dp, kp, float(scale), tp, wsp, wsn, on.handle), "wn_embed_backward")
+    return dtable
+
+
+def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None, stream=None):
+    """wn_clip: scales the tensors of ``grads`` so that the norm over all of them is at most max_norm, in
+    place or into ``outs``; returns that norm before (float32 [], on the device).  Where it is not finite the
+    tensors are left as they are."""
+    import torch
+    grads, lib = list(grads), load_library()
+    if not grads:
+        raise ValueError("grads is empty")
+    outs = grads if outs is None else list(outs)
+    if len(outs) != len(grads):
+        raise ValueError("%d outs for %d grads" % (len(outs), len(grads)))
+    for i, g in enumerate(grads):
+        _train_dtype(g, "grads[%d]" % i)
+    on = _On(grads[0], stream)
+    arrays = (ClipArray * len(grads))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        a = arrays[i]
+        a.g = on.ptr(g, g.dtype, g.shape, "grads[%d]" % i)
+        a.out = a.g if o is g else on.ptr(o, g.dtype, g.shape, "outs[%d]" % i)
+        a.n, a.dtype = g.numel(), WN_F32 if g.dtype == torch.float32 else WN_BF16
+    norm, np_ = on.out(norm, (), torch.float32, "norm")
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_clip_workspace_bytes())
+    _check(lib.wn_clip(len(grads), arrays, float(max_norm), np_, wsp, wsn, on.handle), "wn_clip")
+    return norm

@@ -1,0 +1,205 @@
+// The norm over many gradient arrays and their clip (gfx950).  Declarations and contracts are in
+// include/wn_train.h.
+//
+// Two passes over the arrays: sums of squares per block, then every block joins the blocks' sums in the same
+// order and scales its share.  The arrays go to the kernels as arguments (kArrays of them a launch), cut
+// into chunks of kElems elements that the blocks take in turn, so that one launch serves arrays of any
+// sizes.  Squares are summed in fp64: a chunk's sum of fp32 squares would overflow from gradients of 1e19 on
+// and vanish below 1e-23.
+#include "wn_arrays.h"
+
+#include "wn_wave.h"
+
+#include <cmath>
+
+namespace {
+
+using namespace wnt;
+
+constexpr int kArrays = 96;    // arrays of a launch: the arguments stay under 4 KB
+constexpr int kThreads = 256;
+constexpr int kElems = 8192;   // of a chunk
+constexpr int kSlots = 1024;   // blocks of a launch, partial sums
+
+struct Arrays {
+  const void* g[kArrays];
+  void* out[kArrays];
+  long long n[kArrays];
+  unsigned first[kArrays + 1];  // chunks before the array
+  unsigned char bf16[kArrays];
+  int count;
+};
+static_assert(sizeof(Arrays) < 3800, "kernel arguments");
+
+// Four elements at any element's alignment.
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ int array_of(const Arrays& a, unsigned chunk) {
+  int lo = 0, hi = a.count;  // the last array whose first chunk is at most `chunk` (empty arrays have none)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.first[mid] <= chunk) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double s[kThreads / 64];
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = s[0];
+  for (int w = 1; w < kThreads / 64; ++w) v += s[w];
+  __syncthreads();
+  return v;
+}
+
+__device__ __forceinline__ double squares(u32x4 w, bool bf16) {
+  double v = 0.0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (bf16) {
+      const double a = __uint_as_float(w[e] << 16), b = __uint_as_float(w[e] & 0xffff0000u);
+      v += a * a + b * b;
+    } else {
+      const double a = __uint_as_float(w[e]);
+      v += a * a;
+    }
+  }
+  return v;
+}
+
+// slot[b] (+)= the squares of the chunks b, b + grid, ...
+__global__ __launch_bounds__(kThreads) void clip_squares(const Arrays a, double* slot, int add) {
+  double sum = 0.0;
+  for (unsigned c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
+    const int k = array_of(a, c);
+    const long long at = (long long)(c - a.first[k]) * kElems;
+    const int n = (int)min((long long)kElems, a.n[k] - at);
+    const bool bf = a.bf16[k];
+    const int per = bf ? 8 : 4;
+    const char* p = static_cast<const char*>(a.g[k]) + at * (bf ? 2 : 4);
+    const int whole = n / per;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < whole; i += kThreads) {
+      const u32x4u w = *reinterpret_cast<const u32x4u*>(p + 16 * (size_t)i);
+      sum += squares(u32x4{w[0], w[1], w[2], w[3]}, bf);
+    }
+    const int rest = whole * per + threadIdx.x;
+    if (rest < n) {
+      const double v = bf ? bf16_val(reinterpret_cast<const u16*>(p)[rest]) : reinterpret_cast<const float*>(p)[rest];
+      sum += v * v;
+    }
+  }
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) slot[blockIdx.x] = add ? slot[blockIdx.x] + sum : sum;
+}
+
+__global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const double* slot, int slots, float max_norm, float* norm_out,
+                                                       int first) {
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < slots; i += kThreads) sum += slot[i];
+  const double wide = sqrt(block_sum(sum));
+  const float norm = (float)wide;
+  if (first && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+  // (max_norm = 0: 0 times each element)
+  const bool scaled = norm > max_norm && norm < INFINITY;
+  const float f = scaled ? (float)(max_norm / wide) : 1.f;
+  for (unsigned c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
+    const int k = array_of(a, c);
+    if (!scaled && a.out[k] == a.g[k]) continue;
+    const long long at = (long long)(c - a.first[k]) * kElems;
+    const int n = (int)min((long long)kElems, a.n[k] - at);
+    const bool bf = a.bf16[k];
+    const int per = bf ? 8 : 4;
+    const char* p = static_cast<const char*>(a.g[k]) + at * (bf ? 2 : 4);
+    char* o = static_cast<char*>(a.out[k]) + at * (bf ? 2 : 4);
+    const int whole = n / per;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < whole; i += kThreads) {
+      const u32x4u w = *reinterpret_cast<const u32x4u*>(p + 16 * (size_t)i);
+      u32x4u r = w;
+      if (scaled) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          r[e] = bf ? bf16_pair(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f)
+                    : __float_as_uint(__uint_as_float(w[e]) * f);
+      }
+      *reinterpret_cast<u32x4u*>(o + 16 * (size_t)i) = r;
+    }
+    const int rest = whole * per + threadIdx.x;
+    if (rest < n) {
+      if (bf) {
+        const u16 v = reinterpret_cast<const u16*>(p)[rest];
+        reinterpret_cast<u16*>(o)[rest] = scaled ? bf16_bits(bf16_val(v) * f) : v;
+      } else {
+        const float v = reinterpret_cast<const float*>(p)[rest];
+        reinterpret_cast<float*>(o)[rest] = scaled ? v * f : v;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wn_clip_workspace_bytes(void) { return kSlots * sizeof(double); }
+
+int wn_clip(int32_t n_arrays, const wn_clip_array* arrays, float max_norm, float* norm, void* workspace, size_t ws_bytes,
+            void* stream) {
+  wn_clear_last_error();
+  if (n_arrays < 0 || n_arrays > 1 << 20) return wn_set_last_error(WN_EINVAL, "n_arrays must be 0..2^20");
+  if ((n_arrays && !arrays) || !norm) return wn_set_last_error(WN_EINVAL, "null pointer");
+  if (!(max_norm >= 0.f)) return wn_set_last_error(WN_EINVAL, "max_norm must be >= 0");
+  unsigned long long chunks = 0;
+  for (int k = 0; k < n_arrays; ++k) {
+    const wn_clip_array& a = arrays[k];
+    const int rc = bad_dtype(a.dtype);
+    if (rc != WN_OK) return rc;
+    if (a.n < 0 || a.n > 1LL << 40) return wn_set_last_error(WN_EINVAL, "an array's n must be 0..2^40");
+    if (a.n && (!a.g || !a.out)) return wn_set_last_error(WN_EINVAL, "null pointer");
+    const uintptr_t size = a.dtype == WN_BF16 ? 2 : 4;
+    if (a.n && (reinterpret_cast<uintptr_t>(a.g) % size || reinterpret_cast<uintptr_t>(a.out) % size))
+      return wn_set_last_error(WN_EINVAL, "an array is not aligned to its elements");
+    chunks += ceil_div((size_t)a.n, kElems);
+  }
+  if (chunks > 1ull << 31) return wn_set_last_error(WN_EINVAL, "too many elements");
+  int rc = bad_workspace(workspace, ws_bytes, wn_clip_workspace_bytes());
+  if (rc != WN_OK) return rc;
+  ArrayScope scope;
+  if ((rc = scope.check(norm, "norm")) != WN_OK || (rc = scope.check(workspace, "workspace")) != WN_OK) return rc;
+  for (int k = 0; k < n_arrays; ++k)
+    if (arrays[k].n && ((rc = scope.check(arrays[k].g, "g")) != WN_OK ||
+                        (arrays[k].out != arrays[k].g && (rc = scope.check(arrays[k].out, "out")) != WN_OK)))
+      return rc;
+  if ((rc = scope.enter()) != WN_OK) return rc;
+  double* const slot = static_cast<double*>(workspace);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const unsigned grid = (unsigned)std::max<unsigned long long>(1, std::min<unsigned long long>(kSlots, chunks));
+  for (int pass = 0; pass < 2; ++pass) {
+    int k = 0;
+    bool first = true;
+    do {
+      Arrays a{};
+      for (; k < n_arrays && a.count < kArrays; ++k) {
+        if (!arrays[k].n) continue;
+        const int i = a.count++;
+        a.g[i] = arrays[k].g;
+        a.out[i] = arrays[k].out;
+        a.n[i] = arrays[k].n;
+        a.bf16[i] = arrays[k].dtype == WN_BF16;
+        a.first[i + 1] = a.first[i] + (unsigned)ceil_div((size_t)arrays[k].n, kElems);
+      }
+      if (pass == 0) hipLaunchKernelGGL(clip_squares, dim3(grid), dim3(kThreads), 0, st, a, slot, !first);
+      else hipLaunchKernelGGL(clip_scale, dim3(grid), dim3(kThreads), 0, st, a, slot, (int)grid, max_norm, norm, (int)first);
+      first = false;
+    } while (k < n_arrays);
+  }
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+}
+
+}  // extern "C"

@@ -1,0 +1,801 @@
+// The loss of an output layer and its gradients without keeping the logits (gfx950).  Declarations and
+// contracts are in include/wn_train.h.
+//
+// Everything heavy is one product C[b][a] = sum_k A[a][k] B[b][k] with different ends (product):
+//   logits   A = w, B = x           the tile's largest logit and sum of exponentials of each row (forward), or
+//                                   q = g (exp(l - lse) - [v = y]) as the next products' operand (backward)
+//   dx       A = w transposed, B = q
+//   dw       A = x transposed, B = q transposed
+// Both operands lie along k in memory, so the transposed ones are copies (pack_cols); the backward pass takes
+// the vocabulary in pieces, so that they and q stay within a fixed size.
+//
+// Operands are 16-bit: bf16 arrays as they are, fp32 ones in two fp16 parts each (pack_rows, pack_cols): a
+// row is scaled by a power of two so that its largest value lies in [2^14, 2^15), hi = fp16(v),
+// lo = fp16(v - hi), which holds v to 2^-22 of itself or 2^-39 of the row's largest, and a product takes
+// hi hi + hi lo + lo hi (lo lo is below 2^-22 of it), summed in fp32.
+#include "wn_arrays.h"
+
+#include "wn_wave.h"
+
+namespace {
+
+using namespace wnt;
+
+// A row of an operand is a run of chunks of 64 16-bit units (128 bytes): 64 bf16 values, or the hi parts of
+// 32 values and then their lo parts.
+constexpr int kChunk = 64;
+__host__ __device__ constexpr int chunk_values(bool sp) { return sp ? 32 : 64; }
+inline int padded_units(int k, bool sp) { return (int)ceil_div(k, chunk_values(sp)) * kChunk; }
+
+struct Operand {
+  const u16* p;
+  long long rows;
+  int ld;  // units from row to row (a multiple of 8; 16-byte aligned)
+  int k;   // units of a row that hold values; those behind read as 0
+};
+
+struct Product {
+  Operand a, b;
+  int ta, tb;    // tiles
+  int splits, cps;  // parts of the sum over k, chunks of each
+};
+
+typedef __amdgpu_buffer_rsrc_t rsrc;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Tiles of TA x TB outputs by WA x WB waves.
+template <int TA_, int TB_, int WA_, int WB_>
+struct Tile {
+  static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_;
+  static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves;
+  static constexpr int NA = TA / WA / 16, NB = TB / WB / 16;  // 16 x 16 outputs of a wave
+  static constexpr int kStage = (TA + TB) * kChunk * 2;        // bytes of a chunk of both operands
+  static constexpr int kLds = 2 * kStage;
+  static constexpr int IA = TA * 8 / kThreads, IB = TB * 8 / kThreads;  // 16-byte pieces of a chunk per thread
+};
+using Big = Tile<256, 256, 2, 4>;
+using Small = Tile<128, 128, 2, 2>;
+
+// A wave's place in the tile's outputs: lane (n, quad) ends with outputs a = a0 + 16 i + 4 quad + 0..3 of
+// row b = b0 + 16 j + n.
+struct Place {
+  int ta, tb, split;  // tile
+  int a0, b0;         // this wave's first output
+  int wa, wb, n, quad;
+};
+
+template <class T, bool SP, class End>
+__global__ __launch_bounds__(T::kThreads) void product(const Product g, const End end) {
+  extern __shared__ __align__(16) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Place pl;
+  {
+    int t = blockIdx.x;
+    pl.split = t % g.splits;
+    t /= g.splits;
+    pl.ta = t % g.ta;
+    pl.tb = t / g.ta;
+  }
+  pl.wa = wave / T::WB;
+  pl.wb = wave % T::WB;
+  pl.n = lane & 15;
+  pl.quad = lane >> 4;
+  const int ra = pl.wa * (T::TA / T::WA), rb = pl.wb * (T::TB / T::WB);
+  pl.a0 = pl.ta * T::TA + ra;
+  pl.b0 = pl.tb * T::TB + rb;
+
+  auto resource = [&](const Operand& o, long long row0, int rows) {
+    const long long left = o.rows - row0 < rows ? o.rows - row0 : rows;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<u16*>(o.p) + row0 * o.ld, (short)0,
+                                             (int)(((left - 1) * o.ld + o.k) * 2), 0x00020000);
+  };
+  const rsrc ares = resource(g.a, (long long)pl.ta * T::TA, T::TA), bres = resource(g.b, (long long)pl.tb * T::TB, T::TB);
+  // 16-byte piece `pos` of row r in LDS is piece pos ^ (r >> 1 & 7) of the row's chunk: the 16 rows that 16 lanes
+  // read at one piece then fall on different banks
+  int voff[T::IA + T::IB], piece[1];
+#pragma unroll
+  for (int i = 0; i < T::IA + T::IB; ++i) {
+    const int p = (i < T::IA ? i : i - T::IA) * T::kThreads + tid, r = p >> 3, c = (p & 7) ^ (r >> 1 & 7);
+    voff[i] = r * (i < T::IA ? g.a.ld : g.b.ld) * 2 + c * 16;
+  }
+  piece[0] = (tid & 7) ^ (tid >> 4 & 7);  // of every piece above: kThreads / 8 rows is a multiple of 16
+  const int kc = (max(g.a.k, g.b.k) + kChunk - 1) / kChunk;
+  const int c0 = pl.split * g.cps, c1 = min(kc, c0 + g.cps);
+  auto stage = [&](int c, char* to) {
+    const int left = g.a.k - c * kChunk, leftb = g.b.k - c * kChunk;
+#pragma unroll
+    for (int i = 0; i < T::IA + T::IB; ++i) {
+      const bool isa = i < T::IA;
+      const int at = ((isa ? i : i - T::IA) * T::kThreads + wave * 64) * 16 + (isa ? 0 : T::TA * kChunk * 2);
+      // (a piece behind the row's values reads past the buffer's end, which gives 0)
+      const int v = piece[0] * 8 < (isa ? left : leftb) ? voff[i] : (int)0x80000000;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(isa ? ares : bres, (lds_void*)(to + at), 16, v, c * kChunk * 2, 0, 0);
+    }
+  };
+  f32x4 acc[T::NA][T::NB];
+#pragma unroll
+  for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (c0 < c1) stage(c0, lds);
+  const int sw = pl.n >> 1;
+  const int fa = (ra + pl.n) * kChunk * 2, fb = (T::TA + rb + pl.n) * kChunk * 2;
+  const int s0 = (pl.quad ^ sw) * 16, s1 = ((4 + pl.quad) ^ sw) * 16;
+  for (int c = c0; c < c1; ++c) {
+    char* const at = lds + ((c - c0) & 1) * T::kStage;
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (c + 1 < c1) stage(c + 1, lds + ((c + 1 - c0) & 1) * T::kStage);
+    if constexpr (SP) {
+      f16x8 ah[T::NA], al[T::NA], bh[T::NB], bl[T::NB];
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) {
+        ah[i] = *reinterpret_cast<const f16x8*>(at + fa + i * 16 * kChunk * 2 + s0);
+        al[i] = *reinterpret_cast<const f16x8*>(at + fa + i * 16 * kChunk * 2 + s1);
+      }
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) {
+        bh[j] = *reinterpret_cast<const f16x8*>(at + fb + j * 16 * kChunk * 2 + s0);
+        bl[j] = *reinterpret_cast<const f16x8*>(at + fb + j * 16 * kChunk * 2 + s1);
+      }
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int j = 0; j < T::NB; ++j) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        bf16x8 a[T::NA], b[T::NB];
+#pragma unroll
+        for (int i = 0; i < T::NA; ++i) a[i] = *reinterpret_cast<const bf16x8*>(at + fa + i * 16 * kChunk * 2 + (s ? s1 : s0));
+#pragma unroll
+        for (int j = 0; j < T::NB; ++j) b[j] = *reinterpret_cast<const bf16x8*>(at + fb + j * 16 * kChunk * 2 + (s ? s1 : s0));
+#pragma unroll
+        for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+          for (int j = 0; j < T::NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+  __syncthreads();
+  end.template operator()<T>(acc, pl, lds);
+}
+
+// What both ends of the logits product need: l[n][v] = acc 2^-(ex[n] + ew[v]) + b[v].
+struct Logits {
+  const int *ex, *ew;  // the operands' scales (fp32 arrays), or null
+  const float* bias;   // of the piece, or null
+  const int32_t* y;
+  int N, V, v0, V_all;  // rows; classes of the piece, the first of them, and of the layer
+  template <class T>
+  __device__ void take(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = pl.a0 + 16 * i + 4 * pl.quad + e, vc = min(v, V - 1);
+        const float bv = bias ? bias[vc] : 0.f;
+        const int sv = ew ? ew[vc] : 0;
+#pragma unroll
+        for (int j = 0; j < T::NB; ++j) {
+          const int n = min(pl.b0 + 16 * j + pl.n, N - 1);
+          float l = acc[i][j][e];
+          if (ew) l = ldexpf(l, -(sv + ex[n]));
+          acc[i][j][e] = v < V ? l + bv : -INFINITY;
+        }
+      }
+  }
+};
+
+__device__ __forceinline__ float across_quads_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float across_quads_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// Forward: (largest logit, sum of exp(l - largest)) of each row in the tile's classes, and the target's logit.
+struct StatsEnd {
+  Logits l;
+  float2* part;   // [tiles of all pieces][N]
+  int tile0;      // the piece's first
+  float* target;  // [N]
+  template <class T>
+  __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
+    l.take<T>(acc, pl);
+    float2* const s = reinterpret_cast<float2*>(lds);  // [WA][TB]
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      const int n = pl.b0 + 16 * j + pl.n;
+      const int t = n < l.N ? l.y[n] - l.v0 : -1;
+      float m = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = acc[i][j][e];
+          m = fmaxf(m, v);
+          if (t == pl.a0 + 16 * i + 4 * pl.quad + e) target[n] = v;  // (t < V: v0 + V is a tile's end or the last class)
+        }
+      m = across_quads_max(m);
+      // (a row without a class yet: every exponential is 0, not exp(-inf + inf))
+      const float at = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += wnk::expf_fast(acc[i][j][e] - at);
+      sum = across_quads_sum(sum);
+      if (pl.quad == 0) s[pl.wa * T::TB + pl.wb * (T::TB / T::WB) + 16 * j + pl.n] = make_float2(m, sum);
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < T::TB; k += T::kThreads) {
+      const int n = pl.tb * T::TB + k;
+      float2 r = s[k];
+#pragma unroll
+      for (int w = 1; w < T::WA; ++w) {
+        const float2 o = s[w * T::TB + k];
+        const float m = fmaxf(r.x, o.x), at = m == -INFINITY ? 0.f : m;
+        r = make_float2(m, r.y * wnk::expf_fast(r.x - at) + o.y * wnk::expf_fast(o.x - at));
+      }
+      if (n < l.N) part[(size_t)(tile0 + pl.ta) * l.N + n] = r;
+    }
+  }
+};
+
+// 16-bit operand units of q (three forms: bf16, or the fp16 parts of q 2^14).
+constexpr int kQScale = 14;
+__device__ __forceinline__ void split(float v, u16& hi, u16& lo) {
+  const _Float16 h = (_Float16)v;
+  const float r = v - (float)h;
+  hi = __builtin_bit_cast(u16, h);
+  lo = __builtin_bit_cast(u16, (_Float16)(r == r ? r : 0.f));  // (an infinity has no rest)
+}
+
+// Backward: q of the tile's rows and classes as the operands of dx ([n][v]) and dw ([v][n]), and the sums of g q
+// over the tile's rows.  fp32: q without g (|q| <= 1); bf16: g q.
+template <bool SP>
+struct GradEnd {
+  Logits l;
+  const float *lse, *g;
+  u16 *q, *qt;     // or null
+  int ldq, ldqt;
+  float* db;       // [tiles of rows][V], or null
+  template <class T>
+  __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
+    l.take<T>(acc, pl);
+    float* const s = reinterpret_cast<float*>(lds);  // [WB][TA]
+    float gn[T::NB];
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      const int n = pl.b0 + 16 * j + pl.n;
+      const int yn = n < l.N ? l.y[n] : -1;
+      const bool ok = yn >= 0 && yn < l.V_all;
+      const int t = ok ? yn - l.v0 : -1;
+      const float ln = ok ? lse[n] : 0.f;
+      gn[j] = ok ? g[n] : 0.f;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) {
+        const int v = pl.a0 + 16 * i + 4 * pl.quad;
+        f32x4 p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = ok ? wnk::expf_fast(acc[i][j][e] - ln) - (v + e == t ? 1.f : 0.f) : 0.f;
+          if (v + e >= l.V) p[e] = 0.f;
+          acc[i][j][e] = ok ? p[e] * gn[j] : 0.f;
+        }
+        if constexpr (SP) {
+          u16 hi[4], lo[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) split(ldexpf(p[e], kQScale), hi[e], lo[e]);
+          if (q && n < l.N && v < ldq / 2) {
+            u16* d = q + (size_t)n * ldq + v / 32 * kChunk + v % 32;
+            *reinterpret_cast<u32x2*>(d) = u32x2{(unsigned)hi[0] | (unsigned)hi[1] << 16, (unsigned)hi[2] | (unsigned)hi[3] << 16};
+            *reinterpret_cast<u32x2*>(d + 32) = u32x2{(unsigned)lo[0] | (unsigned)lo[1] << 16, (unsigned)lo[2] | (unsigned)lo[3] << 16};
+          }
+          if (qt && n < ldqt / 2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v + e < l.V) {
+                u16* d = qt + (size_t)(v + e) * ldqt + n / 32 * kChunk + n % 32;
+                d[0] = hi[e];
+                d[32] = lo[e];
+              }
+        } else {
+          if (q && n < l.N && v < ldq)
+            *reinterpret_cast<u32x2*>(q + (size_t)n * ldq + v) =
+                u32x2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
+          if (qt && n < ldqt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v + e < l.V) qt[(size_t)(v + e) * ldqt + n] = bf16_bits(acc[i][j][e]);
+        }
+      }
+    }
+    if (!db) return;
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < T::NB; ++j) sum += acc[i][j][e];
+        sum = wnk::gsum16(sum);
+        if (pl.n == 0) s[pl.wb * T::TA + pl.wa * (T::TA / T::WA) + 16 * i + 4 * pl.quad + e] = sum;
+      }
+    __syncthreads();
+    for (int k = threadIdx.x; k < T::TA; k += T::kThreads) {
+      const int v = pl.ta * T::TA + k;
+      float sum = s[k];
+#pragma unroll
+      for (int w = 1; w < T::WB; ++w) sum += s[w * T::TA + k];
+      if (v < l.V) db[(size_t)pl.tb * l.V + v] = sum;
+    }
+  }
+};
+
+// dx and dw: out[b][a] (rows of D).
+struct OutEnd {
+  int A, B;           // D, rows
+  const int* ea;      // scales of operand A's rows, or null; then the product is acc 2^-(ea[a] + kQScale)
+  const int32_t* y;   // dx: rows whose y is outside 0 .. V-1 are 0; or null
+  const float* g;     // fp32 dx: the row's factor, or null
+  int V;
+  float* sum;         // [splits][B][A], set (add = 0) or added to; or null
+  int add;
+  void* out;          // where sum is null
+  int bf16;
+  template <class T>
+  __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char*) const {
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      const int b = pl.b0 + 16 * j + pl.n;
+      if (b >= B) continue;
+      const int yb = y ? y[b] : 0;
+      const bool ok = yb >= 0 && yb < V;
+      const float f = g && ok ? g[b] : 1.f;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) {
+        const int a = pl.a0 + 16 * i + 4 * pl.quad;
+        f32x4 v = acc[i][j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (ea) v[e] = ldexpf(v[e], -(ea[min(a + e, A - 1)] + kQScale)) * f;
+          if (!ok) v[e] = 0.f;
+        }
+        if (sum) {
+          float* d = sum + ((size_t)pl.split * B + b) * A + a;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (a + e < A) d[e] = add ? d[e] + v[e] : v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (a + e < A) {
+              if (bf16) static_cast<u16*>(out)[(size_t)b * A + a + e] = bf16_bits(v[e]);
+              else static_cast<float*>(out)[(size_t)b * A + a + e] = v[e];
+            }
+        }
+      }
+    }
+  }
+};
+
+// ------------------------------------------------------------------------------------------------
+// The operands
+// ------------------------------------------------------------------------------------------------
+// The scale of a row whose largest magnitude is m: m 2^e in [2^14, 2^15).
+__device__ __forceinline__ int scale_of(float m) { return m > 0.f && m < INFINITY ? 14 - ilogbf(m) : 0; }
+
+// Rows [R][K] as they are; a wave per row.
+template <class E>
+__global__ __launch_bounds__(256) void pack_rows(const E* src, int R, int K, u16* dst, int units, int* scale) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (r >= R) return;
+  const E* s = src + (size_t)r * K;
+  u16* d = dst + (size_t)r * units;
+  if constexpr (sizeof(E) == 2) {
+    for (int k = lane; k < units; k += 64) d[k] = k < K ? s[k] : (u16)0;
+  } else {
+    float m = 0.f;
+    for (int k = lane; k < K; k += 64) m = fmaxf(m, fabsf(s[k]));
+    const int e = scale_of(wnk::wave_max(m));
+    if (lane == 0) scale[r] = e;
+    for (int k = lane; k < units / 2; k += 64) {
+      u16 hi, lo;
+      split(k < K ? ldexpf(s[k], e) : 0.f, hi, lo);
+      u16* p = d + k / 32 * kChunk + k % 32;
+      p[0] = hi;
+      p[32] = lo;
+    }
+  }
+}
+
+// A row of x counts in the sums over rows by its factor: g (fp32 arrays) or 1; not at all without a target.
+struct RowFactor {
+  const int32_t* y;  // null: every row counts
+  const float* g;    // null: factor 1
+  int V;
+  __device__ bool ok(int r) const { return !y || (y[r] >= 0 && y[r] < V); }
+  __device__ float factor(int r) const { return g ? g[r] : 1.f; }
+};
+
+// Largest magnitudes of the columns of [R][K], over the rows r = blockIdx.y, + gridDim.y, ..: part[blockIdx.y][K].
+__global__ __launch_bounds__(256) void column_max(const float* src, int R, int K, RowFactor f, float* part) {
+  __shared__ float s[4][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k = blockIdx.x * 64 + lane;
+  float m = 0.f;
+  if (k < K)
+    for (int r = blockIdx.y * 4 + w; r < R; r += gridDim.y * 4)
+      if (f.ok(r)) m = fmaxf(m, fabsf(src[(size_t)r * K + k] * f.factor(r)));
+  s[w][lane] = m;
+  __syncthreads();
+  if (w == 0 && k < K) part[(size_t)blockIdx.y * K + k] = fmaxf(fmaxf(s[0][lane], s[1][lane]), fmaxf(s[2][lane], s[3][lane]));
+}
+
+// The columns of [R][K] as rows: dst[k][r], 64 x 64 values per block.
+template <class E>
+__global__ __launch_bounds__(256) void pack_cols(const E* src, int R, int K, RowFactor f, u16* dst, int units,
+                                                 const float* part, int parts, int* scale) {
+  __shared__ float s[64][65];
+  __shared__ int se[64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
+  if (sizeof(E) == 4 && w == 0) {
+    float m = 0.f;
+    if (k0 + lane < K)
+      for (int i = 0; i < parts; ++i) m = fmaxf(m, part[(size_t)i * K + k0 + lane]);
+    se[lane] = scale_of(m);
+    if (blockIdx.y == 0 && k0 + lane < K) scale[k0 + lane] = se[lane];
+  }
+  for (int i = w; i < 64; i += 4) {
+    const int r = r0 + i, k = k0 + lane;
+    s[i][lane] = r < R && k < K && f.ok(r) ? value(src[(size_t)r * K + k]) * f.factor(r) : 0.f;
+  }
+  __syncthreads();
+  for (int i = w; i < 64; i += 4) {
+    const int k = k0 + i, r = r0 + lane;
+    if (k >= K) break;
+    u16* d = dst + (size_t)k * units;
+    if constexpr (sizeof(E) == 2) {
+      if (r < units) d[r] = bf16_bits(s[lane][i]);
+    } else if (r < units / 2) {
+      u16 hi, lo;
+      split(ldexpf(s[lane][i], se[i]), hi, lo);
+      d += r / 32 * kChunk + r % 32;
+      d[0] = hi;
+      d[32] = lo;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Joins
+// ------------------------------------------------------------------------------------------------
+// lse and loss of a row from its tiles' (largest, sum): 16 rows by 16 runs of tiles per block.
+__global__ __launch_bounds__(256) void join_loss(const float2* part, int tiles, const float* target, const int32_t* y,
+                                                 int N, int V, float* loss, float* lse) {
+  __shared__ float2 s[16][16];
+  const int c = threadIdx.x & 15, w = threadIdx.x >> 4, n = blockIdx.x * 16 + c;
+  float m = -INFINITY, sum = 0.f;
+  if (n < N)
+    for (int t = w; t < tiles; t += 16) {
+      const float2 p = part[(size_t)t * N + n];
+      const float top = fmaxf(m, p.x), at = top == -INFINITY ? 0.f : top;
+      sum = sum * wnk::expf_fast(m - at) + p.y * wnk::expf_fast(p.x - at);
+      m = top;
+    }
+  s[w][c] = make_float2(m, sum);
+  __syncthreads();
+  if (w || n >= N) return;
+  for (int k = 1; k < 16; ++k) {
+    const float2 p = s[k][c];
+    const float top = fmaxf(m, p.x), at = top == -INFINITY ? 0.f : top;
+    sum = sum * wnk::expf_fast(m - at) + p.y * wnk::expf_fast(p.x - at);
+    m = top;
+  }
+  const float z = m + logf(sum);  // (no class at all: -inf)
+  lse[n] = z;
+  const int t = y[n];
+  loss[n] = t >= 0 && t < V ? z - target[n] : 0.f;
+}
+
+// out[i] = sum over the parts, in their order.
+template <class E>
+__global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float v = part[i];
+  for (int k = 1; k < parts; ++k) v += part[k * n + i];
+  put(out + i, v);
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void fill_zero(E* out, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) out[i] = (E)0;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Host
+// ------------------------------------------------------------------------------------------------
+constexpr size_t kForwardPiece = (size_t)64 << 20;    // bytes of packed w in the forward pass
+constexpr size_t kBackwardPiece = (size_t)512 << 20;  // bytes of w's forms and q in the backward pass
+constexpr int kMaxN = 1 << 20, kMaxD = 1 << 16, kMaxV = 1 << 24;
+constexpr int kTarget = 512;      // blocks that fill the chip
+constexpr int kColumnParts = 32;  // of column_max
+
+bool sizes_ok(int dtype, int N, int D, int V) {
+  return (dtype == WN_F32 || dtype == WN_BF16) && N >= 0 && N <= kMaxN && D >= 1 && D <= kMaxD && V >= 1 && V <= kMaxV;
+}
+
+// Tiles of 256 x 256 where they fill the chip, else 128 x 128.
+bool use_big(size_t a, size_t b) { return ceil_div(a, 256) * ceil_div(b, 256) >= 256; }
+
+// Classes of a piece: a multiple of 256, pieces alike, `each` bytes a class.
+int piece_classes(int V, size_t each, size_t budget) {
+  size_t most = budget / each / 256 * 256;
+  most = std::max<size_t>(256, most);
+  const size_t pieces = ceil_div(V, most);
+  return (int)std::min<size_t>(ceil_div(ceil_div(V, pieces), 256) * 256, ceil_div(V, 256) * 256);
+}
+
+struct Carve {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t off = at;
+    at += up256(bytes);
+    return off;
+  }
+};
+
+// The workspace's parts, with room for every form that a call with these sizes may take.
+struct Forward {
+  int piece;  // classes
+  size_t part, target, x, ex, w, ew, total;
+  Forward(bool sp, int N, int D, int V) {
+    const size_t units = padded_units(D, sp);
+    Carve c;
+    piece = piece_classes(V, units * 2 + 4, kForwardPiece);
+    part = c.take(ceil_div(V, 128) * N * sizeof(float2));
+    target = c.take((size_t)N * 4);
+    x = c.take((size_t)N * units * 2);
+    ex = c.take((size_t)N * 4);
+    w = c.take(std::min(piece, V) * units * 2);
+    ew = c.take((size_t)piece * 4);
+    total = c.at;
+  }
+};
+
+// How many parts the sum over k of a product is taken in: enough that its tiles fill the chip, each of 8 chunks
+// at least.
+int splits_for(size_t a, size_t b, int units) {
+  const size_t t = use_big(a, b) ? ceil_div(a, 256) * ceil_div(b, 256) : ceil_div(a, 128) * ceil_div(b, 128);
+  const size_t chunks = ceil_div(units, kChunk);
+  return (int)std::max<size_t>(1, std::min(kTarget / t, chunks / 8));
+}
+
+struct Backward {
+  int piece;
+  int sx, sw;  // splits of dx and dw
+  size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, db, cmax, dx, dw, total;
+  Backward(bool sp, int N, int D, int V) {
+    const size_t ud = padded_units(D, sp), un = padded_units(N, sp), e = sp ? 4 : 2;
+    piece = std::min(V, piece_classes(V, ud * 2 + D * e + 2 * un * 2, kBackwardPiece));
+    const size_t uv = padded_units(piece, sp);
+    sx = splits_for(D, N, (int)uv);
+    sw = splits_for(D, piece, (int)un);
+    Carve c;
+    x = c.take((size_t)N * ud * 2);
+    ex = c.take((size_t)N * 4);
+    xt = c.take((size_t)D * un * 2);
+    ext = c.take((size_t)D * 4);
+    w = c.take((size_t)piece * ud * 2);
+    ew = c.take((size_t)piece * 4);
+    wt = c.take((size_t)D * uv * 2);
+    ewt = c.take((size_t)D * 4);
+    q = c.take((size_t)N * uv * 2);
+    qt = c.take((size_t)piece * un * 2);
+    db = c.take(ceil_div(N, 128) * piece * 4);
+    cmax = c.take((size_t)kColumnParts * D * 4);
+    const bool whole = piece == V;
+    dx = c.take(whole && sx == 1 ? 0 : (size_t)sx * N * D * 4);
+    dw = c.take(sw == 1 ? 0 : (size_t)sw * piece * D * 4);
+    total = c.at;
+  }
+};
+
+template <class T, bool SP, class End>
+hipError_t launch_product(Product g, const End& end, hipStream_t st) {
+  g.ta = (int)ceil_div(g.a.rows, T::TA);
+  g.tb = (int)ceil_div(g.b.rows, T::TB);
+  const int kc = (int)ceil_div(std::max(g.a.k, g.b.k), kChunk);
+  g.cps = (int)ceil_div(kc, g.splits);
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(product<T, SP, End>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((product<T, SP, End>), dim3((unsigned)g.ta * g.tb * g.splits), dim3(T::kThreads), T::kLds, st, g, end);
+  return hipGetLastError();
+}
+
+// Rows of the tile are a tile's rows in `part` and `db`: big says which.
+template <bool SP, class End>
+hipError_t run_product(const Product& g, bool big, const End& end, hipStream_t st) {
+  return big ? launch_product<Big, SP>(g, end, st) : launch_product<Small, SP>(g, end, st);
+}
+
+// [R][K] as an operand: as it lies, or packed into `dst`.
+template <class E>
+Operand rows_operand(const E* src, int R, int K, u16* dst, int* scale, hipStream_t st) {
+  constexpr bool sp = sizeof(E) == 4;
+  if (!sp && K % 8 == 0 && reinterpret_cast<uintptr_t>(src) % 16 == 0) return {reinterpret_cast<const u16*>(src), R, K, K};
+  const int units = padded_units(K, sp);
+  hipLaunchKernelGGL(pack_rows<E>, dim3((unsigned)ceil_div(R, 4)), dim3(256), 0, st, src, R, K, dst, units, scale);
+  return {dst, R, units, units};
+}
+
+template <class E>
+Operand cols_operand(const E* src, int R, int K, const RowFactor& f, u16* dst, float* part, int* scale, hipStream_t st) {
+  constexpr bool sp = sizeof(E) == 4;
+  const int units = padded_units(R, sp);
+  const int parts = (int)std::min<size_t>(kColumnParts, ceil_div(R, 64));
+  const unsigned kb = (unsigned)ceil_div(K, 64);
+  if constexpr (sp)
+    hipLaunchKernelGGL(column_max, dim3(kb, parts), dim3(256), 0, st, src, R, K, f, part);
+  hipLaunchKernelGGL(pack_cols<E>, dim3(kb, (unsigned)ceil_div(R, 64)), dim3(256), 0, st, src, R, K, f, dst, units, part, parts, scale);
+  return {dst, K, units, units};
+}
+
+template <class E>
+int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, const int32_t* y, float* loss, float* lse,
+                char* ws, hipStream_t st) {
+  constexpr bool sp = sizeof(E) == 4;
+  const Forward f(sp, N, D, V);
+  int* const ex = reinterpret_cast<int*>(ws + f.ex);
+  int* const ew = reinterpret_cast<int*>(ws + f.ew);
+  u16* const wp = reinterpret_cast<u16*>(ws + f.w);
+  const Operand ox = rows_operand(x, N, D, reinterpret_cast<u16*>(ws + f.x), ex, st);
+  const bool direct = !sp && D % 8 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
+  const int piece = direct ? V : f.piece;
+  int tiles = 0;
+  for (int v0 = 0; v0 < V; v0 += piece) {
+    const int n = std::min(piece, V - v0);
+    const Operand ow = rows_operand(w + (size_t)v0 * D, n, D, wp, ew, st);
+    const bool big = use_big(n, N);
+    StatsEnd end{{sp ? ex : nullptr, sp ? ew : nullptr, b ? b + v0 : nullptr, y, N, n, v0, V},
+                 reinterpret_cast<float2*>(ws + f.part), tiles, reinterpret_cast<float*>(ws + f.target)};
+    const hipError_t e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
+    if (e != hipSuccess) return wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+    tiles += (int)ceil_div(n, big ? 256 : 128);
+  }
+  hipLaunchKernelGGL(join_loss, dim3((unsigned)ceil_div(N, 16)), dim3(256), 0, st, reinterpret_cast<const float2*>(ws + f.part),
+                     tiles, reinterpret_cast<const float*>(ws + f.target), y, N, V, loss, lse);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+}
+
+template <class E>
+hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st) {
+  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out);
+  return hipGetLastError();
+}
+
+template <class E>
+int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, const int32_t* y, const float* lse,
+                 const float* g, E* dx, E* dw, float* db, char* ws, hipStream_t st) {
+  constexpr bool sp = sizeof(E) == 4;
+  const Backward f(sp, N, D, V);
+  auto ints = [&](size_t off) { return reinterpret_cast<int*>(ws + off); };
+  auto units = [&](size_t off) { return reinterpret_cast<u16*>(ws + off); };
+  auto floats = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  const Operand ox = rows_operand(x, N, D, units(f.x), ints(f.ex), st);
+  Operand oxt{};
+  // (bf16: q holds g; fp32: x transposed does, so that q stays within its scale)
+  if (dw) oxt = cols_operand(x, N, D, RowFactor{y, sp ? g : nullptr, V}, units(f.xt), floats(f.cmax), ints(f.ext), st);
+  hipError_t e = hipGetLastError();
+  for (int v0 = 0; v0 < V && e == hipSuccess; v0 += f.piece) {
+    const int n = std::min(f.piece, V - v0);
+    const E* wv = w + (size_t)v0 * D;
+    const int ldq = padded_units(n, sp), ldqt = padded_units(N, sp);
+    const Operand ow = rows_operand(wv, n, D, units(f.w), ints(f.ew), st);
+    bool big = use_big(n, N);
+    GradEnd<sp> end{{sp ? ints(f.ex) : nullptr, sp ? ints(f.ew) : nullptr, b ? b + v0 : nullptr, y, N, n, v0, V},
+                    lse, g, dx ? units(f.q) : nullptr, dw ? units(f.qt) : nullptr, ldq, ldqt, db ? floats(f.db) : nullptr};
+    e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
+    if (e == hipSuccess && db) e = join(floats(f.db), (int)ceil_div(N, big ? 256 : 128), n, db + v0, st);
+    if (e == hipSuccess && dx) {
+      const Operand owt = cols_operand(wv, n, D, RowFactor{nullptr, nullptr, 0}, units(f.wt), floats(f.cmax), ints(f.ewt), st);
+      const bool whole = f.piece == V && f.sx == 1;
+      OutEnd o{D, N, sp ? ints(f.ewt) : nullptr, y, sp ? g : nullptr, V, whole ? nullptr : floats(f.dx), v0 > 0, dx, !sp};
+      e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.sx, 0}, use_big(D, N), o, st);
+      if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.sx, (size_t)N * D, dx, st);
+    }
+    if (e == hipSuccess && dw) {
+      E* const out = dw + (size_t)v0 * D;
+      OutEnd o{D, n, sp ? ints(f.ext) : nullptr, nullptr, nullptr, 1, f.sw == 1 ? nullptr : floats(f.dw), 0, out, !sp};
+      e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.sw, 0}, use_big(D, n), o, st);
+      if (e == hipSuccess && f.sw > 1) e = join(floats(f.dw), f.sw, (size_t)n * D, out, st);
+    }
+  }
+  return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+}
+
+int check_sizes(int dtype, int N, int D, int V) {
+  const int rc = bad_dtype(dtype);
+  if (rc != WN_OK) return rc;
+  return sizes_ok(dtype, N, D, V) ? WN_OK : wn_set_last_error(WN_EINVAL, "N must be 0..2^20, D 1..2^16, V 1..2^24");
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wn_loss_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V) {
+  if (!sizes_ok(dtype, N, D, V) || N == 0) return 0;
+  return Forward(dtype == WN_F32, N, D, V).total;
+}
+
+size_t wn_loss_backward_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V) {
+  if (!sizes_ok(dtype, N, D, V) || N == 0) return 0;
+  return Backward(dtype == WN_F32, N, D, V).total;
+}
+
+int wn_loss(int32_t dtype, int32_t N, int32_t D, int32_t V, const void* x, const void* w, const float* b, const int32_t* y,
+            float* loss, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  wn_clear_last_error();
+  int rc = check_sizes(dtype, N, D, V);
+  if (rc != WN_OK || N == 0) return rc;
+  if (!x || !w || !y || !loss || !lse) return wn_set_last_error(WN_EINVAL, "null pointer");
+  rc = bad_workspace(workspace, ws_bytes, wn_loss_workspace_bytes(dtype, N, D, V));
+  if (rc != WN_OK) return rc;
+  ArrayScope scope;
+  const struct { const void* p; const char* name; } arrays[] = {{x, "x"}, {w, "w"}, {b, "b"}, {y, "y"}, {loss, "loss"},
+                                                                {lse, "lse"}, {workspace, "workspace"}};
+  for (const auto& a : arrays)
+    if (a.p && (rc = scope.check(a.p, a.name)) != WN_OK) return rc;
+  if ((rc = scope.enter()) != WN_OK) return rc;
+  char* const ws = static_cast<char*>(workspace);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == WN_F32)
+    return run_forward(N, D, V, static_cast<const float*>(x), static_cast<const float*>(w), b, y, loss, lse, ws, st);
+  return run_forward(N, D, V, static_cast<const u16*>(x), static_cast<const u16*>(w), b, y, loss, lse, ws, st);
+}
+
+int wn_loss_backward(int32_t dtype, int32_t N, int32_t D, int32_t V, const void* x, const void* w, const float* b,
+                     const int32_t* y, const float* lse, const float* g, void* dx, void* dw, float* db, void* workspace,
+                     size_t ws_bytes, void* stream) {
+  wn_clear_last_error();
+  int rc = check_sizes(dtype, N, D, V);
+  if (rc != WN_OK) return rc;
+  if (!dx && !dw && !db) return wn_set_last_error(WN_EINVAL, "no gradient is wanted");
+  if (N > 0 && (!x || !w || !y || !lse || !g)) return wn_set_last_error(WN_EINVAL, "null pointer");
+  if (N == 0 && !dw && !db) return WN_OK;
+  rc = bad_workspace(workspace, ws_bytes, wn_loss_backward_workspace_bytes(dtype, N, D, V));
+  if (rc != WN_OK) return rc;
+  ArrayScope scope;
+  const struct { const void* p; const char* name; } arrays[] = {
+      {N ? x : nullptr, "x"}, {N ? w : nullptr, "w"}, {N ? b : nullptr, "b"}, {N ? y : nullptr, "y"}, {N ? lse : nullptr, "lse"},
+      {N ? g : nullptr, "g"}, {N ? dx : nullptr, "dx"}, {dw, "dw"}, {db, "db"}, {N ? workspace : nullptr, "workspace"}};
+  for (const auto& a : arrays)
+    if (a.p && (rc = scope.check(a.p, a.name)) != WN_OK) return rc;
+  if ((rc = scope.enter()) != WN_OK) return rc;
+  char* const ws = static_cast<char*>(workspace);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (N == 0) {
+    if (dw && dtype == WN_F32) hipLaunchKernelGGL(fill_zero<float>, dim3(1024), dim3(256), 0, st, static_cast<float*>(dw), (size_t)V * D);
+    if (dw && dtype == WN_BF16) hipLaunchKernelGGL(fill_zero<u16>, dim3(1024), dim3(256), 0, st, static_cast<u16*>(dw), (size_t)V * D);
+    if (db) hipLaunchKernelGGL(fill_zero<float>, dim3(1024), dim3(256), 0, st, db, (size_t)V);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+  }
+  if (dtype == WN_F32)
+    return run_backward(N, D, V, static_cast<const float*>(x), static_cast<const float*>(w), b, y, lse, g,
+                        static_cast<float*>(dx), static_cast<float*>(dw), db, ws, st);
+  return run_backward(N, D, V, static_cast<const u16*>(x), static_cast<const u16*>(w), b, y, lse, g, static_cast<u16*>(dx),
+                      static_cast<u16*>(dw), db, ws, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,341 @@
+"""The loss of an output layer and its gradients (wn_loss, wn_loss_backward) against the formulas in 64 bits.
+
+Tolerances.  u = 2^-24 is fp32's half step.  A logit is a sum of D products x w and a bias; with
+S = sum |x w| its error is at most
+  bf16: D u S (products are exact in fp32)
+  fp32: 3 * 2^-22 S (each value is held to 2^-22 of itself or 2^-39 of its row's largest, and the product of the
+        two low parts, at most 2^-22 of the product, is left out) + 3 D u S + 2^-38 D max|x| max|w|
+plus u (|l| + |b|) for the bias: E.  exp(l - m) is off by a relative 2 E + 2^-23 (1 + |l - m|) (its argument's
+rounding twice, exp2's own last place) and the sum of V of them by (V / 2048 + 128) u (the lengths of the
+chains: 32 a lane, 16 the joins, then a tile of 128 in 16 parts), so
+  loss: 2 E + (V / 2048 + 128) u + 2^-22 (1 + |lse| + |l_y|)
+  p:    a relative d = 2 E + tol(lse) + 2^-22 (1 + |l - lse|)
+With A = sum |q w| (or over rows |q x|) over K terms, the gradients' products are off by
+  bf16: (2^-8 + K u) A for q's rounding and the sum, and 2^-8 of the result
+  fp32: (3 * 2^-22 + 3 K u) A + 2^-38 K max max, and 4 u of the result
+and by sum d |p| g |w| for q.  Probabilities and products below 2^-126, fp32's smallest normal value, may vanish:
+another 2^-126 (1 + max|w|) for each term.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _inputs(N, D, V, dtype, seed, bias=True, ignored=0.2, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn((N, D), generator=g) * std).to(dtype)
+    w = (torch.randn((V, D), generator=g) * 1.5 / D ** 0.5 / std).to(dtype)
+    b = torch.randn((V,), generator=g) if bias else None
+    y = torch.randint(0, V, (N,), generator=g, dtype=torch.int32)
+    off = torch.rand((N,), generator=g) < ignored
+    y[off] = torch.where(torch.arange(int(off.sum())) % 2 == 0, -1, V).to(torch.int32)
+    grad = torch.rand((N,), generator=g) / N - 0.2 / N
+    return x, w, b, y, grad
+
+
+def _formulas(x, w, b, y, grad):
+    """Results in 64 bits and the tolerances of each."""
+    f32 = x.dtype == torch.float32
+    N, D = x.shape
+    V = w.shape[0]
+    X, W = x.double(), w.double()
+    ok = (y >= 0) & (y < V)
+    B = torch.zeros(V, dtype=torch.float64, device=x.device) if b is None else b.double()
+    l = X @ W.t().contiguous() + B
+    S = X.abs() @ W.abs().t().contiguous()
+    far = 2.0 ** -38 * float(X.abs().max()) * float(W.abs().max())
+    fin = torch.where(torch.isfinite(l), l, torch.zeros_like(l))
+    E = ((3 * 2.0 ** -22 + 3 * D * U) * S + D * far if f32 else D * U * S) + U * (fin.abs() + torch.where(torch.isfinite(B), B, 0.0).abs())
+    lse = torch.logsumexp(l, dim=1)
+    yc = torch.where(ok, y, 0).long()[:, None]
+    ly = l.gather(1, yc)[:, 0]
+    loss = torch.where(ok, lse - ly, 0.0)
+    Em = E.max(dim=1).values
+    t_lse = Em + (V / 2048 + 128) * U + 2.0 ** -22 * (1 + lse.abs())
+    t_loss = 2 * Em + (V / 2048 + 128) * U + 2.0 ** -22 * (1 + lse.abs() + ly.abs())
+    p = (l - lse[:, None]).exp()
+    d = 2 * E + t_lse[:, None] + 2.0 ** -22 * (1 + (fin - lse[:, None]).abs())
+    gr = torch.where(ok, grad.double(), 0.0)[:, None]
+    q = p.clone()
+    q.scatter_add_(1, yc, -torch.ones_like(lse)[:, None])
+    q *= gr
+    dq = d * p * gr.abs()
+    out = {"loss": (loss, t_loss), "lse": (lse, t_lse)}
+    for name, a, c, qq, e in (("dx", q, W, q.abs(), dq), ("dw", q.t().contiguous(), X, q.abs().t().contiguous(), dq.t().contiguous())):
+        K = a.shape[1]
+        v, A = a @ c, qq @ c.abs()
+        if f32:
+            m = float(qq.max()) if name == "dw" else float(gr.abs().max())
+            t = (3 * 2.0 ** -22 + 3 * K * U) * A + 2.0 ** -38 * K * float(gr.abs().max()) * float(c.abs().max()) + 4 * U * v.abs()
+        else:
+            t = (2.0 ** -8 + K * U) * A + 2.0 ** -8 * v.abs()
+        out[name] = (v, t + e @ c.abs() + K * 2.0 ** -126 * (1 + float(c.abs().max())))
+    out["db"] = (q.sum(dim=0), dq.sum(dim=0) + N * U * q.abs().sum(dim=0) + N * 2.0 ** -126)
+    return out
+
+
+def _near(got, want, name):
+    v, t = want
+    got = got.double()
+    assert got.shape == v.shape, name
+    bad = ~((got - v).abs() <= t)
+    if bool(bad.any()):
+        at = tuple(int(i) for i in bad.nonzero()[0])
+        raise AssertionError("%s%s: %r, not %r within %.3g (%d of %d off)" % (name, at, float(got[at]), float(v[at]),
+                                                                        float(t[at]), int(bad.sum()), bad.numel()))
+
+
+def _check(x, w, b, y, grad, need=("dx", "dw", "db"), device="cuda"):
+    import paper_1702_07825_amd as wn
+    print("loss", tuple(x.shape), tuple(w.shape), x.dtype, flush=True)
+    want = _formulas(*(None if t is None else t.to(device) for t in (x, w, b, y, grad)))
+    X, W, B, Y, G = (None if t is None else t.cuda() for t in (x, w, b, y, grad))
+    loss, lse = wn.head_loss(X, W, Y, b=B)
+    got = wn.head_loss_backward(X, W, Y, lse, G, b=B, need=need)
+    _near(loss.to(device), want["loss"], "loss")
+    _near(lse.to(device), want["lse"], "lse")
+    for name, t in zip(("dx", "dw", "db"), got):
+        assert (t is None) == (name not in need)
+        if t is not None:
+            _near(t.to(device), want[name], name)
+    return loss, lse, got
+
+
+SIZES = [(1, 1, 1), (1, 64, 256), (1, 1000, 777), (2, 7, 5), (15, 64, 100), (16, 64, 256), (17, 65, 129), (33, 8, 2000),
+         (64, 32, 1000), (100, 100, 127), (127, 72, 128), (128, 128, 128), (129, 256, 257), (200, 100, 3001), (256, 256, 256),
+         (300, 513, 777), (1000, 64, 300), (2111, 40, 64)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,D,V", SIZES)
+def test_sizes(N, D, V, dtype):
+    _check(*_inputs(N, D, V, dtype, seed=N + D + V))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,D,V", [(4100, 300, 8200), (5, 2048, 20000), (16000, 32, 9000), (20000, 256, 256)])
+def test_large(N, D, V, dtype):
+    """Tiles that fill the chip; several pieces of the vocabulary forwards (5 rows) and backwards (16000); sums
+    over the rows in parts (20000)."""
+    _check(*_inputs(N, D, V, dtype, seed=3), device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_without_a_bias_and_each_gradient_alone(dtype):
+    args = _inputs(70, 48, 300, dtype, seed=5, bias=False)
+    _, _, all_ = _check(*args)
+    for i, k in enumerate(("dx", "dw", "db")):
+        _, _, got = _check(*args, need=(k,))
+        assert torch.equal(got[i], all_[i])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_padding_holds_anything(dtype):
+    """NaN and infinities in rows without a target, in their upstream gradients and in their lse: the other rows'
+    results are those of the call with zeros there."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(150, 72, 260, dtype, seed=6, ignored=0.4)
+    off = (y < 0) | (y >= 260)
+    clean = x.clone()
+    clean[off] = 0
+    bad = x.clone()
+    bad[off] = float("nan")
+    bad[off.nonzero()[0]] = float("inf")
+    grad_bad = grad.clone()
+    grad_bad[off] = float("nan")
+    _, _, want = _check(clean, w, b, y, grad)
+    X, W, B, Y = bad.cuda(), w.cuda(), b.cuda(), y.cuda()
+    loss, lse = wn.head_loss(X, W, Y, b=B)
+    assert not bool(loss[off.cuda()].any())
+    got = wn.head_loss_backward(X, W, Y, lse, grad_bad.cuda(), b=B)
+    assert not bool(got[0][off.cuda()].any())
+    for a, c in zip(got, want):
+        assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_no_row_has_a_target(dtype):
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(40, 24, 90, dtype, seed=7)
+    y[:] = -5
+    X, W, B, Y, G = (t.cuda() for t in (x, w, b, y, grad))
+    loss, lse = wn.head_loss(X, W, Y, b=B)
+    assert not bool(loss.any())
+    for t in wn.head_loss_backward(X, W, Y, lse, G, b=B):
+        assert not bool(t.any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("mask", [-float("inf"), torch.finfo(torch.float32).min], ids=["inf", "lowest"])
+def test_masked_classes(dtype, mask):
+    """Classes that a bias masks, whole tiles of them among them."""
+    x, w, b, y, grad = _inputs(90, 40, 700, dtype, seed=8, ignored=0)
+    b[100:600] = mask
+    b[0] = mask
+    y = torch.where((y >= 100) & (y < 600) | (y == 0), 650, y).to(torch.int32)
+    _check(x, w, b, y, grad)
+
+
+def test_a_masked_target_has_an_infinite_loss():
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(20, 40, 300, torch.float32, seed=9, ignored=0)
+    b[7] = -float("inf")
+    y[3] = 7
+    loss, lse = wn.head_loss(x.cuda(), w.cuda(), y.cuda(), b=b.cuda())
+    assert float(loss[3]) == float("inf") and bool(torch.isfinite(loss[:3]).all()) and bool(torch.isfinite(loss[4:]).all())
+    for t in wn.head_loss_backward(x.cuda(), w.cuda(), y.cuda(), lse, grad.cuda(), b=b.cuda()):
+        assert bool(torch.isfinite(t).all())
+
+
+def test_not_finite_values_show():
+    """A NaN in a row with a target reaches its loss and dw; an infinity in w every loss whose logit it raises (where x is
+    negative the logit is -inf, and the class has probability 0)."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(20, 40, 300, torch.float32, seed=10, ignored=0)
+    x[4, 5] = float("nan")
+    loss, lse = wn.head_loss(x.cuda(), w.cuda(), y.cuda(), b=b.cuda())
+    assert bool(torch.isnan(loss[4])) and int(torch.isnan(loss).sum()) == 1
+    assert bool(torch.isnan(wn.head_loss_backward(x.cuda(), w.cuda(), y.cuda(), lse, grad.cuda(), b=b.cuda())[1]).any())
+    w[9, 0] = float("inf")
+    assert not bool(torch.isfinite(wn.head_loss(x.cuda(), w.cuda(), y.cuda(), b=b.cuda())[0].cpu()[x[:, 0] > 0]).any())
+
+
+@pytest.mark.parametrize("std", [2.0 ** -100, 2.0 ** -30, 2.0 ** 30, 2.0 ** 100])
+def test_fp32_values_far_from_one(std):
+    """x of any size (w the other way): the fp16 parts are scaled row by row."""
+    _check(*_inputs(70, 48, 200, torch.float32, seed=11, std=std))
+
+
+def test_fp32_rows_of_unlike_sizes():
+    """Rows of x and w, and upstream gradients, that differ by powers of ten."""
+    x, w, b, y, grad = _inputs(64, 48, 200, torch.float32, seed=12)
+    x *= 10.0 ** torch.linspace(-8, 0, 64)[:, None]
+    w *= 10.0 ** torch.linspace(-8, 0, 200)[:, None]
+    grad *= 10.0 ** torch.linspace(-6, 6, 64)
+    _check(x, w, b, y, grad)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_large_logits(dtype):
+    """Logits of some hundreds: the largest is taken off before the exponentials."""
+    x, w, b, y, grad = _inputs(80, 64, 500, dtype, seed=13)
+    _check((x.float() * 100).to(dtype), w, b, y, grad)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,D,V", [(37, 64, 300), (20, 33, 150)])
+def test_arrays_that_start_anywhere(dtype, N, D, V):
+    """Inputs and outputs one element into their allocations; what lies around the outputs stays."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(N, D, V, dtype, seed=14)
+    loss, lse, want = _check(x, w, b, y, grad)
+
+    def at1(t):
+        s = torch.full((t.numel() + 2,), 7, dtype=t.dtype, device="cuda")
+        v = s[1:-1].view(t.shape)
+        v.copy_(t)
+        return s, v
+
+    (_, X), (_, W), (_, B), (_, Y), (_, G) = (at1(t) for t in (x, w, b, y, grad))
+    outs = [at1(torch.zeros_like(t)) for t in (loss, lse, *want)]
+    wn.head_loss(X, W, Y, b=B, loss=outs[0][1], lse=outs[1][1])
+    wn.head_loss_backward(X, W, Y, outs[1][1], G, b=B, dx=outs[2][1], dw=outs[3][1], db=outs[4][1])
+    for (s, v), t in zip(outs, (loss, lse, *want)):
+        assert torch.equal(v, t)
+        assert float(s[0]) == 7 and float(s[-1]) == 7
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_runs_on_another_stream_and_in_a_graph(dtype):
+    """Captured, replayed on new inputs with other work between, and on a stream of its own: the eager results."""
+    import paper_1702_07825_amd as wn
+    sets = [[None if t is None else t.cuda() for t in _inputs(100, 72, 400, dtype, seed=20 + k)] for k in range(3)]
+
+    def both(x, w, b, y, g):
+        loss, lse = wn.head_loss(x, w, y, b=b)
+        return [loss, lse, *wn.head_loss_backward(x, w, y, lse, g, b=b)]
+
+    want = [[t.clone() for t in both(*s)] for s in sets]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    x, w, b, y, g = sets[1]
+    loss, lse = wn.head_loss(x, w, y, b=b, stream=stream)
+    got = [loss, lse, *wn.head_loss_backward(x, w, y, lse, g, b=b, stream=stream)]
+    torch.cuda.current_stream().wait_stream(stream)
+    assert all(torch.equal(a, c) for a, c in zip(got, want[1]))
+    held = [t.clone() for t in sets[0]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = both(*held)
+    for k in (0, 1, 2, 1):
+        for h, t in zip(held, sets[k]):
+            h.copy_(t)
+        graph.replay()
+        torch.cuda.synchronize()
+        both(*sets[(k + 1) % 3])  # eager work between the replays
+        assert all(torch.equal(a, c) for a, c in zip(outs, want[k])), k
+
+
+def test_gradient_against_differences():
+    """sum g loss along a direction in x, w and b, from the losses themselves.  The function's third derivative
+    along it is at most 8 max|dl|^3 sum|g| with |dl| the logits' change per unit, so the central difference is off by
+    h^2 / 6 of that, and by the losses' rounding over h."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(40, 32, 120, torch.float32, seed=15)
+    g = torch.Generator().manual_seed(16)
+    dirs = [torch.randn(t.shape, generator=g) / t.numel() ** 0.5 for t in (x, w, b)]
+    X, W, B, Y, G = (t.cuda() for t in (x, w, b, y, grad))
+    loss, lse = wn.head_loss(X, W, Y, b=B)
+    dx, dw, db = wn.head_loss_backward(X, W, Y, lse, G, b=B)
+    for k, (t, d, got) in enumerate(zip((X, W, B), dirs, (dx, dw, db))):
+        d, h = d.cuda(), 2.0 ** -6
+        f = []
+        for s in (h, -h):
+            a = [X, W, B]
+            a[k] = t + s * d
+            f.append(float((G.double() * wn.head_loss(a[0], a[1], Y, b=a[2])[0].double()).sum()))
+        dl = float((d @ W.t() if k == 0 else X @ d.t() if k == 1 else d).abs().max())
+        weight = float(G.abs().sum())
+        tol = h * h / 6 * 8 * dl ** 3 * weight + 2e-5 * weight / h + 1e-6
+        assert abs((f[0] - f[1]) / (2 * h) - float((got.double() * d.double()).sum())) <= tol
+
+
+def test_the_same_call_twice_gives_the_same_bits():
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = (t.cuda() for t in _inputs(3000, 96, 5000, torch.bfloat16, seed=17))
+    got = []
+    for _ in range(3):
+        loss, lse = wn.head_loss(x, w, y, b=b)
+        got.append([loss, lse, *wn.head_loss_backward(x, w, y, lse, grad, b=b)])
+    for g in got[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(g, got[0]))
+
+
+def test_no_rows():
+    import paper_1702_07825_amd as wn
+    x, y = torch.empty((0, 16), device="cuda"), torch.empty((0,), dtype=torch.int32, device="cuda")
+    w, g = torch.ones((30, 16), device="cuda"), torch.empty((0,), device="cuda")
+    loss, lse = wn.head_loss(x, w, y)
+    assert loss.shape == (0,) and lse.shape == (0,)
+    dx, dw, db = wn.head_loss_backward(x, w, y, lse, g)
+    assert dx.shape == (0, 16) and not bool(dw.any()) and not bool(db.any())
+
+
+def test_refusals():
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = (t.cuda() for t in _inputs(8, 16, 30, torch.float32, seed=18))
+    lse = torch.zeros(8, device="cuda")
+    for kw in (dict(x=x.t()), dict(x=x.half()), dict(w=w.bfloat16()), dict(w=w[:, :8]), dict(y=y.long()), dict(y=y[:4]),
+               dict(b=b[:4]), dict(b=b.bfloat16()), dict(x=x.cpu()), dict(y=y.cpu()), dict(w=w[0])):
+        a = {**dict(x=x, w=w, y=y, b=b), **kw}
+        with pytest.raises((ValueError, TypeError)):
+            wn.head_loss(a["x"], a["w"], a["y"], b=a["b"])
+    for kw in (dict(need=()), dict(need=("dz",)), dict(dx=torch.zeros(3, device="cuda")), dict(grad=grad[:3]), dict(lse=lse[:3])):
+        a = {**dict(lse=lse, grad=grad, need=("dx",), dx=None), **kw}
+        with pytest.raises((ValueError, TypeError)):
+            wn.head_loss_backward(x, w, y, a["lse"], a["grad"], b=b, need=a["need"], dx=a["dx"])
+    with pytest.raises(wn.WnError):
+        wn.head_loss(x, w, y, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
