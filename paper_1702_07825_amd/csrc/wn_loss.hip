@@ -52,7 +52,10 @@ struct Tile {
   static constexpr int kStage = (TA + TB) * kChunk * 2;        // bytes of a chunk of both operands
   static constexpr int kLds = 2 * kStage;
   static constexpr int IA = TA * 8 / kThreads, IB = TB * 8 / kThreads;  // 16-byte pieces of a chunk per thread
+  static constexpr int kOccupancy = 2;  // waves of a SIMD
+  static_assert(NB <= NA, "the order of the reads in product");
 };
+constexpr int kBand = 8;
 using Big = Tile<256, 256, 2, 4>;
 using Small = Tile<128, 128, 2, 2>;
 
@@ -64,17 +67,29 @@ struct Place {
   int wa, wb, n, quad;
 };
 
+// Four 16-bit or fp32 values at any element's alignment.
+typedef u16 u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
 template <class T, bool SP, class End>
-__global__ __launch_bounds__(T::kThreads) void product(const Product g, const End end) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Product g, const End end) {
   extern __shared__ __align__(16) char lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Place pl;
   {
-    int t = blockIdx.x;
-    pl.split = t % g.splits;
-    t /= g.splits;
-    pl.ta = t % g.ta;
-    pl.tb = t / g.ta;
+    // Block b runs on XCD b mod 8.  Each XCD takes a run of tiles, in the order of bands of kBand tiles of b:
+    // the tiles it works on at a time share the operands' rows in its L2.
+    const int blocks = gridDim.x, xcd = blockIdx.x & 7, per = blocks >> 3, rem = blocks & 7;
+    int t = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
+    const int tiles = g.ta * g.tb;
+    pl.split = t / tiles;
+    t -= pl.split * tiles;
+    const int band = t / (kBand * g.ta), in = t - band * kBand * g.ta, wide = min(kBand, g.tb - band * kBand);
+    pl.ta = in / wide;
+    pl.tb = band * kBand + in - pl.ta * wide;
   }
   pl.wa = wave / T::WB;
   pl.wb = wave % T::WB;
@@ -91,14 +106,10 @@ __global__ __launch_bounds__(T::kThreads) void product(const Product g, const En
   };
   const rsrc ares = resource(g.a, (long long)pl.ta * T::TA, T::TA), bres = resource(g.b, (long long)pl.tb * T::TB, T::TB);
   // 16-byte piece `pos` of row r in LDS is piece pos ^ (r >> 1 & 7) of the row's chunk: the 16 rows that 16 lanes
-  // read at one piece then fall on different banks
-  int voff[T::IA + T::IB], piece[1];
-#pragma unroll
-  for (int i = 0; i < T::IA + T::IB; ++i) {
-    const int p = (i < T::IA ? i : i - T::IA) * T::kThreads + tid, r = p >> 3, c = (p & 7) ^ (r >> 1 & 7);
-    voff[i] = r * (i < T::IA ? g.a.ld : g.b.ld) * 2 + c * 16;
-  }
-  piece[0] = (tid & 7) ^ (tid >> 4 & 7);  // of every piece above: kThreads / 8 rows is a multiple of 16
+  // read at one piece then fall on different banks.  A thread's pieces are all at the same place of their rows
+  // (kThreads / 8 rows is a multiple of 16).
+  const int piece = (tid & 7) ^ (tid >> 4 & 7);
+  const int va = (tid >> 3) * g.a.ld * 2 + piece * 16, vb = (tid >> 3) * g.b.ld * 2 + piece * 16;
   const int kc = (max(g.a.k, g.b.k) + kChunk - 1) / kChunk;
   const int c0 = pl.split * g.cps, c1 = min(kc, c0 + g.cps);
   auto stage = [&](int c, char* to) {
@@ -106,9 +117,10 @@ __global__ __launch_bounds__(T::kThreads) void product(const Product g, const En
 #pragma unroll
     for (int i = 0; i < T::IA + T::IB; ++i) {
       const bool isa = i < T::IA;
-      const int at = ((isa ? i : i - T::IA) * T::kThreads + wave * 64) * 16 + (isa ? 0 : T::TA * kChunk * 2);
+      const int k = isa ? i : i - T::IA;
+      const int at = (k * T::kThreads + wave * 64) * 16 + (isa ? 0 : T::TA * kChunk * 2);
       // (a piece behind the row's values reads past the buffer's end, which gives 0)
-      const int v = piece[0] * 8 < (isa ? left : leftb) ? voff[i] : (int)0x80000000;
+      const int v = piece * 8 < (isa ? left : leftb) ? (isa ? va : vb) + k * (T::kThreads / 8) * (isa ? g.a.ld : g.b.ld) * 2 : (int)0x80000000;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(isa ? ares : bres, (lds_void*)(to + at), 16, v, c * kChunk * 2, 0, 0);
     }
   };
@@ -117,49 +129,70 @@ __global__ __launch_bounds__(T::kThreads) void product(const Product g, const En
   for (int i = 0; i < T::NA; ++i)
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (c0 < c1) stage(c0, lds);
+  typedef typename std::conditional<SP, f16x8, bf16x8>::type V8;
   const int sw = pl.n >> 1;
   const int fa = (ra + pl.n) * kChunk * 2, fb = (T::TA + rb + pl.n) * kChunk * 2;
   const int s0 = (pl.quad ^ sw) * 16, s1 = ((4 + pl.quad) ^ sw) * 16;
+  auto buffer = [&](int c) { return lds + ((c - c0) & 1) * T::kStage; };
+  auto get = [&](const char* at, int row, int s) { return *reinterpret_cast<const V8*>(at + row + s); };
+  constexpr int kRow = 16 * kChunk * 2;
+  // a chunk's first and second half of each operand's values (SP: hi and lo parts)
+  V8 a0[T::NA], a1[T::NA], b0[T::NB], b1[T::NB];
+  if (c0 < c1) {
+    stage(c0, buffer(c0));
+    if (c0 + 1 < c1) {
+      stage(c0 + 1, buffer(c0 + 1));
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(T::IA + T::IB) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    const char* at = buffer(c0);
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) b0[j] = get(at, fb + j * kRow, s0);
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i) a0[i] = get(at, fa + i * kRow, s0);
+  }
+  // A chunk in two halves, each half's operands read from LDS during the products of the half before.  The one
+  // barrier stands where a chunk's last reads are done: it lets the chunk after next into its buffer and says that the
+  // next one has arrived.
   for (int c = c0; c < c1; ++c) {
-    char* const at = lds + ((c - c0) & 1) * T::kStage;
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    if (c + 1 < c1) stage(c + 1, lds + ((c + 1 - c0) & 1) * T::kStage);
+    const char* at = buffer(c);
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i) {
+      a1[i] = get(at, fa + i * kRow, s1);
+      if (i < T::NB) b1[i] = get(at, fb + i * kRow, s1);
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) acc[i][j] = mma(a0[i], b0[j], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (c + 2 < c1) stage(c + 2, buffer(c));
+    at = buffer(c + 1);
     if constexpr (SP) {
-      f16x8 ah[T::NA], al[T::NA], bh[T::NB], bl[T::NB];
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
-        ah[i] = *reinterpret_cast<const f16x8*>(at + fa + i * 16 * kChunk * 2 + s0);
-        al[i] = *reinterpret_cast<const f16x8*>(at + fa + i * 16 * kChunk * 2 + s1);
+#pragma unroll
+        for (int j = 0; j < T::NB; ++j) acc[i][j] = mma(a1[i], b0[j], acc[i][j]);
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < T::NB; ++j) {
-        bh[j] = *reinterpret_cast<const f16x8*>(at + fb + j * 16 * kChunk * 2 + s0);
-        bl[j] = *reinterpret_cast<const f16x8*>(at + fb + j * 16 * kChunk * 2 + s1);
+      for (int i = 0; i < T::NA; ++i) {
+        if (i < T::NB) b0[i] = get(at, fb + i * kRow, s0);
+#pragma unroll
+        for (int j = 0; j < T::NB; ++j) acc[i][j] = mma(a0[i], b1[j], acc[i][j]);
+        a0[i] = get(at, fa + i * kRow, s0);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int i = 0; i < T::NA; ++i)
-#pragma unroll
-        for (int j = 0; j < T::NB; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
-        }
     } else {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        bf16x8 a[T::NA], b[T::NB];
+      for (int i = 0; i < T::NA; ++i) {
+        a0[i] = get(at, fa + i * kRow, s0);
+        if (i < T::NB) b0[i] = get(at, fb + i * kRow, s0);
 #pragma unroll
-        for (int i = 0; i < T::NA; ++i) a[i] = *reinterpret_cast<const bf16x8*>(at + fa + i * 16 * kChunk * 2 + (s ? s1 : s0));
-#pragma unroll
-        for (int j = 0; j < T::NB; ++j) b[j] = *reinterpret_cast<const bf16x8*>(at + fb + j * 16 * kChunk * 2 + (s ? s1 : s0));
-#pragma unroll
-        for (int i = 0; i < T::NA; ++i)
-#pragma unroll
-          for (int j = 0; j < T::NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < T::NB; ++j) acc[i][j] = mma(a1[i], b1[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
   __syncthreads();
   end.template operator()<T>(acc, pl, lds);
@@ -258,7 +291,9 @@ __device__ __forceinline__ void split(float v, u16& hi, u16& lo) {
 }
 
 // Backward: q of the tile's rows and classes as the operands of dx ([n][v]) and dw ([v][n]), and the sums of g q
-// over the tile's rows.  fp32: q without g (|q| <= 1); bf16: g q.
+// over the tile's rows.  fp32: q without g (|q| <= 1); bf16: g q.  A lane holds four classes of a row, so [n][v] is
+// stored from the registers (32-byte runs); [v][n] goes through LDS, a wave's classes by 64 rows (fp32: 32 rows,
+// hi and lo parts) at a time, so that its stores are runs of 128 bytes.
 template <bool SP>
 struct GradEnd {
   Logits l;
@@ -269,25 +304,56 @@ struct GradEnd {
   template <class T>
   __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
     l.take<T>(acc, pl);
-    float* const s = reinterpret_cast<float*>(lds);  // [WB][TA]
-    float gn[T::NB];
+    constexpr int RA = 16 * T::NA, RB = 16 * T::NB;  // the wave's classes and rows
+    static_assert(RB == 64, "a row of the transposed tile is 128 bytes");
+    char* const tr = lds + (pl.wa * T::WB + pl.wb) * RA * 128;
+    const int lane = threadIdx.x & 63;
+    // Two lanes that hold neighbouring rows (n even, n + 1) swap two of their four classes: the even lane then holds
+    // classes 0 and 1 of both rows, the odd one classes 2 and 3, and each writes pairs.
+    const bool odd = lane & 1;
+    auto swap = [&](u16 (&v)[4], unsigned& p0, unsigned& p1) {
+      const unsigned lo = (unsigned)v[0] | (unsigned)v[1] << 16, hi = (unsigned)v[2] | (unsigned)v[3] << 16;
+      const unsigned give = odd ? lo : hi, keep = odd ? hi : lo;
+      const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give, 0xB1, 0xf, 0xf, false);
+      const unsigned e = odd ? got : keep, o = odd ? keep : got;  // of the even and the odd row
+      p0 = (e & 0xffffu) | o << 16;
+      p1 = e >> 16 | (o & 0xffff0000u);
+    };
+    // piece (16 bytes) of row v of the transposed tile, as it lies
+    auto place = [](int v, int piece) { return v * 128 + ((piece ^ (v >> 1 & 7)) << 4); };
+    auto put_pair = [&](int i, int col, u16 (&v)[4]) {  // col: unit of the row's first of the two
+      unsigned p0, p1;
+      swap(v, p0, p1);
+      const int r = 16 * i + 4 * pl.quad + (odd ? 2 : 0);
+      *reinterpret_cast<unsigned*>(tr + place(r, col >> 3) + (col & 7) * 2) = p0;
+      *reinterpret_cast<unsigned*>(tr + place(r + 1, col >> 3) + (col & 7) * 2) = p1;
+    };
+    auto store_rows = [&](int units) {  // the transposed tile's rows to qt, from unit `units` of them
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own part of LDS)
+#pragma unroll 4
+      for (int k = 0; k < RA / 8; ++k) {
+        const int r = 8 * k + (lane >> 3), v = pl.a0 + r, piece = lane & 7;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(tr + place(r, piece));
+        if (v < l.V && units + 8 * piece < ldqt) *reinterpret_cast<u32x4*>(qt + (size_t)v * ldqt + units + 8 * piece) = x;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
       const int n = pl.b0 + 16 * j + pl.n;
       const int yn = n < l.N ? l.y[n] : -1;
       const bool ok = yn >= 0 && yn < l.V_all;
       const int t = ok ? yn - l.v0 : -1;
-      const float ln = ok ? lse[n] : 0.f;
-      gn[j] = ok ? g[n] : 0.f;
+      const float ln = ok ? lse[n] : 0.f, gn = ok ? g[n] : 0.f;
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
         const int v = pl.a0 + 16 * i + 4 * pl.quad;
         f32x4 p;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = ok ? wnk::expf_fast(acc[i][j][e] - ln) - (v + e == t ? 1.f : 0.f) : 0.f;
-          if (v + e >= l.V) p[e] = 0.f;
-          acc[i][j][e] = ok ? p[e] * gn[j] : 0.f;
+          p[e] = wnk::expf_fast(acc[i][j][e] - ln) - (v + e == t ? 1.f : 0.f);
+          p[e] = ok && v + e < l.V ? p[e] : 0.f;
+          acc[i][j][e] = p[e] * gn;
         }
         if constexpr (SP) {
           u16 hi[4], lo[4];
@@ -298,26 +364,26 @@ struct GradEnd {
             *reinterpret_cast<u32x2*>(d) = u32x2{(unsigned)hi[0] | (unsigned)hi[1] << 16, (unsigned)hi[2] | (unsigned)hi[3] << 16};
             *reinterpret_cast<u32x2*>(d + 32) = u32x2{(unsigned)lo[0] | (unsigned)lo[1] << 16, (unsigned)lo[2] | (unsigned)lo[3] << 16};
           }
-          if (qt && n < ldqt / 2)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v + e < l.V) {
-                u16* d = qt + (size_t)(v + e) * ldqt + n / 32 * kChunk + n % 32;
-                d[0] = hi[e];
-                d[32] = lo[e];
-              }
+          if (qt) {
+            put_pair(i, 16 * (j & 1) + (pl.n & ~1), hi);
+            put_pair(i, 32 + 16 * (j & 1) + (pl.n & ~1), lo);
+          }
         } else {
+          u16 h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = bf16_bits(acc[i][j][e]);
           if (q && n < l.N && v < ldq)
             *reinterpret_cast<u32x2*>(q + (size_t)n * ldq + v) =
-                u32x2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
-          if (qt && n < ldqt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v + e < l.V) qt[(size_t)(v + e) * ldqt + n] = bf16_bits(acc[i][j][e]);
+                u32x2{(unsigned)h[0] | (unsigned)h[1] << 16, (unsigned)h[2] | (unsigned)h[3] << 16};
+          if (qt) put_pair(i, 16 * j + (pl.n & ~1), h);
         }
       }
+      if (SP && qt && j & 1) store_rows((pl.b0 + 16 * (j - 1)) * 2);
     }
+    if (!SP && qt) store_rows(pl.b0);
     if (!db) return;
+    __syncthreads();
+    float* const s = reinterpret_cast<float*>(lds);  // [WB][TA]
 #pragma unroll
     for (int i = 0; i < T::NA; ++i)
 #pragma unroll
@@ -340,46 +406,68 @@ struct GradEnd {
 };
 
 // dx and dw: out[b][a] (rows of D).
+template <class E>
 struct OutEnd {
   int A, B;           // D, rows
-  const int* ea;      // scales of operand A's rows, or null; then the product is acc 2^-(ea[a] + kQScale)
+  const int* ea;      // fp32: scales of operand A's rows; the product is acc 2^-(ea[a] + kQScale)
   const int32_t* y;   // dx: rows whose y is outside 0 .. V-1 are 0; or null
-  const float* g;     // fp32 dx: the row's factor, or null
+  const float* g;     // fp32 dx: the row's factor; or null
   int V;
   float* sum;         // [splits][B][A], set (add = 0) or added to; or null
   int add;
-  void* out;          // where sum is null
-  int bf16;
+  E* out;             // where sum is null
   template <class T>
   __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char*) const {
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int s = -(ea[min(pl.a0 + 16 * i + 4 * pl.quad + e, A - 1)] + kQScale);
+#pragma unroll
+          for (int j = 0; j < T::NB; ++j) acc[i][j][e] = ldexpf(acc[i][j][e], s);
+        }
+    }
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
       const int b = pl.b0 + 16 * j + pl.n;
-      if (b >= B) continue;
-      const int yb = y ? y[b] : 0;
-      const bool ok = yb >= 0 && yb < V;
-      const float f = g && ok ? g[b] : 1.f;
+      const bool in = b < B;
+      float f = 1.f;
+      bool ok = true;
+      if (y) {
+        const int yb = in ? y[b] : -1;
+        ok = yb >= 0 && yb < V;
+        if (g && ok) f = g[b];
+      }
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
         const int a = pl.a0 + 16 * i + 4 * pl.quad;
-        f32x4 v = acc[i][j];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (ea) v[e] = ldexpf(v[e], -(ea[min(a + e, A - 1)] + kQScale)) * f;
-          if (!ok) v[e] = 0.f;
-        }
+        f32x4 v = acc[i][j] * f;
+        if (!ok) v = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (!in) continue;
         if (sum) {
           float* d = sum + ((size_t)pl.split * B + b) * A + a;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (a + e < A) d[e] = add ? d[e] + v[e] : v[e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (a + e < A) {
-              if (bf16) static_cast<u16*>(out)[(size_t)b * A + a + e] = bf16_bits(v[e]);
-              else static_cast<float*>(out)[(size_t)b * A + a + e] = v[e];
+          if (a + 3 < A) {
+            if (add) {
+              const f32x4u o = *reinterpret_cast<const f32x4u*>(d);
+              v += f32x4{o[0], o[1], o[2], o[3]};
             }
+            *reinterpret_cast<f32x4u*>(d) = f32x4u{v[0], v[1], v[2], v[3]};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (a + e < A) d[e] = add ? d[e] + v[e] : v[e];
+          }
+        } else {
+          E* d = out + (size_t)b * A + a;
+          if (a + 3 < A) {
+            if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(d) = f32x4u{v[0], v[1], v[2], v[3]};
+            else *reinterpret_cast<u16x4u*>(d) = u16x4u{bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3])};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (a + e < A) put(d + e, v[e]);
+          }
         }
       }
     }
@@ -709,13 +797,13 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
     if (e == hipSuccess && dx) {
       const Operand owt = cols_operand(wv, n, D, RowFactor{nullptr, nullptr, 0}, units(f.wt), floats(f.cmax), ints(f.ewt), st);
       const bool whole = f.piece == V && f.sx == 1;
-      OutEnd o{D, N, sp ? ints(f.ewt) : nullptr, y, sp ? g : nullptr, V, whole ? nullptr : floats(f.dx), v0 > 0, dx, !sp};
+      const OutEnd<E> o{D, N, ints(f.ewt), y, sp ? g : nullptr, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
       e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.sx, 0}, use_big(D, N), o, st);
       if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.sx, (size_t)N * D, dx, st);
     }
     if (e == hipSuccess && dw) {
       E* const out = dw + (size_t)v0 * D;
-      OutEnd o{D, n, sp ? ints(f.ext) : nullptr, nullptr, nullptr, 1, f.sw == 1 ? nullptr : floats(f.dw), 0, out, !sp};
+      const OutEnd<E> o{D, n, ints(f.ext), nullptr, nullptr, 1, f.sw == 1 ? nullptr : floats(f.dw), 0, out};
       e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.sw, 0}, use_big(D, n), o, st);
       if (e == hipSuccess && f.sw > 1) e = join(floats(f.dw), f.sw, (size_t)n * D, out, st);
     }
