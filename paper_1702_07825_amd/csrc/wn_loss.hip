@@ -112,17 +112,24 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
   const int va = (tid >> 3) * g.a.ld * 2 + piece * 16, vb = (tid >> 3) * g.b.ld * 2 + piece * 16;
   const int kc = (max(g.a.k, g.b.k) + kChunk - 1) / kChunk;
   const int c0 = pl.split * g.cps, c1 = min(kc, c0 + g.cps);
+  auto stage_piece = [&](int c, char* to, int i) {
+    const bool isa = i < T::IA;
+    const int k = isa ? i : i - T::IA;
+    const int at = (k * T::kThreads + wave * 64) * 16 + (isa ? 0 : T::TA * kChunk * 2);
+    // (a piece behind the row's values reads past the buffer's end, which gives 0)
+    const int v = piece * 8 < (isa ? g.a.k : g.b.k) - c * kChunk ? (isa ? va : vb) + k * (T::kThreads / 8) * (isa ? g.a.ld : g.b.ld) * 2 : (int)0x80000000;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(isa ? ares : bres, (lds_void*)(to + at), 16, v, c * kChunk * 2, 0, 0);
+  };
+  constexpr int kPieces = T::IA + T::IB;
   auto stage = [&](int c, char* to) {
-    const int left = g.a.k - c * kChunk, leftb = g.b.k - c * kChunk;
 #pragma unroll
-    for (int i = 0; i < T::IA + T::IB; ++i) {
-      const bool isa = i < T::IA;
-      const int k = isa ? i : i - T::IA;
-      const int at = (k * T::kThreads + wave * 64) * 16 + (isa ? 0 : T::TA * kChunk * 2);
-      // (a piece behind the row's values reads past the buffer's end, which gives 0)
-      const int v = piece * 8 < (isa ? left : leftb) ? (isa ? va : vb) + k * (T::kThreads / 8) * (isa ? g.a.ld : g.b.ld) * 2 : (int)0x80000000;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(isa ? ares : bres, (lds_void*)(to + at), 16, v, c * kChunk * 2, 0, 0);
-    }
+    for (int i = 0; i < kPieces; ++i) stage_piece(c, to, i);
+  };
+  // the pieces that step i of T::NA issues
+  auto stage_part = [&](int c, char* to, int i) {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      if (k * T::NA / kPieces == i) stage_piece(c, to, k);
   };
   f32x4 acc[T::NA][T::NB];
 #pragma unroll
@@ -153,10 +160,12 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
     for (int i = 0; i < T::NA; ++i) a0[i] = get(at, fa + i * kRow, s0);
   }
   // A chunk in two halves, each half's operands read from LDS during the products of the half before.  The one
-  // barrier stands where a chunk's last reads are done: it lets the chunk after next into its buffer and says that the
-  // next one has arrived.
+  // barrier stands where a chunk's last reads are done: it lets the chunk after next into its buffer, whose loads are
+  // spread over the second half's products, and says that the next one has arrived.
   for (int c = c0; c < c1; ++c) {
     const char* at = buffer(c);
+    char* const to = buffer(c);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < T::NA; ++i) {
       a1[i] = get(at, fa + i * kRow, s1);
@@ -165,10 +174,13 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
       for (int j = 0; j < T::NB; ++j) acc[i][j] = mma(a0[i], b0[j], acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (c + 2 < c1) stage(c + 2, buffer(c));
+    const bool more = c + 2 < c1;
     at = buffer(c + 1);
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (SP) {
+      if (more) stage(c + 2, to);  // (spread over the products they spill)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
 #pragma unroll
@@ -186,6 +198,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
     } else {
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
+        if (more) stage_part(c + 2, to, i);
         a0[i] = get(at, fa + i * kRow, s0);
         if (i < T::NB) b0[i] = get(at, fb + i * kRow, s0);
 #pragma unroll
@@ -193,6 +206,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
   }
   __syncthreads();
   end.template operator()<T>(acc, pl, lds);
@@ -205,24 +219,68 @@ struct Logits {
   const int32_t* y;
   int N, V, v0, V_all;  // rows; classes of the piece, the first of them, and of the layer
   template <class T>
-  __device__ void take(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
+  __device__ __forceinline__ void take(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
+    if (ew) {
+      int sn[T::NB];
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) sn[j] = ex[min(pl.b0 + 16 * j + pl.n, N - 1)];
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int sv = ew[min(pl.a0 + 16 * i + 4 * pl.quad + e, V - 1)];
+#pragma unroll
+          for (int j = 0; j < T::NB; ++j) acc[i][j][e] = ldexpf(acc[i][j][e], -(sv + sn[j]));
+        }
+    }
+    if (bias) {
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float bv = bias[min(pl.a0 + 16 * i + 4 * pl.quad + e, V - 1)];
+#pragma unroll
+          for (int j = 0; j < T::NB; ++j) acc[i][j][e] += bv;
+        }
+    }
+    if (pl.a0 + 16 * T::NA > V) {  // the last tile: no classes behind V
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = pl.a0 + 16 * i + 4 * pl.quad + e < V;
+#pragma unroll
+          for (int j = 0; j < T::NB; ++j) acc[i][j][e] = in ? acc[i][j][e] : -INFINITY;
+        }
+    }
+  }
+  // Calls f(i, e) where this lane holds class t (of the piece) as its output i, e of a row; few waves hold any
+  // row's target, so the search is skipped where none does.
+  template <class T, class F>
+  __device__ __forceinline__ static void at_target(const Place& pl, int t, F f) {
+    const int r = t - pl.a0 - 4 * pl.quad;
+    if (!__any(t >= pl.a0 && t < pl.a0 + 16 * T::NA)) return;
 #pragma unroll
     for (int i = 0; i < T::NA; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int v = pl.a0 + 16 * i + 4 * pl.quad + e, vc = min(v, V - 1);
-        const float bv = bias ? bias[vc] : 0.f;
-        const int sv = ew ? ew[vc] : 0;
-#pragma unroll
-        for (int j = 0; j < T::NB; ++j) {
-          const int n = min(pl.b0 + 16 * j + pl.n, N - 1);
-          float l = acc[i][j][e];
-          if (ew) l = ldexpf(l, -(sv + ex[n]));
-          acc[i][j][e] = v < V ? l + bv : -INFINITY;
-        }
-      }
+      for (int e = 0; e < 4; ++e)
+        if (r == 16 * i + e) f(i, e);
   }
 };
+
+// exp(l - at) as 2^(l log2 e - at log2 e): the product of `at` is the row's.  Where `at` is so large that it would
+// overflow (every class of the row masked by fp32's lowest value), `at` is taken off the logits first.
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float exp_from(float l, float at_log2e) { return __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -at_log2e)); }
+template <class T>
+__device__ __forceinline__ float take_off_far(f32x4 (&acc)[T::NA][T::NB], int j, float at) {
+  const bool far = fabsf(at) > 1e37f && fabsf(at) < INFINITY;
+  if (__any(far)) {
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i) acc[i][j] -= far ? at : 0.f;
+  }
+  return far ? 0.f : at * kLog2e;
+}
 
 __device__ __forceinline__ float across_quads_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
@@ -246,23 +304,18 @@ struct StatsEnd {
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
       const int n = pl.b0 + 16 * j + pl.n;
-      const int t = n < l.N ? l.y[n] - l.v0 : -1;
+      const int t = n < l.N ? l.y[n] - l.v0 : -1;  // (no class behind the piece is a target of it: at_target stops at V)
       float m = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < T::NA; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = acc[i][j][e];
-          m = fmaxf(m, v);
-          if (t == pl.a0 + 16 * i + 4 * pl.quad + e) target[n] = v;  // (t < V: v0 + V is a tile's end or the last class)
-        }
+      for (int i = 0; i < T::NA; ++i) m = fmaxf(fmaxf(fmaxf(m, acc[i][j][0]), acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
       m = across_quads_max(m);
+      Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { target[n] = acc[i][j][e]; });
       // (a row without a class yet: every exponential is 0, not exp(-inf + inf))
-      const float at = m == -INFINITY ? 0.f : m;
+      const float at = take_off_far<T>(acc, j, m == -INFINITY ? 0.f : m);
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += wnk::expf_fast(acc[i][j][e] - at);
+        for (int e = 0; e < 4; ++e) sum += exp_from(acc[i][j][e], at);
       sum = across_quads_sum(sum);
       if (pl.quad == 0) s[pl.wa * T::TB + pl.wb * (T::TB / T::WB) + 16 * j + pl.n] = make_float2(m, sum);
     }
@@ -344,17 +397,20 @@ struct GradEnd {
       const int yn = n < l.N ? l.y[n] : -1;
       const bool ok = yn >= 0 && yn < l.V_all;
       const int t = ok ? yn - l.v0 : -1;
-      const float ln = ok ? lse[n] : 0.f, gn = ok ? g[n] : 0.f;
+      const float ln = take_off_far<T>(acc, j, ok ? lse[n] : 0.f), gn = ok ? g[n] : 0.f;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = exp_from(acc[i][j][e], ln);
+          acc[i][j][e] = ok ? p : 0.f;  // (whatever a row without a target holds)
+        }
+      Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { acc[i][j][e] -= 1.f; });
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
         const int v = pl.a0 + 16 * i + 4 * pl.quad;
-        f32x4 p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = wnk::expf_fast(acc[i][j][e] - ln) - (v + e == t ? 1.f : 0.f);
-          p[e] = ok && v + e < l.V ? p[e] : 0.f;
-          acc[i][j][e] = p[e] * gn;
-        }
+        const f32x4 p = acc[i][j];
+        acc[i][j] = p * gn;
         if constexpr (SP) {
           u16 hi[4], lo[4];
 #pragma unroll
@@ -480,7 +536,31 @@ struct OutEnd {
 // The scale of a row whose largest magnitude is m: m 2^e in [2^14, 2^15).
 __device__ __forceinline__ int scale_of(float m) { return m > 0.f && m < INFINITY ? 14 - ilogbf(m) : 0; }
 
-// Rows [R][K] as they are; a wave per row.
+// Values k .. k + 3 of a row of K, zeros behind it.
+__device__ __forceinline__ f32x4 four(const float* s, int k, int K) {
+  if (k + 3 < K) {
+    const f32x4u x = *reinterpret_cast<const f32x4u*>(s + k);
+    return f32x4{x[0], x[1], x[2], x[3]};
+  }
+  return f32x4{k < K ? s[k] : 0.f, k + 1 < K ? s[k + 1] : 0.f, k + 2 < K ? s[k + 2] : 0.f, 0.f};
+}
+// Four values' hi and lo parts to a row's place for value k (a multiple of 4).
+__device__ __forceinline__ void put_split(u16* row, int k, f32x4 v) {
+  u16 hi[4], lo[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) split(v[e], hi[e], lo[e]);
+  u16* p = row + k / 32 * kChunk + k % 32;
+  *reinterpret_cast<u32x2*>(p) = u32x2{(unsigned)hi[0] | (unsigned)hi[1] << 16, (unsigned)hi[2] | (unsigned)hi[3] << 16};
+  *reinterpret_cast<u32x2*>(p + 32) = u32x2{(unsigned)lo[0] | (unsigned)lo[1] << 16, (unsigned)lo[2] | (unsigned)lo[3] << 16};
+}
+__device__ __forceinline__ f32x4 scaled(f32x4 v, int e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], e);
+  return v;
+}
+
+// Rows [R][K] as they are; a wave per row.  fp32 rows of up to 1024 values stay in registers between the search
+// for their scale and the split.
 template <class E>
 __global__ __launch_bounds__(256) void pack_rows(const E* src, int R, int K, u16* dst, int units, int* scale) {
   const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -488,19 +568,38 @@ __global__ __launch_bounds__(256) void pack_rows(const E* src, int R, int K, u16
   const E* s = src + (size_t)r * K;
   u16* d = dst + (size_t)r * units;
   if constexpr (sizeof(E) == 2) {
-    for (int k = lane; k < units; k += 64) d[k] = k < K ? s[k] : (u16)0;
+    typedef u16 u16x8u __attribute__((ext_vector_type(8), aligned(2)));
+    typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+    for (int k = 8 * lane; k < units; k += 512) {
+      u16x8 x;
+      if (k + 7 < K) {
+        const u16x8u v = *reinterpret_cast<const u16x8u*>(s + k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = v[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = k + e < K ? s[k + e] : (u16)0;
+      }
+      *reinterpret_cast<u16x8*>(d + k) = x;
+    }
   } else {
+    constexpr int H = 4;
+    f32x4 v[H];
     float m = 0.f;
-    for (int k = lane; k < K; k += 64) m = fmaxf(m, fabsf(s[k]));
+#pragma unroll
+    for (int h = 0; h < H; ++h) v[h] = 256 * h < K ? four(s, 256 * h + 4 * lane, K) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < H; ++h) m = fmaxf(fmaxf(fmaxf(m, fabsf(v[h][0])), fabsf(v[h][1])), fmaxf(fabsf(v[h][2]), fabsf(v[h][3])));
+    for (int k = 256 * H + 4 * lane; k < K; k += 256) {
+      const f32x4 x = four(s, k, K);
+      m = fmaxf(fmaxf(fmaxf(m, fabsf(x[0])), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+    }
     const int e = scale_of(wnk::wave_max(m));
     if (lane == 0) scale[r] = e;
-    for (int k = lane; k < units / 2; k += 64) {
-      u16 hi, lo;
-      split(k < K ? ldexpf(s[k], e) : 0.f, hi, lo);
-      u16* p = d + k / 32 * kChunk + k % 32;
-      p[0] = hi;
-      p[32] = lo;
-    }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+      if (256 * h + 4 * lane < units / 2) put_split(d, 256 * h + 4 * lane, scaled(v[h], e));
+    for (int k = 256 * H + 4 * lane; k < units / 2; k += 256) put_split(d, k, scaled(four(s, k, K), e));
   }
 }
 
@@ -513,51 +612,96 @@ struct RowFactor {
   __device__ float factor(int r) const { return g ? g[r] : 1.f; }
 };
 
-// Largest magnitudes of the columns of [R][K], over the rows r = blockIdx.y, + gridDim.y, ..: part[blockIdx.y][K].
-__global__ __launch_bounds__(256) void column_max(const float* src, int R, int K, RowFactor f, float* part) {
-  __shared__ float s[4][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k = blockIdx.x * 64 + lane;
-  float m = 0.f;
+// Largest magnitudes of the columns of [R][K], over the rows of blockIdx.y's run: part[blockIdx.y][K].
+__global__ __launch_bounds__(256) void column_max(const float* src, int R, int K, int run, RowFactor f, float* part) {
+  __shared__ f32x4 s[16][16];
+  const int c = threadIdx.x & 15, w = threadIdx.x >> 4, k = blockIdx.x * 64 + 4 * c;
+  const int r0 = blockIdx.y * run, r1 = min(R, r0 + run);
+  f32x4 m{0.f, 0.f, 0.f, 0.f};
   if (k < K)
-    for (int r = blockIdx.y * 4 + w; r < R; r += gridDim.y * 4)
-      if (f.ok(r)) m = fmaxf(m, fabsf(src[(size_t)r * K + k] * f.factor(r)));
-  s[w][lane] = m;
+#pragma unroll 4
+    for (int r = r0 + w; r < r1; r += 16) {
+      const f32x4 v = four(src + (size_t)r * K, k, K);
+      const float g = f.ok(r) ? f.factor(r) : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = fmaxf(m[e], g == 0.f ? 0.f : fabsf(v[e] * g));
+    }
+  s[w][c] = m;
   __syncthreads();
-  if (w == 0 && k < K) part[(size_t)blockIdx.y * K + k] = fmaxf(fmaxf(s[0][lane], s[1][lane]), fmaxf(s[2][lane], s[3][lane]));
+  if (threadIdx.x < 64 && blockIdx.x * 64 + threadIdx.x < K) {
+    float v = 0.f;
+    for (int i = 0; i < 16; ++i) v = fmaxf(v, s[i][threadIdx.x >> 2][threadIdx.x & 3]);
+    part[(size_t)blockIdx.y * K + blockIdx.x * 64 + threadIdx.x] = v;
+  }
 }
 
 // The columns of [R][K] as rows: dst[k][r], 64 x 64 values per block.
-template <class E>
-__global__ __launch_bounds__(256) void pack_cols(const E* src, int R, int K, RowFactor f, u16* dst, int units,
-                                                 const float* part, int parts, int* scale) {
+__global__ __launch_bounds__(256) void pack_cols(const float* src, int R, int K, RowFactor f, u16* dst, int units, const float* part,
+                                                 int parts, int* scale) {
   __shared__ float s[64][65];
   __shared__ int se[64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
-  if (sizeof(E) == 4 && w == 0) {
-    float m = 0.f;
-    if (k0 + lane < K)
-      for (int i = 0; i < parts; ++i) m = fmaxf(m, part[(size_t)i * K + k0 + lane]);
-    se[lane] = scale_of(m);
-    if (blockIdx.y == 0 && k0 + lane < K) scale[k0 + lane] = se[lane];
+  const int tid = threadIdx.x, k0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int i = 16 * h + (tid >> 4), c = 4 * (tid & 15), r = r0 + i;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    if (r < R && f.ok(r)) {
+      v = four(src + (size_t)r * K, k0 + c, K) * f.factor(r);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[i][c + e] = v[e];
   }
-  for (int i = w; i < 64; i += 4) {
-    const int r = r0 + i, k = k0 + lane;
-    s[i][lane] = r < R && k < K && f.ok(r) ? value(src[(size_t)r * K + k]) * f.factor(r) : 0.f;
+  {
+    const int k = k0 + (tid >> 2);
+    float m = 0.f;
+    if (k < K)
+      for (int i = tid & 3; i < parts; i += 4) m = fmaxf(m, part[(size_t)i * K + k]);
+    m = fmaxf(m, wnk::dpp<0xB1>(m));
+    m = fmaxf(m, wnk::dpp<0x4E>(m));
+    if ((tid & 3) == 0) {
+      se[tid >> 2] = scale_of(m);
+      if (blockIdx.y == 0 && k < K) scale[k] = se[tid >> 2];
+    }
   }
   __syncthreads();
-  for (int i = w; i < 64; i += 4) {
-    const int k = k0 + i, r = r0 + lane;
-    if (k >= K) break;
-    u16* d = dst + (size_t)k * units;
-    if constexpr (sizeof(E) == 2) {
-      if (r < units) d[r] = bf16_bits(s[lane][i]);
-    } else if (r < units / 2) {
-      u16 hi, lo;
-      split(ldexpf(s[lane][i], se[i]), hi, lo);
-      d += r / 32 * kChunk + r % 32;
-      d[0] = hi;
-      d[32] = lo;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int i = 16 * h + (tid >> 4), c = 4 * (tid & 15);
+    if (k0 + i >= K || r0 + c >= units / 2) continue;
+    put_split(dst + (size_t)(k0 + i) * units, r0 + c, scaled(f32x4{s[c][i], s[c + 1][i], s[c + 2][i], s[c + 3][i]}, se[i]));
+  }
+}
+__global__ __launch_bounds__(256) void pack_cols(const u16* src, int R, int K, RowFactor f, u16* dst, int units) {
+  __shared__ __align__(16) u16 s[64][72];  // [k][r]
+  typedef u16 u16x8u __attribute__((ext_vector_type(8), aligned(2)));
+  const int tid = threadIdx.x, k0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
+  // a thread reads 8 columns of two neighbouring rows and writes pairs
+  {
+    const int c = 8 * (tid & 7), i = 2 * (tid >> 3), k = k0 + c;
+    u16 v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = r0 + i + h;
+      const bool on = r < R && f.ok(r);
+      const u16* p = src + (size_t)r * K + k;
+      if (on && k + 7 < K) {
+        const u16x8u x = *reinterpret_cast<const u16x8u*>(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[h][e] = x[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[h][e] = on && k + e < K ? p[e] : (u16)0;
+      }
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) *reinterpret_cast<unsigned*>(&s[c + e][i]) = (unsigned)v[0][e] | (unsigned)v[1][e] << 16;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = 32 * h + (tid >> 3), c = 8 * (tid & 7);
+    if (k0 + i < K && r0 + c < units)
+      *reinterpret_cast<u32x4*>(dst + (size_t)(k0 + i) * units + r0 + c) = *reinterpret_cast<const u32x4*>(&s[i][c]);
   }
 }
 
@@ -586,20 +730,41 @@ __global__ __launch_bounds__(256) void join_loss(const float2* part, int tiles, 
     sum = sum * wnk::expf_fast(m - at) + p.y * wnk::expf_fast(p.x - at);
     m = top;
   }
-  const float z = m + logf(sum);  // (no class at all: -inf)
-  lse[n] = z;
+  const float z = logf(sum);
+  lse[n] = m + z;  // (no class at all: -inf)
   const int t = y[n];
-  loss[n] = t >= 0 && t < V ? z - target[n] : 0.f;
+  loss[n] = t >= 0 && t < V ? m - target[n] + z : 0.f;  // (in this order log(sum) is not lost beside a large m)
 }
 
-// out[i] = sum over the parts, in their order.
+// out[i] = sum over the parts: 64 places of four values by 4 runs of parts per block, then the runs in order.
 template <class E>
 __global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float v = part[i];
-  for (int k = 1; k < parts; ++k) v += part[k * n + i];
-  put(out + i, v);
+  __shared__ f32x4 s[3][64];
+  const int c = threadIdx.x & 63, w = threadIdx.x >> 6, each = (parts + 3) / 4;
+  const size_t i = ((size_t)blockIdx.x * 64 + c) * 4;
+  f32x4 v{0.f, 0.f, 0.f, 0.f};
+  if (i + 3 < n) {
+#pragma unroll 8
+    for (int k = w * each; k < min(parts, (w + 1) * each); ++k) {
+      const f32x4u x = *reinterpret_cast<const f32x4u*>(part + k * n + i);
+      v += f32x4{x[0], x[1], x[2], x[3]};
+    }
+  } else if (i < n) {
+    for (int k = w * each; k < min(parts, (w + 1) * each); ++k)
+      for (int e = 0; e < 3; ++e)
+        if (i + e < n) v[e] += part[k * n + i + e];
+  }
+  if (w) s[w - 1][c] = v;
+  __syncthreads();
+  if (w || i >= n) return;
+  v = ((v + s[0][c]) + s[1][c]) + s[2][c];
+  if (i + 3 < n) {
+    if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(out + i) = f32x4u{v[0], v[1], v[2], v[3]};
+    else *reinterpret_cast<u16x4u*>(out + i) = u16x4u{bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3])};
+  } else {
+    for (int e = 0; e < 3; ++e)
+      if (i + e < n) put(out + i + e, v[e]);
+  }
 }
 
 template <class E>
@@ -613,22 +778,43 @@ __global__ __launch_bounds__(256) void fill_zero(E* out, size_t n) {
 constexpr size_t kForwardPiece = (size_t)64 << 20;    // bytes of packed w in the forward pass
 constexpr size_t kBackwardPiece = (size_t)512 << 20;  // bytes of w's forms and q in the backward pass
 constexpr int kMaxN = 1 << 20, kMaxD = 1 << 16, kMaxV = 1 << 24;
-constexpr int kTarget = 512;      // blocks that fill the chip
-constexpr int kColumnParts = 32;  // of column_max
+constexpr size_t kSplitFloats = (size_t)64 << 20;     // values of a product's parts, at most
+constexpr int kColumnParts = 64;  // of column_max
 
 bool sizes_ok(int dtype, int N, int D, int V) {
   return (dtype == WN_F32 || dtype == WN_BF16) && N >= 0 && N <= kMaxN && D >= 1 && D <= kMaxD && V >= 1 && V <= kMaxV;
 }
 
-// Tiles of 256 x 256 where they fill the chip, else 128 x 128.
-bool use_big(size_t a, size_t b) { return ceil_div(a, 256) * ceil_div(b, 256) >= 256; }
+// How a product of a x b outputs over `chunks` chunks is tiled, and in how many parts its sum is taken: the shortest
+// time by a model of the two tiles.  A chunk of 256 x 256 outputs takes a CU 1.4 us (three products of fp16 parts:
+// 2.1), of 128 x 128 two blocks on a CU 1.2 us; a tile's start and end 6 and 4 us; parts are written and joined
+// at 4.5 TB/s.
+struct Shape {
+  bool big;
+  int splits;
+  double us;
+};
+Shape shape_for(size_t a, size_t b, int units, bool sp, bool may_split) {
+  static const int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128};
+  const size_t chunks = ceil_div(units, kChunk);
+  Shape best{false, 1, 1e30};
+  for (int big = 0; big < 2; ++big) {
+    const size_t t = big ? 256 : 128, tiles = ceil_div(a, t) * ceil_div(b, t), room = big ? 256 : 512;
+    const double chunk = (big ? 1.4 : 1.2) * (sp ? 1.5 : 1.0), ends = big ? 6.0 : 4.0;
+    for (int s : kSplits) {
+      if (s > 1 && (!may_split || chunks / s < 4 || (size_t)s * a * b > kSplitFloats)) break;
+      const double us = (double)ceil_div(tiles * s, room) * ((double)ceil_div(chunks, s) * chunk + ends) +
+                        (s > 1 ? 5.0 + (s + 1.0) * a * b * 4 / 4.5e6 : 0.0);
+      if (us < best.us) best = {big != 0, s, us};
+    }
+  }
+  return best;
+}
 
-// Classes of a piece: a multiple of 256, pieces alike, `each` bytes a class.
-int piece_classes(int V, size_t each, size_t budget) {
-  size_t most = budget / each / 256 * 256;
-  most = std::max<size_t>(256, most);
-  const size_t pieces = ceil_div(V, most);
-  return (int)std::min<size_t>(ceil_div(ceil_div(V, pieces), 256) * 256, ceil_div(V, 256) * 256);
+// Classes of a forward piece: a multiple of 256, pieces alike.
+int forward_piece(int V, size_t each) {
+  const size_t most = std::max<size_t>(256, kForwardPiece / each / 256 * 256), pieces = ceil_div(V, most);
+  return (int)std::min<size_t>(V, ceil_div(ceil_div(V, pieces), 256) * 256);
 }
 
 struct Carve {
@@ -647,35 +833,48 @@ struct Forward {
   Forward(bool sp, int N, int D, int V) {
     const size_t units = padded_units(D, sp);
     Carve c;
-    piece = piece_classes(V, units * 2 + 4, kForwardPiece);
+    piece = forward_piece(V, units * 2 + 4);
     part = c.take(ceil_div(V, 128) * N * sizeof(float2));
     target = c.take((size_t)N * 4);
     x = c.take((size_t)N * units * 2);
     ex = c.take((size_t)N * 4);
-    w = c.take(std::min(piece, V) * units * 2);
+    w = c.take(piece * units * 2);
     ew = c.take((size_t)piece * 4);
     total = c.at;
   }
 };
 
-// How many parts the sum over k of a product is taken in: enough that its tiles fill the chip, each of 8 chunks
-// at least.
-int splits_for(size_t a, size_t b, int units) {
-  const size_t t = use_big(a, b) ? ceil_div(a, 256) * ceil_div(b, 256) : ceil_div(a, 128) * ceil_div(b, 128);
-  const size_t chunks = ceil_div(units, kChunk);
-  return (int)std::max<size_t>(1, std::min(kTarget / t, chunks / 8));
-}
-
 struct Backward {
   int piece;
-  int sx, sw;  // splits of dx and dw
+  Shape logits, dxs, dws;  // of a whole piece
   size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, db, cmax, dx, dw, total;
+  void plan(bool sp, int N, int D, int p) {
+    piece = p;
+    logits = shape_for(p, N, padded_units(D, sp), sp, false);
+    dxs = shape_for(D, N, padded_units(p, sp), sp, true);
+    dws = shape_for(D, p, padded_units(N, sp), sp, true);
+  }
   Backward(bool sp, int N, int D, int V) {
     const size_t ud = padded_units(D, sp), un = padded_units(N, sp), e = sp ? 4 : 2;
-    piece = std::min(V, piece_classes(V, ud * 2 + D * e + 2 * un * 2, kBackwardPiece));
+    const size_t each = ud * 2 + D * e + 2 * un * 2;
+    // pieces alike, the fewest that fit and a few more, or of whole rounds of the products' tiles: the fastest by the model
+    const size_t most = std::min<size_t>(V, std::max<size_t>(256, kBackwardPiece / each / 256 * 256)), fewest = ceil_div(V, most);
+    const size_t round = 256 * std::max<size_t>(1, 256 / ceil_div(D, 256));
+    double best = 1e30;
+    int at = (int)most;
+    for (int c = 0; c < 5; ++c) {
+      size_t p = c < 4 ? std::min<size_t>(V, ceil_div(ceil_div(V, fewest + c), 256) * 256) : most / round * round;
+      if (p == 0 || p > most) continue;
+      plan(sp, N, D, (int)p);
+      const double us = (logits.us + dxs.us + dws.us + 10) * (double)V / (double)p;
+      if (us < best * 0.999) {
+        best = us;
+        at = (int)p;
+      }
+      if (fewest == 1) break;
+    }
+    plan(sp, N, D, at);
     const size_t uv = padded_units(piece, sp);
-    sx = splits_for(D, N, (int)uv);
-    sw = splits_for(D, piece, (int)un);
     Carve c;
     x = c.take((size_t)N * ud * 2);
     ex = c.take((size_t)N * 4);
@@ -689,9 +888,8 @@ struct Backward {
     qt = c.take((size_t)piece * un * 2);
     db = c.take(ceil_div(N, 128) * piece * 4);
     cmax = c.take((size_t)kColumnParts * D * 4);
-    const bool whole = piece == V;
-    dx = c.take(whole && sx == 1 ? 0 : (size_t)sx * N * D * 4);
-    dw = c.take(sw == 1 ? 0 : (size_t)sw * piece * D * 4);
+    dx = c.take(piece == V && dxs.splits == 1 ? 0 : (size_t)dxs.splits * N * D * 4);
+    dw = c.take(dws.splits == 1 ? 0 : (size_t)dws.splits * piece * D * 4);
     total = c.at;
   }
 };
@@ -729,11 +927,16 @@ template <class E>
 Operand cols_operand(const E* src, int R, int K, const RowFactor& f, u16* dst, float* part, int* scale, hipStream_t st) {
   constexpr bool sp = sizeof(E) == 4;
   const int units = padded_units(R, sp);
-  const int parts = (int)std::min<size_t>(kColumnParts, ceil_div(R, 64));
-  const unsigned kb = (unsigned)ceil_div(K, 64);
-  if constexpr (sp)
-    hipLaunchKernelGGL(column_max, dim3(kb, parts), dim3(256), 0, st, src, R, K, f, part);
-  hipLaunchKernelGGL(pack_cols<E>, dim3(kb, (unsigned)ceil_div(R, 64)), dim3(256), 0, st, src, R, K, f, dst, units, part, parts, scale);
+  const dim3 grid((unsigned)ceil_div(K, 64), (unsigned)ceil_div(R, 64));
+  if constexpr (sp) {
+    const int run = (int)ceil_div(R, std::min<size_t>(kColumnParts, ceil_div(R, 64))), parts = (int)ceil_div(R, run);
+    hipLaunchKernelGGL(column_max, dim3(grid.x, parts), dim3(256), 0, st, src, R, K, run, f, part);
+    hipLaunchKernelGGL(static_cast<void (*)(const float*, int, int, RowFactor, u16*, int, const float*, int, int*)>(pack_cols), grid,
+                       dim3(256), 0, st, src, R, K, f, dst, units, part, parts, scale);
+  } else {
+    hipLaunchKernelGGL(static_cast<void (*)(const u16*, int, int, RowFactor, u16*, int)>(pack_cols), grid, dim3(256), 0, st, src, R, K,
+                       f, dst, units);
+  }
   return {dst, K, units, units};
 }
 
@@ -752,7 +955,7 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
   for (int v0 = 0; v0 < V; v0 += piece) {
     const int n = std::min(piece, V - v0);
     const Operand ow = rows_operand(w + (size_t)v0 * D, n, D, wp, ew, st);
-    const bool big = use_big(n, N);
+    const bool big = shape_for(n, N, ox.k, sp, false).big;
     StatsEnd end{{sp ? ex : nullptr, sp ? ew : nullptr, b ? b + v0 : nullptr, y, N, n, v0, V},
                  reinterpret_cast<float2*>(ws + f.part), tiles, reinterpret_cast<float*>(ws + f.target)};
     const hipError_t e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
@@ -767,7 +970,7 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
 
 template <class E>
 hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st) {
-  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out);
+  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out);  // (256 values a block)
   return hipGetLastError();
 }
 
@@ -789,23 +992,23 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
     const E* wv = w + (size_t)v0 * D;
     const int ldq = padded_units(n, sp), ldqt = padded_units(N, sp);
     const Operand ow = rows_operand(wv, n, D, units(f.w), ints(f.ew), st);
-    bool big = use_big(n, N);
+    const bool big = f.logits.big;
     GradEnd<sp> end{{sp ? ints(f.ex) : nullptr, sp ? ints(f.ew) : nullptr, b ? b + v0 : nullptr, y, N, n, v0, V},
                     lse, g, dx ? units(f.q) : nullptr, dw ? units(f.qt) : nullptr, ldq, ldqt, db ? floats(f.db) : nullptr};
     e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
     if (e == hipSuccess && db) e = join(floats(f.db), (int)ceil_div(N, big ? 256 : 128), n, db + v0, st);
     if (e == hipSuccess && dx) {
       const Operand owt = cols_operand(wv, n, D, RowFactor{nullptr, nullptr, 0}, units(f.wt), floats(f.cmax), ints(f.ewt), st);
-      const bool whole = f.piece == V && f.sx == 1;
+      const bool whole = f.piece == V && f.dxs.splits == 1;
       const OutEnd<E> o{D, N, ints(f.ewt), y, sp ? g : nullptr, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
-      e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.sx, 0}, use_big(D, N), o, st);
-      if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.sx, (size_t)N * D, dx, st);
+      e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.dxs.splits, 0}, f.dxs.big, o, st);
+      if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.dxs.splits, (size_t)N * D, dx, st);
     }
     if (e == hipSuccess && dw) {
       E* const out = dw + (size_t)v0 * D;
-      const OutEnd<E> o{D, n, ints(f.ext), nullptr, nullptr, 1, f.sw == 1 ? nullptr : floats(f.dw), 0, out};
-      e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.sw, 0}, use_big(D, n), o, st);
-      if (e == hipSuccess && f.sw > 1) e = join(floats(f.dw), f.sw, (size_t)n * D, out, st);
+      const OutEnd<E> o{D, n, ints(f.ext), nullptr, nullptr, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
+      e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.dws.splits, 0}, f.dws.big, o, st);
+      if (e == hipSuccess && f.dws.splits > 1) e = join(floats(f.dw), f.dws.splits, (size_t)n * D, out, st);
     }
   }
   return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));

@@ -179,6 +179,21 @@ def test_masked_classes(dtype, mask):
     _check(x, w, b, y, grad)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_every_class_masked_by_the_lowest_value(dtype):
+    """The logits' differences are lost beside the mask, so the classes are alike: loss log V, q = g (1 / V - [v = y])."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(90, 40, 700, dtype, seed=8, ignored=0)
+    b[:] = torch.finfo(torch.float32).min
+    loss, lse = wn.head_loss(x.cuda(), w.cuda(), y.cuda(), b=b.cuda())
+    assert bool(((loss.cpu().double() - np.log(700)).abs() <= 1e-5).all())
+    db = wn.head_loss_backward(x.cuda(), w.cuda(), y.cuda(), lse, grad.cuda(), b=b.cuda(), need=("db",))[2]
+    # (lse itself is the mask: log 700 is lost in it, and exp(l - lse) is 1)
+    q = torch.ones((90, 700), dtype=torch.float64)
+    q[torch.arange(90), y.long()] -= 1
+    assert bool(((db.cpu().double() - (q * grad.double()[:, None]).sum(dim=0)).abs() <= 1e-6).all())
+
+
 def test_a_masked_target_has_an_infinite_loss():
     import paper_1702_07825_amd as wn
     x, w, b, y, grad = _inputs(20, 40, 300, torch.float32, seed=9, ignored=0)
