@@ -1,0 +1,33 @@
+// Interface of the loss's kernels for few rows (gfx950).
+#pragma once
+#include "wn_arrays.h"
+
+// Calls of up to this many rows read w from memory straight into registers, once each pass, instead of through tiles
+// in LDS.
+constexpr int kFewRows = 64;
+constexpr int kFewClasses = 64;  // classes of a block: a place in `part`
+
+struct WnFew {
+  int N, D, V;
+  const void *x, *w;  // float or bf16
+  const float* b;     // or null
+  const int32_t* y;
+};
+
+// Forward: (largest logit, sum of exponentials) of each row in each run of kFewClasses classes, part[run][N], and the
+// targets' logits.
+template <class E>
+hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st);
+
+// Backward.  Workspace of the q's ([N][V] and [V][N], padded) and of dx's parts; `parts` of them, [parts][N][D] fp32,
+// are left in `sum` for the caller to join (rows without a target hold anything there).
+struct WnFewPlan {
+  int vpad;                 // row of q
+  int npad;                 // row of the transposed one
+  int slabs, parts, each;   // dx: runs of columns, of classes; classes of a run
+  size_t q_bytes, qt_bytes, sum_bytes;
+};
+WnFewPlan wn_few_plan(bool f32, int N, int D, int V);
+template <class E>
+hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, const float* g, bool dx, void* dw, float* db, void* q,
+                        void* qt, float* sum, hipStream_t st);

@@ -1,0 +1,444 @@
+// The loss of an output layer and its gradients for up to 64 rows (gfx950): scoring single tokens, or the last rows
+// of short sequences.
+//
+// So few rows leave the products bound by the reads of w (and dw by its writes), so w goes from memory straight to the
+// operands' registers, once in each pass, at whatever alignment it has and without a packed copy: bf16 on
+// v_mfma_f32_16x16x32_bf16, fp32 on v_mfma_f32_16x16x4f32, whose rate just covers 64 rows at the memory's.  x is read
+// the same way and stays in the caches.  Operand A's index is the classes (logits) or the columns (dx, dw),
+// operand B's the rows, NB tiles of 16.
+#include "wn_few.h"
+
+#include "wn_wave.h"
+
+namespace {
+
+using namespace wnt;
+
+typedef u16 u16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+// A 16-byte piece of a row: 8 bf16 or 4 fp32 values.
+template <class E>
+struct Piece;
+template <>
+struct Piece<u16> {
+  typedef u16x8 type;
+  typedef u16x8u any;
+  static constexpr int n = 8;
+};
+template <>
+struct Piece<float> {
+  typedef f32x4 type;
+  typedef f32x4u any;
+  static constexpr int n = 4;
+};
+template <class E>
+using P = typename Piece<E>::type;
+
+// Elements k .. of p, of which `left` exist (any number); the rest are 0.
+template <class E>
+__device__ __forceinline__ P<E> piece_at(const E* p, int left) {
+  constexpr int n = Piece<E>::n;
+  P<E> v;
+  if (left >= n) {
+    const typename Piece<E>::any x = *reinterpret_cast<const typename Piece<E>::any*>(p);
+#pragma unroll
+    for (int e = 0; e < n; ++e) v[e] = x[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < n; ++e) v[e] = e < left ? p[e] : (E)0;
+  }
+  return v;
+}
+template <class E>
+__device__ __forceinline__ P<E> whole_piece(const E* p) {
+  const typename Piece<E>::any x = *reinterpret_cast<const typename Piece<E>::any*>(p);
+  P<E> v;
+#pragma unroll
+  for (int e = 0; e < Piece<E>::n; ++e) v[e] = x[e];
+  return v;
+}
+template <class E>
+__device__ __forceinline__ P<E> no_piece() {
+  P<E> v;
+#pragma unroll
+  for (int e = 0; e < Piece<E>::n; ++e) v[e] = (E)0;
+  return v;
+}
+
+// c += A B over 32 (bf16) or 16 (fp32) values of k: lane (n, quad) holds row n's pieces at 8 quad or 4 quad; product e
+// of fp32 takes the values at 4 quad + e.
+__device__ __forceinline__ f32x4 mma(u16x8 a, u16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Logits: a wave takes 16 classes, a block 64.  The next U pieces of w are in flight during the current ones'
+// products.
+// ------------------------------------------------------------------------------------------------
+template <class E, int NB, class End>
+__global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End end) {
+  constexpr int W = Piece<E>::n, K = 4 * W, U = NB == 4 ? 4 : 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
+  const int v0 = blockIdx.x * kFewClasses + wave * 16;
+  // rows behind the last one repeat it: what they give is not used
+  const E* w = static_cast<const E*>(f.w) + (size_t)min(v0 + n, f.V - 1) * f.D + quad * W;
+  const E* x[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) x[j] = static_cast<const E*>(f.x) + (size_t)min(16 * j + n, f.N - 1) * f.D + quad * W;
+  f32x4 acc[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int chunks = f.D / (U * K);
+  P<E> a[U];
+  if (chunks)
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = whole_piece(w + u * K);
+  for (int c = 0; c < chunks; ++c) {
+    P<E> next[U], b[U][NB];
+    const int k = c * U * K, kn = min(c + 1, chunks - 1) * U * K;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) b[u][j] = whole_piece(x[j] + k + u * K);
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = whole_piece(w + kn + u * K);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[j] = mma(a[u], b[u][j], acc[j]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = next[u];
+  }
+  for (int k = chunks * U * K; k < f.D; k += K) {
+    const int left = f.D - k - quad * W;
+    const P<E> t = piece_at(w + k, left);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[j] = mma(t, piece_at(x[j] + k, left), acc[j]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int v = v0 + 4 * quad + e;
+    const float bv = f.b ? f.b[min(v, f.V - 1)] : 0.f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[j][e] = v < f.V ? acc[j][e] + bv : -INFINITY;
+  }
+  end(f, acc, v0 + 4 * quad, n, quad, wave);
+}
+
+__device__ __forceinline__ float quads_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float quads_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+struct FewStats {
+  float2* part;
+  float* target;
+  template <int NB>
+  __device__ void operator()(const WnFew& f, f32x4 (&acc)[NB], int v, int n, int quad, int wave) const {
+    __shared__ float2 s[4][16 * NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int r = 16 * j + n;
+      const int t = r < f.N ? f.y[r] : -1;
+      const f32x4 l = acc[j];
+      const float m = quads_max(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])));
+      const float at = m == -INFINITY ? 0.f : m;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum += wnk::expf_fast(l[e] - at);
+        if (t == v + e && t < f.V) target[r] = l[e];
+      }
+      sum = quads_sum(sum);
+      if (quad == 0) s[wave][r] = make_float2(m, sum);
+    }
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r >= f.N) return;
+    float2 o = s[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float2 p = s[w][r];
+      const float m = fmaxf(o.x, p.x), at = m == -INFINITY ? 0.f : m;
+      o = make_float2(m, o.y * wnk::expf_fast(o.x - at) + p.y * wnk::expf_fast(p.x - at));
+    }
+    part[(size_t)blockIdx.x * f.N + r] = o;
+  }
+};
+
+// g q as the operands of dx ([n][v]) and dw ([v][n]), and db, all of whose rows are here.
+template <class E>
+struct FewGrad {
+  const float *lse, *g;
+  E *q, *qt;  // or null
+  int vpad, npad;
+  float* db;  // or null
+  template <int NB>
+  __device__ void operator()(const WnFew& f, f32x4 (&acc)[NB], int v, int n, int quad, int) const {
+    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int r = 16 * j + n;
+      const int t = r < f.N ? f.y[r] : -1;
+      const bool ok = t >= 0 && t < f.V;
+      const float ln = ok ? lse[r] : 0.f, gn = ok ? g[r] : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = wnk::expf_fast(acc[j][e] - ln) - (v + e == t ? 1.f : 0.f);
+        acc[j][e] = ok && v + e < f.V ? p * gn : 0.f;
+      }
+      sum += acc[j];
+      if (q && r < f.N && v < vpad) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put(q + (size_t)r * vpad + v + e, acc[j][e]);
+      }
+      if (qt && r < npad) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v + e < f.V) put(qt + (size_t)(v + e) * npad + r, acc[j][e]);
+      }
+    }
+    if (NB == 1 && qt) {  // (bf16 takes 32 rows at a time)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v + e < f.V) put(qt + (size_t)(v + e) * npad + 16 + n, 0.f);
+    }
+    if (!db) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float s = wnk::gsum16(sum[e]);
+      if (n == 0 && v + e < f.V) db[v + e] = s;
+    }
+  }
+};
+
+// ------------------------------------------------------------------------------------------------
+// dx and dw: operand A is a row-major array's columns, kSlab of them, its k the array's rows.  A lane reads a piece of
+// a row at column W n, for the rows at W quad .. + W - 1 of a step: piece t, element u is then column W n + u of row
+// W quad + t, so fragment u (columns W n + u, n = 0 .. 15) takes element u of every piece.  (bf16: pairs
+// of rows by one v_perm each.)
+// ------------------------------------------------------------------------------------------------
+template <class E>
+constexpr int kSlab = 16 * Piece<E>::n;
+template <class E>
+constexpr int kStep = 4 * Piece<E>::n;  // rows of a step
+
+template <class E>
+struct Columns {
+  P<E> f[Piece<E>::n];
+  // rows r0 + W quad + t of [R][D] (rows behind the last: the last again), columns c0 + W n ..
+  __device__ __forceinline__ void load(const E* p, int R, int D, int r0, int c, int quad) {
+    constexpr int W = Piece<E>::n;
+#pragma unroll
+    for (int t = 0; t < W; ++t) f[t] = piece_at(p + (size_t)min(r0 + W * quad + t, R - 1) * D + c, D - c);
+  }
+  __device__ __forceinline__ P<E> fragment(int u) const {
+    constexpr int W = Piece<E>::n;
+    P<E> r;
+    if constexpr (W == 4) {
+#pragma unroll
+      for (int t = 0; t < W; ++t) r[t] = f[t][u];
+    } else {
+      u32x4 o;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const unsigned a = __builtin_bit_cast(u32x4, f[2 * t])[u >> 1], b = __builtin_bit_cast(u32x4, f[2 * t + 1])[u >> 1];
+        o[t] = __builtin_amdgcn_perm(b, a, u & 1 ? 0x07060302u : 0x05040100u);
+      }
+      r = __builtin_bit_cast(P<E>, o);
+    }
+    return r;
+  }
+};
+
+// dx's parts: a block takes a slab of columns and a run of classes, its waves a quarter of the run each, and adds the
+// quarters up.
+template <class E, int NB>
+__global__ __launch_bounds__(256, 2) void few_dx(const WnFew f, const E* q, int vpad, int each, float* sum) {
+  constexpr int W = Piece<E>::n, S = kStep<E>;
+  extern __shared__ __align__(16) char dyn[];
+  f32x4* const s = reinterpret_cast<f32x4*>(dyn);  // [W NB][64]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
+  const int c = blockIdx.x * kSlab<E> + W * n;
+  const int quarter = each / 4, v0 = blockIdx.y * each + wave * quarter, v1 = min(f.V, v0 + quarter);
+  const E* w = static_cast<const E*>(f.w);
+  f32x4 acc[W][NB];
+#pragma unroll
+  for (int u = 0; u < W; ++u)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int cc = min(c, f.D - 1);  // (columns behind the last are not stored)
+  if (v0 < v1) {
+    Columns<E> a, next;
+    a.load(w, f.V, f.D, v0, cc, quad);
+    for (int v = v0; v < v1; v += S) {
+      P<E> b[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        b[j] = 16 * j + n < f.N ? whole_piece(q + (size_t)(16 * j + n) * vpad + v + W * quad) : no_piece<E>();
+      next.load(w, f.V, f.D, v + S < v1 ? v + S : v, cc, quad);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        const P<E> x = a.fragment(u);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[u][j] = mma(x, b[j], acc[u][j]);
+      }
+      a = next;
+    }
+  }
+  for (int w4 = 1; w4 < 4; ++w4) {
+    __syncthreads();
+    if (wave == w4)
+#pragma unroll
+      for (int u = 0; u < W; ++u)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) s[(u * NB + j) * 64 + lane] = acc[u][j];
+    __syncthreads();
+    if (wave == 0)
+#pragma unroll
+      for (int u = 0; u < W; ++u)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[u][j] += s[(u * NB + j) * 64 + lane];
+  }
+  if (wave) return;
+  // lane (n, quad): columns W (4 quad + i) + u of row 16 j + n
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int r = 16 * j + n;
+    if (r >= f.N) continue;
+    float* d = sum + ((size_t)blockIdx.y * f.N + r) * f.D + blockIdx.x * kSlab<E>;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        const int k = W * (4 * quad + i) + u;
+        if (blockIdx.x * kSlab<E> + k < f.D) d[k] = acc[u][j][i];
+      }
+  }
+}
+
+// dw: a wave keeps its slab of x's columns in registers and goes over its classes, 16 at a time.
+template <class E, int NB>
+__global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int npad, E* dw) {
+  constexpr int W = Piece<E>::n, S = kStep<E>, K = (16 * NB + S - 1) / S, kTiles = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
+  const int c0 = blockIdx.x * kSlab<E>, c = min(c0 + W * n, f.D - 1);
+  P<E> a[K][W];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    Columns<E> t;
+    // (rows behind N and rows without a target meet zeros in q: anything but a NaN would do, so they are zeroed)
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const int r = k * S + W * quad + i, yr = r < f.N ? f.y[r] : -1;
+      t.f[i] = yr >= 0 && yr < f.V ? piece_at(static_cast<const E*>(f.x) + (size_t)r * f.D + c, f.D - c) : no_piece<E>();
+    }
+#pragma unroll
+    for (int u = 0; u < W; ++u) a[k][u] = t.fragment(u);
+  }
+  for (int t = 0; t < kTiles; ++t) {
+    const int v0 = ((blockIdx.y * 4 + wave) * kTiles + t) * 16;
+    if (v0 >= f.V) return;
+    const int v = v0 + n;
+    f32x4 acc[W];
+#pragma unroll
+    for (int u = 0; u < W; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const P<E> b = whole_piece(qt + (size_t)min(v, f.V - 1) * npad + k * S + W * quad);
+#pragma unroll
+      for (int u = 0; u < W; ++u) acc[u] = mma(a[k][u], b, acc[u]);
+    }
+    if (v >= f.V) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = c0 + W * (4 * quad + i);
+      E* d = dw + (size_t)v * f.D + k;
+      if (k + W <= f.D) {
+        typename Piece<E>::any o;
+#pragma unroll
+        for (int u = 0; u < W; ++u) {
+          E e;
+          put(&e, acc[u][i]);
+          o[u] = e;
+        }
+        *reinterpret_cast<typename Piece<E>::any*>(d) = o;
+      } else {
+#pragma unroll
+        for (int u = 0; u < W; ++u)
+          if (k + u < f.D) put(d + u, acc[u][i]);
+      }
+    }
+  }
+}
+
+template <class F>
+void by_tiles(int N, F f) {
+  if (N <= 16) f(std::integral_constant<int, 1>{});
+  else if (N <= 32) f(std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+template <class E>
+hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st) {
+  by_tiles(f.N, [&](auto nb) {
+    const FewStats end{part, target};
+    hipLaunchKernelGGL((few_logits<E, decltype(nb)::value, FewStats>), dim3((unsigned)ceil_div(f.V, kFewClasses)), dim3(256), 0, st, f, end);
+  });
+  return hipGetLastError();
+}
+
+WnFewPlan wn_few_plan(bool f32, int N, int D, int V) {
+  WnFewPlan p;
+  const int step = f32 ? 16 : 32, e = f32 ? 4 : 2, slab = f32 ? 64 : 128;
+  // q's rows hold zeros from V to the last block's end, past which no step reads; each block of dx takes 4 quarters of whole steps, some 1024 blocks
+  p.vpad = (int)ceil_div(V, kFewClasses) * kFewClasses;
+  p.npad = N <= 32 ? 32 : 64;
+  p.slabs = (int)ceil_div(D, slab);
+  const size_t want = std::max<size_t>(1, 1024 / p.slabs);
+  p.each = (int)(std::max<size_t>(1, ceil_div(V, want * 4 * step)) * 4 * step);
+  p.parts = (int)ceil_div(V, p.each);
+  p.q_bytes = (size_t)N * p.vpad * e;
+  p.qt_bytes = (size_t)V * p.npad * e;
+  p.sum_bytes = (size_t)p.parts * N * D * 4;
+  return p;
+}
+
+template <class E>
+hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, const float* g, bool dx, void* dw, float* db, void* q,
+                        void* qt, float* sum, hipStream_t st) {
+  by_tiles(f.N, [&](auto nb) {
+    constexpr int NB = decltype(nb)::value, W = Piece<E>::n;
+    const FewGrad<E> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad, p.npad, db};
+    hipLaunchKernelGGL((few_logits<E, NB, FewGrad<E>>), dim3((unsigned)ceil_div(f.V, kFewClasses)), dim3(256), 0, st, f, end);
+    if (dx)
+      hipLaunchKernelGGL((few_dx<E, NB>), dim3(p.slabs, p.parts), dim3(256), W * NB * 64 * 16, st, f, static_cast<const E*>(q), p.vpad,
+                         p.each, sum);
+    if (dw)
+      hipLaunchKernelGGL((few_dw<E, NB>), dim3(p.slabs, (unsigned)ceil_div(f.V, 256)), dim3(256), 0, st, f, static_cast<const E*>(qt),
+                         p.npad, static_cast<E*>(dw));
+  });
+  return hipGetLastError();
+}
+
+template hipError_t wn_few_loss<float>(const WnFew&, float2*, float*, hipStream_t);
+template hipError_t wn_few_loss<u16>(const WnFew&, float2*, float*, hipStream_t);
+template hipError_t wn_few_grads<float>(const WnFew&, const WnFewPlan&, const float*, const float*, bool, void*, float*, void*, void*,
+                                        float*, hipStream_t);
+template hipError_t wn_few_grads<u16>(const WnFew&, const WnFewPlan&, const float*, const float*, bool, void*, float*, void*, void*,
+                                      float*, hipStream_t);

@@ -13,7 +13,7 @@
 // row is scaled by a power of two so that its largest value lies in [2^14, 2^15), hi = fp16(v),
 // lo = fp16(v - hi), which holds v to 2^-22 of itself or 2^-39 of the row's largest, and a product takes
 // hi hi + hi lo + lo hi (lo lo is below 2^-22 of it), summed in fp32.
-#include "wn_arrays.h"
+#include "wn_few.h"
 
 #include "wn_wave.h"
 
@@ -736,9 +736,33 @@ __global__ __launch_bounds__(256) void join_loss(const float2* part, int tiles, 
   loss[n] = t >= 0 && t < V ? m - target[n] + z : 0.f;  // (in this order log(sum) is not lost beside a large m)
 }
 
+// The same for few rows: a block per row.
+__global__ __launch_bounds__(256) void join_loss_few(const float2* part, int tiles, const float* target, const int32_t* y, int N,
+                                                     int V, float* loss, float* lse) {
+  __shared__ float2 s[4];
+  const int n = blockIdx.x;
+  float2 a{-INFINITY, 0.f};
+  auto add = [&](float2 p) {
+    const float top = fmaxf(a.x, p.x), at = top == -INFINITY ? 0.f : top;
+    a = make_float2(top, a.y * wnk::expf_fast(a.x - at) + p.y * wnk::expf_fast(p.x - at));
+  };
+#pragma unroll 4
+  for (int t = threadIdx.x; t < tiles; t += 256) add(part[(size_t)t * N + n]);
+  for (int d = 32; d; d >>= 1) add(make_float2(__shfl_xor(a.x, d, 64), __shfl_xor(a.y, d, 64)));
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = a;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int w = 1; w < 4; ++w) add(s[w]);
+  const float z = logf(a.y);
+  lse[n] = a.x + z;
+  const int t = y[n];
+  loss[n] = t >= 0 && t < V ? a.x - target[n] + z : 0.f;
+}
+
 // out[i] = sum over the parts: 64 places of four values by 4 runs of parts per block, then the runs in order.
+// With y the values are rows of D, and those without a target are 0 whatever the parts hold.
 template <class E>
-__global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out) {
+__global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out, const int32_t* y, int V, unsigned D) {
   __shared__ f32x4 s[3][64];
   const int c = threadIdx.x & 63, w = threadIdx.x >> 6, each = (parts + 3) / 4;
   const size_t i = ((size_t)blockIdx.x * 64 + c) * 4;
@@ -758,6 +782,13 @@ __global__ __launch_bounds__(256) void join_parts(const float* part, int parts, 
   __syncthreads();
   if (w || i >= n) return;
   v = ((v + s[0][c]) + s[1][c]) + s[2][c];
+  if (y) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int t = i + e < n ? y[(unsigned)(i + e) / D] : -1;
+      if (t < 0 || t >= V) v[e] = 0.f;
+    }
+  }
   if (i + 3 < n) {
     if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(out + i) = f32x4u{v[0], v[1], v[2], v[3]};
     else *reinterpret_cast<u16x4u*>(out + i) = u16x4u{bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3])};
@@ -776,7 +807,7 @@ __global__ __launch_bounds__(256) void fill_zero(E* out, size_t n) {
 // Host
 // ------------------------------------------------------------------------------------------------
 constexpr size_t kForwardPiece = (size_t)64 << 20;    // bytes of packed w in the forward pass
-constexpr size_t kBackwardPiece = (size_t)512 << 20;  // bytes of w's forms and q in the backward pass
+constexpr size_t kBackwardPiece = (size_t)1 << 30;   // bytes of w's forms and q in the backward pass
 constexpr int kMaxN = 1 << 20, kMaxD = 1 << 16, kMaxV = 1 << 24;
 constexpr size_t kSplitFloats = (size_t)64 << 20;     // values of a product's parts, at most
 constexpr int kColumnParts = 64;  // of column_max
@@ -833,6 +864,12 @@ struct Forward {
   Forward(bool sp, int N, int D, int V) {
     const size_t units = padded_units(D, sp);
     Carve c;
+    if (N <= kFewRows) {
+      part = c.take(ceil_div(V, kFewClasses) * N * sizeof(float2));
+      target = c.take((size_t)N * 4);
+      total = c.at;
+      return;
+    }
     piece = forward_piece(V, units * 2 + 4);
     part = c.take(ceil_div(V, 128) * N * sizeof(float2));
     target = c.take((size_t)N * 4);
@@ -848,6 +885,7 @@ struct Backward {
   int piece;
   Shape logits, dxs, dws;  // of a whole piece
   size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, db, cmax, dx, dw, total;
+  WnFewPlan few;
   void plan(bool sp, int N, int D, int p) {
     piece = p;
     logits = shape_for(p, N, padded_units(D, sp), sp, false);
@@ -855,6 +893,15 @@ struct Backward {
     dws = shape_for(D, p, padded_units(N, sp), sp, true);
   }
   Backward(bool sp, int N, int D, int V) {
+    if (N <= kFewRows) {
+      few = wn_few_plan(sp, N, D, V);
+      Carve c;
+      q = c.take(few.q_bytes);
+      qt = c.take(few.qt_bytes);
+      dx = c.take(few.sum_bytes);
+      total = c.at;
+      return;
+    }
     const size_t ud = padded_units(D, sp), un = padded_units(N, sp), e = sp ? 4 : 2;
     const size_t each = ud * 2 + D * e + 2 * un * 2;
     // pieces alike, the fewest that fit and a few more, or of whole rounds of the products' tiles: the fastest by the model
@@ -945,6 +992,16 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
                 char* ws, hipStream_t st) {
   constexpr bool sp = sizeof(E) == 4;
   const Forward f(sp, N, D, V);
+  if (N <= kFewRows) {
+    float2* const part = reinterpret_cast<float2*>(ws + f.part);
+    float* const target = reinterpret_cast<float*>(ws + f.target);
+    hipError_t e = wn_few_loss<E>({N, D, V, x, w, b, y}, part, target, st);
+    if (e == hipSuccess) {
+      hipLaunchKernelGGL(join_loss_few, dim3(N), dim3(256), 0, st, part, (int)ceil_div(V, kFewClasses), target, y, N, V, loss, lse);
+      e = hipGetLastError();
+    }
+    return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+  }
   int* const ex = reinterpret_cast<int*>(ws + f.ex);
   int* const ew = reinterpret_cast<int*>(ws + f.ew);
   u16* const wp = reinterpret_cast<u16*>(ws + f.w);
@@ -969,8 +1026,8 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
 }
 
 template <class E>
-hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st) {
-  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out);  // (256 values a block)
+hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st, const int32_t* y = nullptr, int V = 0, int D = 1) {
+  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out, y, V, (unsigned)D);
   return hipGetLastError();
 }
 
@@ -982,6 +1039,11 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
   auto ints = [&](size_t off) { return reinterpret_cast<int*>(ws + off); };
   auto units = [&](size_t off) { return reinterpret_cast<u16*>(ws + off); };
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  if (N <= kFewRows) {
+    hipError_t e = wn_few_grads<E>({N, D, V, x, w, b, y}, f.few, lse, g, dx != nullptr, dw, db, ws + f.q, ws + f.qt, floats(f.dx), st);
+    if (e == hipSuccess && dx) e = join(floats(f.dx), f.few.parts, (size_t)N * D, dx, st, y, V, D);
+    return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+  }
   const Operand ox = rows_operand(x, N, D, units(f.x), ints(f.ex), st);
   Operand oxt{};
   // (bf16: q holds g; fp32: x transposed does, so that q stays within its scale)

@@ -114,5 +114,5 @@ def test_workspace_sizes(lib):
             assert f(*args, *bad) == 0
     assert lib.wn_loss_workspace_bytes(2, 4, 8, 16) == 0
     # a fixed multiple of the pieces' budget, whatever the vocabulary: the logits are not kept
-    assert lib.wn_loss_backward_workspace_bytes(1, 8192, 2048, 1 << 20) < 3 << 30
+    assert lib.wn_loss_backward_workspace_bytes(1, 8192, 2048, 1 << 20) < 4 << 30
     assert lib.wn_clip_workspace_bytes() > 0
