@@ -5,7 +5,8 @@
 // Calls of up to this many rows read w from memory straight into registers, once each pass, instead of through tiles
 // in LDS.
 constexpr int kFewRows = 64;
-constexpr int kFewClasses = 64;  // classes of a block: a place in `part`
+// Classes of a block: a place in `part`.
+inline int wn_few_classes(int N) { return N <= 16 ? 64 : 128; }
 
 struct WnFew {
   int N, D, V;
@@ -14,7 +15,7 @@ struct WnFew {
   const int32_t* y;
 };
 
-// Forward: (largest logit, sum of exponentials) of each row in each run of kFewClasses classes, part[run][N], and the
+// Forward: (largest logit, sum of exponentials) of each row in each run of wn_few_classes(N) classes, part[run][N], and the
 // targets' logits.
 template <class E>
 hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st);

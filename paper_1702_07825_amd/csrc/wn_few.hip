@@ -79,57 +79,116 @@ __device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// Logits: a wave takes 16 classes, a block 64.  The next U pieces of w are in flight during the current ones'
-// products.
+// Logits: a wave takes T tiles of 16 classes.  The next U pieces of w are in flight during the current ones'
+// products.  Up to 16 rows of x come from the caches as operands; more go through LDS, once for the block's four
+// waves (straight from the caches, 37 rows x 50021 classes x 777, the reads of x took the pass from 40 to 92 us).
 // ------------------------------------------------------------------------------------------------
+template <int NB>
+constexpr int kTilesOf = NB == 1 ? 1 : 2;  // T (wn_few_classes: 64 T a block)
+constexpr int kRowBytes = 256, kPitch = kRowBytes + 16;  // of a chunk of x in LDS: 16 rows' pieces on different banks
+
 template <class E, int NB, class End>
 __global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End end) {
-  constexpr int W = Piece<E>::n, K = 4 * W, U = NB == 4 ? 4 : 8;
+  constexpr int W = Piece<E>::n, K = 4 * W, T = kTilesOf<NB>, U = NB == 1 ? 8 : kRowBytes / 64;
+  constexpr bool kStaged = NB > 1;
+  __shared__ __align__(16) char xs[kStaged ? 2 * 16 * NB * kPitch : 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
-  const int v0 = blockIdx.x * kFewClasses + wave * 16;
+  const int v0 = (blockIdx.x * 4 + wave) * 16 * T;
   // rows behind the last one repeat it: what they give is not used
-  const E* w = static_cast<const E*>(f.w) + (size_t)min(v0 + n, f.V - 1) * f.D + quad * W;
-  const E* x[NB];
+  const E* w[T];
 #pragma unroll
-  for (int j = 0; j < NB; ++j) x[j] = static_cast<const E*>(f.x) + (size_t)min(16 * j + n, f.N - 1) * f.D + quad * W;
-  f32x4 acc[NB];
+  for (int t = 0; t < T; ++t) w[t] = static_cast<const E*>(f.w) + (size_t)min(v0 + 16 * t + n, f.V - 1) * f.D + quad * W;
+  f32x4 acc[T][NB];
 #pragma unroll
-  for (int j = 0; j < NB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int chunks = f.D / (U * K);
-  P<E> a[U];
-  if (chunks)
+  for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int u = 0; u < U; ++u) a[u] = whole_piece(w + u * K);
-  for (int c = 0; c < chunks; ++c) {
-    P<E> next[U], b[U][NB];
-    const int k = c * U * K, kn = min(c + 1, chunks - 1) * U * K;
+    for (int j = 0; j < NB; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  P<E> a[T][U], next[T][U];
+  const int whole = f.D / (U * K), chunks = (f.D + U * K - 1) / (U * K);
+  auto fetch = [&](P<E> (&to)[T][U], int c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) b[u][j] = whole_piece(x[j] + k + u * K);
+      for (int u = 0; u < U; ++u) {
+        const int k = (c * U + u) * K;
+        to[t][u] = c < whole ? whole_piece(w[t] + k) : piece_at(w[t] + k, f.D - k - quad * W);
+      }
+  };
+  fetch(a, 0);
+  if constexpr (kStaged) {
+    constexpr int kPieces = 16 * NB * (kRowBytes / 16) / 256;  // of a chunk of x per thread
+    P<E> xv[kPieces];
+    const int xr = threadIdx.x >> 4, xc = threadIdx.x & 15;
+    auto fetch_x = [&](int c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = whole_piece(w + kn + u * K);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < kPieces; ++i) {
+        const int k = c * U * K + xc * W;
+        xv[i] = piece_at(static_cast<const E*>(f.x) + (size_t)min(xr + 16 * i, f.N - 1) * f.D + k, f.D - k);
+      }
+    };
+    auto keep_x = [&](int c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int i = 0; i < kPieces; ++i)
+        *reinterpret_cast<P<E>*>(xs + (c & 1) * 16 * NB * kPitch + (xr + 16 * i) * kPitch + xc * 16) = xv[i];
+    };
+    fetch_x(0);
+    keep_x(0);
+    for (int c = 0; c < chunks; ++c) {
+      const bool more = c + 1 < chunks;
+      if (more) {
+        fetch_x(c + 1);
+        fetch(next, c + 1);
+      }
+      wnk::lds_barrier();  // (its waits leave the loads in flight)
+      const char* at = xs + (c & 1) * 16 * NB * kPitch + n * kPitch + quad * 16;
 #pragma unroll
-      for (int j = 0; j < NB; ++j) acc[j] = mma(a[u], b[u][j], acc[j]);
+      for (int u = 0; u < U; ++u) {
+        P<E> b[NB];
 #pragma unroll
-    for (int u = 0; u < U; ++u) a[u] = next[u];
+        for (int j = 0; j < NB; ++j) b[j] = *reinterpret_cast<const P<E>*>(at + j * 16 * kPitch + u * 64);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[t][j] = mma(a[t][u], b[j], acc[t][j]);
+      }
+      if (more) {
+        keep_x(c + 1);  // (the other buffer: its readers passed the barrier above)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int u = 0; u < U; ++u) a[t][u] = next[t][u];
+      }
+    }
+  } else {
+    const E* const x = static_cast<const E*>(f.x) + (size_t)min(n, f.N - 1) * f.D + quad * W;
+    for (int c = 0; c < chunks; ++c) {
+      P<E> b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = (c * U + u) * K;
+        b[u] = c < whole ? whole_piece(x + k) : piece_at(x + k, f.D - k - quad * W);
+      }
+      if (c + 1 < chunks) fetch(next, c + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[t][0] = mma(a[t][u], b[u], acc[t][0]);
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int u = 0; u < U; ++u) a[t][u] = next[t][u];
+    }
   }
-  for (int k = chunks * U * K; k < f.D; k += K) {
-    const int left = f.D - k - quad * W;
-    const P<E> t = piece_at(w + k, left);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) acc[j] = mma(t, piece_at(x[j] + k, left), acc[j]);
-  }
+  for (int t = 0; t < T; ++t)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int v = v0 + 4 * quad + e;
-    const float bv = f.b ? f.b[min(v, f.V - 1)] : 0.f;
+    for (int e = 0; e < 4; ++e) {
+      const int v = v0 + 16 * t + 4 * quad + e;
+      const float bv = f.b ? f.b[min(v, f.V - 1)] : 0.f;
 #pragma unroll
-    for (int j = 0; j < NB; ++j) acc[j][e] = v < f.V ? acc[j][e] + bv : -INFINITY;
-  }
+      for (int j = 0; j < NB; ++j) acc[t][j][e] = v < f.V ? acc[t][j][e] + bv : -INFINITY;
+    }
   end(f, acc, v0 + 4 * quad, n, quad, wave);
 }
 
@@ -145,22 +204,26 @@ __device__ __forceinline__ float quads_sum(float v) {
 struct FewStats {
   float2* part;
   float* target;
-  template <int NB>
-  __device__ void operator()(const WnFew& f, f32x4 (&acc)[NB], int v, int n, int quad, int wave) const {
+  template <int T, int NB>
+  __device__ void operator()(const WnFew& f, f32x4 (&acc)[T][NB], int v, int n, int quad, int wave) const {
     __shared__ float2 s[4][16 * NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int r = 16 * j + n;
-      const int t = r < f.N ? f.y[r] : -1;
-      const f32x4 l = acc[j];
-      const float m = quads_max(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])));
+      const int y = r < f.N ? f.y[r] : -1;
+      float m = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < T; ++t) m = fmaxf(m, fmaxf(fmaxf(acc[t][j][0], acc[t][j][1]), fmaxf(acc[t][j][2], acc[t][j][3])));
+      m = quads_max(m);
       const float at = m == -INFINITY ? 0.f : m;
       float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        sum += wnk::expf_fast(l[e] - at);
-        if (t == v + e && t < f.V) target[r] = l[e];
-      }
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sum += wnk::expf_fast(acc[t][j][e] - at);
+          if (y == v + 16 * t + e && y < f.V) target[r] = acc[t][j][e];
+        }
       sum = quads_sum(sum);
       if (quad == 0) s[wave][r] = make_float2(m, sum);
     }
@@ -185,41 +248,54 @@ struct FewGrad {
   E *q, *qt;  // or null
   int vpad, npad;
   float* db;  // or null
-  template <int NB>
-  __device__ void operator()(const WnFew& f, f32x4 (&acc)[NB], int v, int n, int quad, int) const {
-    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+  template <int T, int NB>
+  __device__ void operator()(const WnFew& f, f32x4 (&acc)[T][NB], int first, int n, int quad, int) const {
+    float ln[NB], gn[NB];
+    int y[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int r = 16 * j + n;
-      const int t = r < f.N ? f.y[r] : -1;
-      const bool ok = t >= 0 && t < f.V;
-      const float ln = ok ? lse[r] : 0.f, gn = ok ? g[r] : 0.f;
+      y[j] = r < f.N ? f.y[r] : -1;
+      if (y[j] >= f.V) y[j] = -1;
+      ln[j] = y[j] >= 0 ? lse[r] : 0.f;
+      gn[j] = y[j] >= 0 ? g[r] : 0.f;
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = wnk::expf_fast(acc[j][e] - ln) - (v + e == t ? 1.f : 0.f);
-        acc[j][e] = ok && v + e < f.V ? p * gn : 0.f;
-      }
-      sum += acc[j];
-      if (q && r < f.N && v < vpad) {
+    for (int t = 0; t < T; ++t) {
+      const int v = first + 16 * t;
+      f32x4 sum{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) put(q + (size_t)r * vpad + v + e, acc[j][e]);
+      for (int j = 0; j < NB; ++j) {
+        const int r = 16 * j + n;
+        f32x4 p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = wnk::expf_fast(acc[t][j][e] - ln[j]) - (v + e == y[j] ? 1.f : 0.f);
+          p[e] = y[j] >= 0 && v + e < f.V ? p[e] * gn[j] : 0.f;
+        }
+        sum += p;
+        if (q && r < f.N && v < vpad) {
+          E* d = q + (size_t)r * vpad + v;
+          if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4*>(d) = p;
+          else *reinterpret_cast<u32x2*>(d) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+        }
+        if (qt) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v + e < f.V) put(qt + (size_t)(v + e) * npad + r, p[e]);
+        }
       }
-      if (qt && r < npad) {
+      if (NB == 1 && qt) {  // (bf16 takes 32 rows at a time)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (v + e < f.V) put(qt + (size_t)(v + e) * npad + r, acc[j][e]);
+          if (v + e < f.V) put(qt + (size_t)(v + e) * npad + 16 + n, 0.f);
       }
-    }
-    if (NB == 1 && qt) {  // (bf16 takes 32 rows at a time)
+      if (!db) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v + e < f.V) put(qt + (size_t)(v + e) * npad + 16 + n, 0.f);
-    }
-    if (!db) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float s = wnk::gsum16(sum[e]);
-      if (n == 0 && v + e < f.V) db[v + e] = s;
+      for (int e = 0; e < 4; ++e) {
+        const float s = wnk::gsum16(sum[e]);
+        if (n == 0 && v + e < f.V) db[v + e] = s;
+      }
     }
   }
 };
@@ -336,6 +412,8 @@ __global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int
   constexpr int W = Piece<E>::n, S = kStep<E>, K = (16 * NB + S - 1) / S, kTiles = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
   const int c0 = blockIdx.x * kSlab<E>, c = min(c0 + W * n, f.D - 1);
+  __shared__ __align__(16) char stage[4][16 * 256];
+  char* const mine = stage[wave];
   P<E> a[K][W];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -362,26 +440,39 @@ __global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int
 #pragma unroll
       for (int u = 0; u < W; ++u) acc[u] = mma(a[k][u], b, acc[u]);
     }
-    if (v >= f.V) continue;
+    // lane (n, quad) holds columns W (4 quad + i) .. + W - 1 of class n; through LDS, so that 16 lanes store a class's
+    // 256 bytes (each lane storing its own pieces, 64 places an instruction, 37 rows x 50021 classes x 777 took 44 us)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int k = c0 + W * (4 * quad + i);
-      E* d = dw + (size_t)v * f.D + k;
-      if (k + W <= f.D) {
-        typename Piece<E>::any o;
+      P<E> o;
 #pragma unroll
-        for (int u = 0; u < W; ++u) {
-          E e;
-          put(&e, acc[u][i]);
-          o[u] = e;
-        }
-        *reinterpret_cast<typename Piece<E>::any*>(d) = o;
+      for (int u = 0; u < W; ++u) {
+        E e;
+        put(&e, acc[u][i]);
+        o[u] = e;
+      }
+      const int p = 4 * quad + i;
+      *reinterpret_cast<P<E>*>(mine + n * 256 + ((p ^ n) << 4)) = o;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own part)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * i + quad, k = c0 + W * n;
+      const P<E> o = *reinterpret_cast<const P<E>*>(mine + r * 256 + ((n ^ r) << 4));
+      if (v0 + r >= f.V) continue;
+      E* d = dw + (size_t)(v0 + r) * f.D + k;
+      if (k + W <= f.D) {
+        typename Piece<E>::any x;
+#pragma unroll
+        for (int u = 0; u < W; ++u) x[u] = o[u];
+        *reinterpret_cast<typename Piece<E>::any*>(d) = x;
       } else {
 #pragma unroll
         for (int u = 0; u < W; ++u)
-          if (k + u < f.D) put(d + u, acc[u][i]);
+          if (k + u < f.D) d[u] = o[u];
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
@@ -398,7 +489,7 @@ template <class E>
 hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st) {
   by_tiles(f.N, [&](auto nb) {
     const FewStats end{part, target};
-    hipLaunchKernelGGL((few_logits<E, decltype(nb)::value, FewStats>), dim3((unsigned)ceil_div(f.V, kFewClasses)), dim3(256), 0, st, f, end);
+    hipLaunchKernelGGL((few_logits<E, decltype(nb)::value, FewStats>), dim3((unsigned)ceil_div(f.V, wn_few_classes(f.N))), dim3(256), 0, st, f, end);
   });
   return hipGetLastError();
 }
@@ -406,11 +497,11 @@ hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t 
 WnFewPlan wn_few_plan(bool f32, int N, int D, int V) {
   WnFewPlan p;
   const int step = f32 ? 16 : 32, e = f32 ? 4 : 2, slab = f32 ? 64 : 128;
-  // q's rows hold zeros from V to the last block's end, past which no step reads; each block of dx takes 4 quarters of whole steps, some 1024 blocks
-  p.vpad = (int)ceil_div(V, kFewClasses) * kFewClasses;
+  // q's rows hold zeros from V to the last block's end, past which no step reads; each block of dx takes 4 quarters of whole steps, some 512 blocks
+  p.vpad = (int)ceil_div(V, 64) * 64;
   p.npad = N <= 32 ? 32 : 64;
   p.slabs = (int)ceil_div(D, slab);
-  const size_t want = std::max<size_t>(1, 1024 / p.slabs);
+  const size_t want = std::max<size_t>(1, 512 / p.slabs);
   p.each = (int)(std::max<size_t>(1, ceil_div(V, want * 4 * step)) * 4 * step);
   p.parts = (int)ceil_div(V, p.each);
   p.q_bytes = (size_t)N * p.vpad * e;
@@ -425,7 +516,7 @@ hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, co
   by_tiles(f.N, [&](auto nb) {
     constexpr int NB = decltype(nb)::value, W = Piece<E>::n;
     const FewGrad<E> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad, p.npad, db};
-    hipLaunchKernelGGL((few_logits<E, NB, FewGrad<E>>), dim3((unsigned)ceil_div(f.V, kFewClasses)), dim3(256), 0, st, f, end);
+    hipLaunchKernelGGL((few_logits<E, NB, FewGrad<E>>), dim3((unsigned)ceil_div(f.V, wn_few_classes(f.N))), dim3(256), 0, st, f, end);
     if (dx)
       hipLaunchKernelGGL((few_dx<E, NB>), dim3(p.slabs, p.parts), dim3(256), W * NB * 64 * 16, st, f, static_cast<const E*>(q), p.vpad,
                          p.each, sum);
