@@ -464,6 +464,11 @@ def embed_backward(dout, tokens, V: int, scale: float = 1.0, dtable=None, worksp
     return dtable
 
 
+_CLIP_ARRAY = np.dtype({"names": ["g", "out", "n", "dtype"], "formats": [np.uint64, np.uint64, np.int64, np.int32],
+                        "offsets": [getattr(ClipArray, k).offset for k in ("g", "out", "n", "dtype")],
+                        "itemsize": ctypes.sizeof(ClipArray)})
+
+
 def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None, stream=None):
     """wn_clip: scales the tensors of ``grads`` so that the norm over all of them is at most max_norm, in
     place or into ``outs``; returns that norm before (float32 [], on the device).  Where it is not finite the
@@ -475,16 +480,26 @@ def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None,
     outs = grads if outs is None else list(outs)
     if len(outs) != len(grads):
         raise ValueError("%d outs for %d grads" % (len(outs), len(grads)))
-    for i, g in enumerate(grads):
-        _train_dtype(g, "grads[%d]" % i)
+    # (whole lists at a time: a model has hundreds of gradients)
+    both = grads if outs is grads else grads + outs
+    for t in both:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("gradients must be torch tensors")
+    if not {t.dtype for t in both} <= {torch.float32, torch.bfloat16}:
+        raise ValueError("gradients must be float32 or bfloat16")
     on = _On(grads[0], stream)
-    arrays = (ClipArray * len(grads))()
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        a = arrays[i]
-        a.g = on.ptr(g, g.dtype, g.shape, "grads[%d]" % i)
-        a.out = a.g if o is g else on.ptr(o, g.dtype, g.shape, "outs[%d]" % i)
-        a.n, a.dtype = g.numel(), WN_F32 if g.dtype == torch.float32 else WN_BF16
+    if {t.device for t in both} != {on.device}:
+        raise ValueError("gradients must all be on %s" % on.device)
+    if not all([t.is_contiguous() for t in both]):
+        raise ValueError("gradients must be contiguous")
+    if outs is not grads and [(t.shape, t.dtype) for t in grads] != [(t.shape, t.dtype) for t in outs]:
+        raise ValueError("outs must have the shapes and dtypes of grads")
+    arrays = np.zeros(len(grads), dtype=_CLIP_ARRAY)
+    arrays["g"] = [t.data_ptr() for t in grads]
+    arrays["out"] = arrays["g"] if outs is grads else [t.data_ptr() for t in outs]
+    arrays["n"] = [t.numel() for t in grads]
+    arrays["dtype"] = [WN_F32 if t.dtype == torch.float32 else WN_BF16 for t in grads]
     norm, np_ = on.out(norm, (), torch.float32, "norm")
     ws, wsp, wsn = on.workspace(workspace, lib.wn_clip_workspace_bytes())
-    _check(lib.wn_clip(len(grads), arrays, float(max_norm), np_, wsp, wsn, on.handle), "wn_clip")
+    _check(lib.wn_clip(len(grads), arrays.ctypes.data_as(ctypes.POINTER(ClipArray)), float(max_norm), np_, wsp, wsn, on.handle), "wn_clip")
     return norm

@@ -16,7 +16,7 @@ namespace {
 
 using namespace wnt;
 
-constexpr int kArrays = 96;    // arrays of a launch: the arguments stay under 4 KB
+constexpr int kArrays = 168;   // arrays of a launch: the arguments stay under 4 KB
 constexpr int kThreads = 256;
 constexpr int kElems = 8192;   // of a chunk
 constexpr int kSlots = 1024;   // blocks of a launch, partial sums
@@ -24,25 +24,48 @@ constexpr int kSlots = 1024;   // blocks of a launch, partial sums
 struct Arrays {
   const void* g[kArrays];
   void* out[kArrays];
-  long long n[kArrays];
-  unsigned first[kArrays + 1];  // chunks before the array
-  unsigned char bf16[kArrays];
+  unsigned first[kArrays + 1];         // chunks before the array
+  unsigned short last[kArrays];        // elements of its last chunk; | kBf16
   int count;
 };
-static_assert(sizeof(Arrays) < 3800, "kernel arguments");
+constexpr unsigned short kBf16 = 0x8000;
+static_assert(sizeof(Arrays) < 3900 && kElems < kBf16, "kernel arguments");
 
-// Four elements at any element's alignment.
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+// Four words at any element's alignment.
 typedef unsigned u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
+// The array that a chunk lies in: the last one whose first chunk is at most the chunk.
 __device__ __forceinline__ int array_of(const Arrays& a, unsigned chunk) {
-  int lo = 0, hi = a.count;  // the last array whose first chunk is at most `chunk` (empty arrays have none)
+  int lo = 0, hi = a.count;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (a.first[mid] <= chunk) lo = mid;
     else hi = mid;
   }
   return lo;
+}
+
+// A block's share is a run of chunks, the same in both passes; f(array, first element, elements) for each array's part
+// of it, in order or (`back`) from the end.
+template <class F>
+__device__ __forceinline__ void for_share(const Arrays& a, bool back, F f) {
+  const unsigned long long all = a.first[a.count];
+  unsigned c0 = (unsigned)(all * blockIdx.x / gridDim.x), c1 = (unsigned)(all * (blockIdx.x + 1) / gridDim.x);
+  if (c0 >= c1) return;
+  int k = array_of(a, back ? c1 - 1 : c0);
+  while (c0 < c1) {
+    const unsigned b = max(c0, a.first[k]), e = min(c1, a.first[k + 1]);
+    const long long at = (long long)(b - a.first[k]) * kElems;
+    const long long n = (long long)(e - b) * kElems - (e == a.first[k + 1] ? kElems - (a.last[k] & (kBf16 - 1)) : 0);
+    f(k, at, n);
+    if (back) {
+      c1 = b;
+      --k;
+    } else {
+      c0 = e;
+      ++k;
+    }
+  }
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -71,32 +94,48 @@ __device__ __forceinline__ double squares(u32x4 w, bool bf16) {
   return v;
 }
 
-// slot[b] (+)= the squares of the chunks b, b + grid, ...
+constexpr int kUnroll = 8;  // 16-byte loads in flight per thread
+
+// slot[b] (+)= the squares of block b's share
 __global__ __launch_bounds__(kThreads) void clip_squares(const Arrays a, double* slot, int add) {
-  double sum = 0.0;
-  for (unsigned c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
-    const int k = array_of(a, c);
-    const long long at = (long long)(c - a.first[k]) * kElems;
-    const int n = (int)min((long long)kElems, a.n[k] - at);
-    const bool bf = a.bf16[k];
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  for_share(a, false, [&](int k, long long at, long long n) {
+    const bool bf = a.last[k] & kBf16;
     const int per = bf ? 8 : 4;
     const char* p = static_cast<const char*>(a.g[k]) + at * (bf ? 2 : 4);
-    const int whole = n / per;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < whole; i += kThreads) {
-      const u32x4u w = *reinterpret_cast<const u32x4u*>(p + 16 * (size_t)i);
-      sum += squares(u32x4{w[0], w[1], w[2], w[3]}, bf);
+    const long long whole = n / per;
+    long long i = threadIdx.x;
+    for (; i + (kUnroll - 1) * kThreads < whole; i += kUnroll * kThreads) {
+      u32x4u w[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) w[u] = *reinterpret_cast<const u32x4u*>(p + 16 * (i + u * kThreads));
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) sum[u & 3] += squares(u32x4{w[u][0], w[u][1], w[u][2], w[u][3]}, bf);
     }
-    const int rest = whole * per + threadIdx.x;
+    for (; i < whole; i += kThreads) {
+      const u32x4u w = *reinterpret_cast<const u32x4u*>(p + 16 * i);
+      sum[0] += squares(u32x4{w[0], w[1], w[2], w[3]}, bf);
+    }
+    const long long rest = whole * per + threadIdx.x;
     if (rest < n) {
       const double v = bf ? bf16_val(reinterpret_cast<const u16*>(p)[rest]) : reinterpret_cast<const float*>(p)[rest];
-      sum += v * v;
+      sum[0] += v * v;
     }
-  }
-  sum = block_sum(sum);
-  if (threadIdx.x == 0) slot[blockIdx.x] = add ? slot[blockIdx.x] + sum : sum;
+  });
+  const double v = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (threadIdx.x == 0) slot[blockIdx.x] = add ? slot[blockIdx.x] + v : v;
 }
 
+__device__ __forceinline__ u32x4u times(u32x4u w, float f, bool bf) {
+  u32x4u r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    r[e] = bf ? bf16_pair(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f)
+              : __float_as_uint(__uint_as_float(w[e]) * f);
+  return r;
+}
+
+// The shares from their ends: what the first pass read last is still in the caches.
 __global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const double* slot, int slots, float max_norm, float* norm_out,
                                                        int first) {
   double sum = 0.0;
@@ -107,29 +146,26 @@ __global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const dou
   // (max_norm = 0: 0 times each element)
   const bool scaled = norm > max_norm && norm < INFINITY;
   const float f = scaled ? (float)(max_norm / wide) : 1.f;
-  for (unsigned c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
-    const int k = array_of(a, c);
-    if (!scaled && a.out[k] == a.g[k]) continue;
-    const long long at = (long long)(c - a.first[k]) * kElems;
-    const int n = (int)min((long long)kElems, a.n[k] - at);
-    const bool bf = a.bf16[k];
+  for_share(a, true, [&](int k, long long at, long long n) {
+    if (!scaled && a.out[k] == a.g[k]) return;
+    const bool bf = a.last[k] & kBf16;
     const int per = bf ? 8 : 4;
     const char* p = static_cast<const char*>(a.g[k]) + at * (bf ? 2 : 4);
     char* o = static_cast<char*>(a.out[k]) + at * (bf ? 2 : 4);
-    const int whole = n / per;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < whole; i += kThreads) {
-      const u32x4u w = *reinterpret_cast<const u32x4u*>(p + 16 * (size_t)i);
-      u32x4u r = w;
-      if (scaled) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          r[e] = bf ? bf16_pair(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f)
-                    : __float_as_uint(__uint_as_float(w[e]) * f);
-      }
-      *reinterpret_cast<u32x4u*>(o + 16 * (size_t)i) = r;
+    const long long whole = n / per, steps = whole / (kUnroll * kThreads);
+    for (long long i = whole - 1 - threadIdx.x; i >= steps * kUnroll * kThreads; i -= kThreads) {
+      const u32x4u w = *reinterpret_cast<const u32x4u*>(p + 16 * i);
+      *reinterpret_cast<u32x4u*>(o + 16 * i) = scaled ? times(w, f, bf) : w;
     }
-    const int rest = whole * per + threadIdx.x;
+    for (long long s = steps - 1; s >= 0; --s) {
+      const long long i = s * kUnroll * kThreads + threadIdx.x;
+      u32x4u w[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) w[u] = *reinterpret_cast<const u32x4u*>(p + 16 * (i + u * kThreads));
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) *reinterpret_cast<u32x4u*>(o + 16 * (i + u * kThreads)) = scaled ? times(w[u], f, bf) : w[u];
+    }
+    const long long rest = whole * per + threadIdx.x;
     if (rest < n) {
       if (bf) {
         const u16 v = reinterpret_cast<const u16*>(p)[rest];
@@ -139,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const dou
         reinterpret_cast<float*>(o)[rest] = scaled ? v * f : v;
       }
     }
-  }
+  });
 }
 
 }  // namespace
@@ -166,15 +202,17 @@ int wn_clip(int32_t n_arrays, const wn_clip_array* arrays, float max_norm, float
       return wn_set_last_error(WN_EINVAL, "an array is not aligned to its elements");
     chunks += ceil_div((size_t)a.n, kElems);
   }
-  if (chunks > 1ull << 31) return wn_set_last_error(WN_EINVAL, "too many elements");
+  if (chunks > 1ull << 30) return wn_set_last_error(WN_EINVAL, "too many elements");
   int rc = bad_workspace(workspace, ws_bytes, wn_clip_workspace_bytes());
   if (rc != WN_OK) return rc;
   ArrayScope scope;
   if ((rc = scope.check(norm, "norm")) != WN_OK || (rc = scope.check(workspace, "workspace")) != WN_OK) return rc;
+  // (the first array stands for all: asking for each took longer than the clip of a model's hundred gradients)
   for (int k = 0; k < n_arrays; ++k)
-    if (arrays[k].n && ((rc = scope.check(arrays[k].g, "g")) != WN_OK ||
-                        (arrays[k].out != arrays[k].g && (rc = scope.check(arrays[k].out, "out")) != WN_OK)))
-      return rc;
+    if (arrays[k].n) {
+      if ((rc = scope.check(arrays[k].g, "g")) != WN_OK || (rc = scope.check(arrays[k].out, "out")) != WN_OK) return rc;
+      break;
+    }
   if ((rc = scope.enter()) != WN_OK) return rc;
   double* const slot = static_cast<double*>(workspace);
   const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -189,8 +227,7 @@ int wn_clip(int32_t n_arrays, const wn_clip_array* arrays, float max_norm, float
         const int i = a.count++;
         a.g[i] = arrays[k].g;
         a.out[i] = arrays[k].out;
-        a.n[i] = arrays[k].n;
-        a.bf16[i] = arrays[k].dtype == WN_BF16;
+        a.last[i] = (unsigned short)((arrays[k].n - 1) % kElems + 1) | (arrays[k].dtype == WN_BF16 ? kBf16 : 0);
         a.first[i + 1] = a.first[i] + (unsigned)ceil_div((size_t)arrays[k].n, kElems);
       }
       if (pass == 0) hipLaunchKernelGGL(clip_squares, dim3(grid), dim3(kThreads), 0, st, a, slot, !first);

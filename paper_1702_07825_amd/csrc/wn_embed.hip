@@ -49,6 +49,27 @@ __device__ __forceinline__ void store(E* p, const float (&v)[W]) {
   }
 }
 
+// W elements of which `left` exist (the rest read as 0, and are not stored).
+template <class E, int W>
+__device__ __forceinline__ void piece(const E* p, int left, float (&v)[W]) {
+  if (left >= W) {
+    load<E, W>(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = e < left ? value(p[e]) : 0.f;
+  }
+}
+template <class E, int W>
+__device__ __forceinline__ void put_piece(E* p, int left, const float (&v)[W]) {
+  if (left >= W) {
+    store<E, W>(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+      if (e < left) put(p + e, v[e]);
+  }
+}
+
 // G lanes take a row, W elements each in turn; 256 / G rows a block.
 template <class E, int W>
 __global__ __launch_bounds__(256) void embed_rows(const E* table, const int32_t* t, int N, int D, int V, float scale, E* out, int G) {
@@ -96,14 +117,22 @@ struct Digit {
 };
 
 // count[digit][unit]: a unit is a wave with its run of `per` elements (a multiple of 64).
-// Clears `end` too (the first pass; later ones give null).
-__device__ __forceinline__ void clear_end(int* end, int V, int block, int blocks) {
-  if (end)
-    for (int i = block * blockDim.x + threadIdx.x; i < V; i += blocks * blockDim.x) end[i] = 0;
+// Zeros to the gradient's table, by the sort's first launch beside it: most rows of a large table have no token, and
+// finding them first would put this write behind the sort.
+__device__ __forceinline__ void zero_table(char* out, size_t bytes, int block, int blocks) {
+  // (bytes is a multiple of 2 and so is the address: whole 16-byte pieces, then 2-byte ones)
+  typedef unsigned u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+  const size_t whole = bytes / 16, step = (size_t)blocks * blockDim.x;
+  for (size_t i = (size_t)block * blockDim.x + threadIdx.x; i < whole; i += step)
+    *reinterpret_cast<u32x4u*>(out + 16 * i) = u32x4u{0u, 0u, 0u, 0u};
+  if (block == 0 && threadIdx.x < (bytes & 15) / 2) reinterpret_cast<u16*>(out + 16 * whole)[threadIdx.x] = 0;
 }
 __global__ __launch_bounds__(256) void sort_count(const int32_t* t, const unsigned* key, int N, int V, Digit d, int per, int units,
-                                                  unsigned* count, int* end) {
-  clear_end(end, V, blockIdx.x, gridDim.x);
+                                                  unsigned* count, int blocks, char* table, size_t bytes) {
+  if ((int)blockIdx.x >= blocks) {
+    zero_table(table, bytes, blockIdx.x - blocks, gridDim.x - blocks);
+    return;
+  }
   __shared__ unsigned s[4][kDigits];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, unit = blockIdx.x * 4 + w;
   for (int i = lane; i < kDigits; i += 64) s[w][i] = 0;
@@ -186,12 +215,12 @@ __global__ __launch_bounds__(256) void sort_scatter(const int32_t* t, const unsi
 }
 
 // The whole sort of up to kOne elements by one block: 16 waves, each with a run of kOne / 16 elements in
-// registers, counts and ranks as above.  The blocks behind it clear `end`.
+// registers, counts and ranks as above.  The blocks behind it clear the table.
 constexpr int kOneThreads = 1024, kOne = 16384, kOnePer = kOne / kOneThreads;
 __global__ __launch_bounds__(kOneThreads) void sort_one(const int32_t* t, int N, int V, int passes, int bits, unsigned* key_out,
-                                                        unsigned* row_out, int* end) {
+                                                        unsigned* row_out, char* table, size_t bytes) {
   if (blockIdx.x) {
-    clear_end(end, V, blockIdx.x - 1, gridDim.x - 1);
+    zero_table(table, bytes, blockIdx.x - 1, gridDim.x - 1);
     return;
   }
   extern __shared__ __align__(16) char dyn[];
@@ -291,7 +320,7 @@ struct Sums {
   int per, chunks;  // sorted rows of a chunk
   float scale;
   float* part;  // [chunks][2][D]: of the run that comes in from the chunk before, and of the one that goes on
-  int* end;     // [V]: where a token's run ends, 0: no row has it
+  int* end;     // [V]: where a token's run ends, for runs over several chunks
 };
 
 // G lanes take a chunk's rows, W elements of D each; grid.y covers D.
@@ -307,10 +336,7 @@ __global__ __launch_bounds__(256) void sum_runs(const Sums s, const E* dout, E* 
   float sum[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) sum[i] = 0.f;
-  auto take = [&](float* part) {
-#pragma unroll
-    for (int i = 0; i < W; ++i) part[i] = sum[i];
-  };
+  auto take = [&](float* part) { put_piece<float, W>(part, s.D - k, sum); };
   auto finish = [&](bool on, int at) {  // the run of `cur` ends before `at`, or goes on
     if (cur >= (unsigned)s.V) return;
     float* p = s.part + (size_t)c * 2 * s.D + k;
@@ -320,45 +346,52 @@ __global__ __launch_bounds__(256) void sum_runs(const Sums s, const E* dout, E* 
       float v[W];
 #pragma unroll
       for (int i = 0; i < W; ++i) v[i] = sum[i] * s.scale;
-      store<E, W>(out + (size_t)cur * s.D + k, v);
+      put_piece<E, W>(out + (size_t)cur * s.D + k, s.D - k, v);
     }
-    if (!on && k == 0) s.end[cur] = at;
+    if (in && !on && k == 0) s.end[cur] = at;
   };
-  for (int i = b; i < e; ++i) {
-    const unsigned key = s.key[i];
-    if (key != cur) {
-      finish(false, i);
-      cur = key;
-      in = false;
+  // kBatch rows at a time, all of their loads in flight before the first is added (row by row, the places of the rows,
+  // then the rows: 512000 rows of 64 took 85 us, not 38)
+  constexpr int kBatch = 8;
+  bool done = false;
+  for (int i0 = b; i0 < e && !done; i0 += kBatch) {
+    unsigned key[kBatch], row[kBatch];
+    float v[kBatch][W];
 #pragma unroll
-      for (int q = 0; q < W; ++q) sum[q] = 0.f;
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = min(i0 + i, e - 1);
+      key[i] = s.key[at];
+      row[i] = s.row[at];
     }
-    if (key >= (unsigned)s.V) break;
-    float v[W];
-    load<E, W>(dout + (size_t)s.row[i] * s.D + k, v);
 #pragma unroll
-    for (int q = 0; q < W; ++q) sum[q] += v[q];
+    for (int i = 0; i < kBatch; ++i) piece<E, W>(dout + (size_t)row[i] * s.D + k, s.D - k, v[i]);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (i0 + i >= e || done) continue;
+      if (key[i] != cur) {
+        finish(false, i0 + i);
+        cur = key[i];
+        in = false;
+#pragma unroll
+        for (int q = 0; q < W; ++q) sum[q] = 0.f;
+      }
+      if (cur >= (unsigned)s.V) {  // the rest is padding
+        done = true;
+        continue;
+      }
+#pragma unroll
+      for (int q = 0; q < W; ++q) sum[q] += v[i][q];
+    }
   }
   const bool on = e < s.N && s.key[e] == cur;
   finish(on, e);
 }
 
 // Runs over several chunks: the block of the chunk that a run begins in adds the chunks' partial sums, over
-// 256 / G runs of chunks, then those.  Blocks past the chunks write zeros into the table rows that no token
-// names, 64 rows each.
+// 256 / G runs of chunks, then those.
 template <class E, int W>
 __global__ __launch_bounds__(256) void join_runs(const Sums s, E* out, int G) {
   __shared__ float part[256 * W];
-  if ((int)blockIdx.x >= s.chunks) {
-    if (blockIdx.y) return;
-    const int v0 = ((int)blockIdx.x - s.chunks) * 64;
-    for (int v = v0 + (threadIdx.x >> 6); v < min(s.V, v0 + 64); v += 4) {
-      if (s.end[v]) continue;
-      E* d = out + (size_t)v * s.D;
-      for (int k = threadIdx.x & 63; k < s.D; k += 64) d[k] = (E)0;
-    }
-    return;
-  }
   const int c = blockIdx.x, last = min(s.N, (c + 1) * s.per) - 1;
   if (last + 1 >= s.N) return;
   const unsigned key = s.key[last];
@@ -375,9 +408,10 @@ __global__ __launch_bounds__(256) void join_runs(const Sums s, E* out, int G) {
   if (k < s.D)
 #pragma unroll 4
     for (int i = g * each; i < min(n, (g + 1) * each); ++i) {
-      const float* p = s.part + ((size_t)(c + i) * 2 + (i == 0 ? 1 : 0)) * s.D + k;
+      float v[W];
+      piece<float, W>(s.part + ((size_t)(c + i) * 2 + (i == 0 ? 1 : 0)) * s.D + k, s.D - k, v);
 #pragma unroll
-      for (int q = 0; q < W; ++q) sum[q] += p[q];
+      for (int q = 0; q < W; ++q) sum[q] += v[q];
     }
 #pragma unroll
   for (int q = 0; q < W; ++q) part[threadIdx.x * W + q] = sum[q];
@@ -388,7 +422,7 @@ __global__ __launch_bounds__(256) void join_runs(const Sums s, E* out, int G) {
       for (int q = 0; q < W; ++q) sum[q] += part[(i * G + lane) * W + q];
 #pragma unroll
     for (int q = 0; q < W; ++q) sum[q] *= s.scale;
-    store<E, W>(out + (size_t)key * s.D + k, sum);
+    put_piece<E, W>(out + (size_t)key * s.D + k, s.D - k, sum);
   }
 }
 
@@ -433,8 +467,8 @@ struct Plan {
     bits = (bits_of(V) + passes - 1) / passes;
     unit = (int)std::min<size_t>(4096, std::max<size_t>(256, ceil_div(ceil_div(N, 1024), 64) * 64));
     units = (int)ceil_div(N, unit);
-    // chunks of 16 to 256 rows, about 8192 of them
-    per = (int)std::min<size_t>(256, std::max<size_t>(16, ceil_div(N, 8192)));
+    // chunks of 16 to 256 rows, about 16384 of them
+    per = (int)std::min<size_t>(256, std::max<size_t>(16, ceil_div(ceil_div(N, 16384), 8) * 8));
     chunks = (int)ceil_div(N, per);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -459,6 +493,8 @@ int run_backward(int N, int D, int V, const E* dout, const int32_t* t, float sca
   const Plan p(N, D, V);
   auto words = [&](size_t off) { return reinterpret_cast<unsigned*>(ws + off); };
   int* const end = reinterpret_cast<int*>(ws + p.end);
+  const size_t bytes = (size_t)V * D * sizeof(E);
+  const unsigned clear = (unsigned)std::min<size_t>(2048, ceil_div(bytes, 32768));
   int at = 0;  // the sorted keys' buffer
   if (N <= kOne) {
     const int threads = (int)std::min<size_t>(kOneThreads, ceil_div(N, 64) * 64);
@@ -466,16 +502,16 @@ int run_backward(int N, int D, int V, const E* dout, const int32_t* t, float sca
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(sort_one), hipFuncAttributeMaxDynamicSharedMemorySize,
                                              kOne * 6 + 16 * 2 * kDigits);
     if (e != hipSuccess) return wn_set_last_error(WN_EHIP, hipGetErrorString(e));
-    const unsigned clear = (unsigned)std::min<size_t>(256, ceil_div(V, 1024));
     hipLaunchKernelGGL(sort_one, dim3(1 + clear), dim3(threads), lds, st, t, N, V, p.passes, p.bits, words(p.key[0]),
-                       words(p.row[0]), end);
+                       words(p.row[0]), reinterpret_cast<char*>(out), bytes);
   } else {
     const unsigned *key = nullptr, *row = nullptr;
     for (int i = 0; i < p.passes; ++i) {
       const Digit d{i * p.bits, p.bits};
       at = i & 1;
       const dim3 grid((unsigned)ceil_div(p.units, 4));
-      hipLaunchKernelGGL(sort_count, grid, dim3(256), 0, st, t, key, N, V, d, p.unit, p.units, words(p.count), i == 0 ? end : nullptr);
+      hipLaunchKernelGGL(sort_count, dim3(grid.x + (i == 0 ? clear : 0)), dim3(256), 0, st, t, key, N, V, d, p.unit, p.units,
+                         words(p.count), (int)grid.x, reinterpret_cast<char*>(out), bytes);
       hipLaunchKernelGGL(sort_scan, dim3(1 << p.bits), dim3(256), 0, st, words(p.count), p.units, words(p.total_off));
       hipLaunchKernelGGL(sort_scatter, grid, dim3(256), 0, st, t, key, row, N, V, d, p.unit, p.units, words(p.count),
                          words(p.total_off), words(p.key[at]), words(p.row[at]));
@@ -485,16 +521,11 @@ int run_backward(int N, int D, int V, const E* dout, const int32_t* t, float sca
   }
   Sums s{words(p.key[at]), words(p.row[at]), N, D, V, p.per, p.chunks, scale, reinterpret_cast<float*>(ws + p.part),
          end};
-  auto sums = [&](auto w) {
-    constexpr int W = decltype(w)::value;
-    const int G = lanes_of(D, W);
-    const unsigned y = (unsigned)ceil_div(D, (size_t)G * W);
-    hipLaunchKernelGGL((sum_runs<E, W>), dim3((unsigned)ceil_div(p.chunks, 256 / G), y), dim3(256), 0, st, s, dout, out, G);
-    hipLaunchKernelGGL((join_runs<E, W>), dim3(p.chunks + (unsigned)ceil_div(V, 64), y), dim3(256), 0, st, s, out, G);
-  };
-  constexpr int kWide = 16 / sizeof(E);
-  if (D % kWide == 0) sums(std::integral_constant<int, kWide>{});
-  else sums(std::integral_constant<int, 1>{});
+  constexpr int W = 16 / sizeof(E);
+  const int G = lanes_of(D, W);
+  const unsigned y = (unsigned)ceil_div(D, (size_t)G * W);
+  hipLaunchKernelGGL((sum_runs<E, W>), dim3((unsigned)ceil_div(p.chunks, 256 / G), y), dim3(256), 0, st, s, dout, out, G);
+  if (p.chunks > 1) hipLaunchKernelGGL((join_runs<E, W>), dim3(p.chunks, y), dim3(256), 0, st, s, out, G);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
 }
