@@ -216,6 +216,34 @@ int wn_teacher_force(wn_handle* h, int32_t B, int32_t T, const float* cond, cons
                      float* logits, void* workspace, size_t ws_bytes, int32_t reset, void* stream);
 
 /*
+ * Teacher forcing that stops before the last product: features = relu(W_relu relu(q) + B_relu), the input of W_out
+ * (logits = W_out features + B_out).  With wn_loss_backward (wn_train.h) they give the gradients of an output layer
+ * that is adapted to recorded speech while the layers below stay.
+ *   features  device fp32 [B][T][a] out
+ * Other arguments and errors as wn_teacher_force, and WN_EUNSUPPORTED where teacher forcing goes step by step
+ * (a handle that WN_KERNEL binds; 1100 and more streams on the batched kernel: split the batch).  The
+ * workspace must hold all of wn_workspace_bytes.
+ */
+int wn_teacher_features(wn_handle* h, int32_t B, int32_t T, const float* cond, const int32_t* y, float* features,
+                        void* workspace, size_t ws_bytes, int32_t reset, void* stream);
+
+/*
+ * Scores recorded speech: nll[b][t] = -log softmax(logits of step t)[y[b][t]], teacher forcing's logits (which it
+ * does not write) with the softmax of wn_loss (wn_train.h; exact exponentials whatever the nonlinearity).  A step
+ * whose y is outside 0 .. a-1 (padding) scores 0 and enters the next step clamped, as in wn_teacher_force.
+ *   nll      device fp32 [B][T] out
+ *   scratch  device, >= wn_score_scratch_bytes(h, B, T) bytes, 256-byte aligned; it holds nothing between calls
+ * The workspace is wn_teacher_force's and its state continues as there.  Errors as wn_teacher_features, and WN_EINVAL for
+ * a null, misaligned or short scratch.  A call that wn_abort ends leaves nll undefined from that step on (wn_status).
+ */
+int wn_score(wn_handle* h, int32_t B, int32_t T, const float* cond, const int32_t* y, float* nll, void* workspace,
+             size_t ws_bytes, void* scratch, size_t scratch_bytes, int32_t reset, void* stream);
+
+/* Bytes of wn_score's scratch (0 for a null handle, B < 1 or T < 1): a KB for each step, whose
+ * features it holds, and some MB. */
+size_t wn_score_scratch_bytes(const wn_handle* h, int32_t B, int32_t T);
+
+/*
  * Wait for `stream` and return the status word the kernels left in `workspace`:
  * WN_OK, WN_ETIMEOUT or WN_EABORTED; WN_EINVAL for null arguments; WN_EHIP if
  * the stream reports an error.  Blocks the calling thread.  The waits for other CUs, in the

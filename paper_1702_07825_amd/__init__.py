@@ -22,7 +22,8 @@ WN_OK, WN_EINVAL, WN_EUNSUPPORTED, WN_ENOMEM, WN_EHIP, WN_ETIMEOUT, WN_EABORTED 
 WN_F32, WN_BF16, WN_I8 = 0, 1, 2
 WN_NONLIN_EXACT, WN_NONLIN_PAPER = 0, 1
 A_CLASSES = 256
-EXPORTED = ("wn_create", "wn_workspace_bytes", "wn_generate", "wn_generate_sampled", "wn_teacher_force", "wn_status",
+EXPORTED = ("wn_create", "wn_workspace_bytes", "wn_generate", "wn_generate_sampled", "wn_teacher_force",
+            "wn_teacher_features", "wn_score", "wn_score_scratch_bytes", "wn_status",
             "wn_abort", "wn_kernel_variant", "wn_launch_info", "wn_destroy", "wn_error_string", "wn_last_error",
             "wn_cond_create", "wn_cond_workspace_bytes", "wn_condition", "wn_condition_static", "wn_cond_destroy",
             "wn_loss", "wn_loss_workspace_bytes", "wn_loss_backward", "wn_loss_backward_workspace_bytes",
@@ -122,6 +123,12 @@ def load_library(path: str = LIB_PATH):
         L.wn_clip_workspace_bytes.argtypes = []
         L.wn_teacher_force.restype = ctypes.c_int
         L.wn_teacher_force.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, vp]
+        L.wn_teacher_features.restype = ctypes.c_int
+        L.wn_teacher_features.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, vp]
+        L.wn_score.restype = ctypes.c_int
+        L.wn_score.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, vp, sz, i32, vp]
+        L.wn_score_scratch_bytes.restype = sz
+        L.wn_score_scratch_bytes.argtypes = [vp, i32, i32]
         L.wn_status.restype = ctypes.c_int
         L.wn_status.argtypes = [vp, vp, vp]
         L.wn_abort.restype = ctypes.c_int
@@ -268,6 +275,33 @@ class WaveNet:
                                           1 if reset else 0, _stream_handle(stream)), "wn_teacher_force")
         return logits
 
+    def teacher_features(self, cond, y, features=None, workspace=None, reset: bool = True, stream=None):
+        """wn_teacher_features: cond fp32 [B,T,l,2r], y int32 [B,T] (device) -> fp32 [B,T,a], the input of w_out."""
+        import torch
+        on = _On(cond, stream)
+        B, T = int(cond.shape[0]), int(cond.shape[1])
+        cp = on.ptr(cond, torch.float32, (B, T, self.n_layers, 2 * self.r), "cond")
+        yp = on.ptr(y, torch.int32, (B, T), "y")
+        features, fp = on.out(features, (B, T, self.a), torch.float32, "features")
+        ws, wsp, wsn = on.workspace(workspace, self.workspace_bytes(B))
+        _check(self._lib.wn_teacher_features(self._h, B, T, cp, yp, fp, wsp, wsn, 1 if reset else 0, on.handle),
+               "wn_teacher_features")
+        return features
+
+    def score(self, cond, y, nll=None, workspace=None, scratch=None, reset: bool = True, stream=None):
+        """wn_score: cond fp32 [B,T,l,2r], y int32 [B,T] (device) -> fp32 [B,T], -log of the probability that the model
+        gives each sample; 0 where y is outside 0..a-1 (padding)."""
+        import torch
+        on = _On(cond, stream)
+        B, T = int(cond.shape[0]), int(cond.shape[1])
+        cp = on.ptr(cond, torch.float32, (B, T, self.n_layers, 2 * self.r), "cond")
+        yp = on.ptr(y, torch.int32, (B, T), "y")
+        nll, np_ = on.out(nll, (B, T), torch.float32, "nll")
+        ws, wsp, wsn = on.workspace(workspace, self.workspace_bytes(B))
+        sc, scp, scn = on.workspace(scratch, int(self._lib.wn_score_scratch_bytes(self._h, B, T)))
+        _check(self._lib.wn_score(self._h, B, T, cp, yp, np_, wsp, wsn, scp, scn, 1 if reset else 0, on.handle), "wn_score")
+        return nll
+
     def abort(self, on: bool = True):
         """wn_abort: ask this model's running and later calls to stop early (on=False withdraws it)."""
         _check(self._lib.wn_abort(self._h, 1 if on else 0), "wn_abort")
@@ -357,27 +391,37 @@ class _On:
 
     def __init__(self, t, stream):
         import torch
-        if t.device.type != "cuda":
+        self.device = device = t.device
+        if device.type != "cuda":
             raise ValueError("tensors must be on a GPU device")
-        self.device = t.device
-        self.stream = torch.cuda.current_stream(t.device) if stream is None else stream
-        if self.stream.device != t.device:
-            raise ValueError("stream is of %s, the tensors are on %s" % (self.stream.device, t.device))
-        self.handle = self.stream.cuda_stream
+        self.other = None  # a stream that is not the current one
+        s = torch.cuda.current_stream(device)
+        if stream is not None and stream != s:
+            if stream.device != device:
+                raise ValueError("stream is of %s, the tensors are on %s" % (stream.device, device))
+            self.other = s = stream
+        self.handle = s.cuda_stream
 
     def empty(self, shape, dtype):
         import torch
-        if self.stream == torch.cuda.current_stream(self.device):
+        if self.other is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self.stream):
+        with torch.cuda.stream(self.other):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def out(self, t, shape, dtype, name):
-        t = self.empty(shape, dtype) if t is None else t
+        if t is None:
+            t = self.empty(shape, dtype)
+            return t, t.data_ptr()
         return t, self.ptr(t, dtype, shape, name)
 
     def ptr(self, t, dtype, shape, name):
-        p = _dev_ptr(t, dtype, shape, name)
+        try:
+            if t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
+                return t.data_ptr()
+        except AttributeError:
+            pass
+        p = _dev_ptr(t, dtype, shape, name)  # (says what is wrong)
         if t.device != self.device:
             raise ValueError("%s is on %s, not on %s" % (name, t.device, self.device))
         return p

@@ -388,17 +388,18 @@ __global__ __launch_bounds__(256) void sum_runs(const Sums s, const E* dout, E* 
 }
 
 // Runs over several chunks: the block of the chunk that a run begins in adds the chunks' partial sums, over
-// 256 / G runs of chunks, then those.
+// kJoin / G runs of chunks, then those.
+constexpr int kJoin = 512;
 template <class E, int W>
-__global__ __launch_bounds__(256) void join_runs(const Sums s, E* out, int G) {
-  __shared__ float part[256 * W];
+__global__ __launch_bounds__(kJoin) void join_runs(const Sums s, E* out, int G) {
+  __shared__ float part[kJoin * W];
   const int c = blockIdx.x, last = min(s.N, (c + 1) * s.per) - 1;
   if (last + 1 >= s.N) return;
   const unsigned key = s.key[last];
   if (key >= (unsigned)s.V || s.key[last + 1] != key) return;
   const int b = c * s.per;
   if (b > 0 && s.key[b - 1] == key) return;  // it began before
-  const int lane = threadIdx.x & (G - 1), g = threadIdx.x / G, groups = 256 / G;
+  const int lane = threadIdx.x & (G - 1), g = threadIdx.x / G, groups = kJoin / G;
   const int n = (s.end[key] - 1) / s.per - c + 1;  // chunks
   const int each = (n + groups - 1) / groups;
   const int k = (blockIdx.y * G + lane) * W;
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(256) void join_runs(const Sums s, E* out, int G) {
 #pragma unroll
   for (int i = 0; i < W; ++i) sum[i] = 0.f;
   if (k < s.D)
-#pragma unroll 4
+#pragma unroll 8
     for (int i = g * each; i < min(n, (g + 1) * each); ++i) {
       float v[W];
       piece<float, W>(s.part + ((size_t)(c + i) * 2 + (i == 0 ? 1 : 0)) * s.D + k, s.D - k, v);
@@ -467,8 +468,8 @@ struct Plan {
     bits = (bits_of(V) + passes - 1) / passes;
     unit = (int)std::min<size_t>(4096, std::max<size_t>(256, ceil_div(ceil_div(N, 1024), 64) * 64));
     units = (int)ceil_div(N, unit);
-    // chunks of 16 to 256 rows, about 16384 of them
-    per = (int)std::min<size_t>(256, std::max<size_t>(16, ceil_div(ceil_div(N, 16384), 8) * 8));
+    // chunks of 16 to 256 rows, about 8192 of them
+    per = (int)std::min<size_t>(256, std::max<size_t>(16, ceil_div(ceil_div(N, 8192), 8) * 8));
     chunks = (int)ceil_div(N, per);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -525,7 +526,7 @@ int run_backward(int N, int D, int V, const E* dout, const int32_t* t, float sca
   const int G = lanes_of(D, W);
   const unsigned y = (unsigned)ceil_div(D, (size_t)G * W);
   hipLaunchKernelGGL((sum_runs<E, W>), dim3((unsigned)ceil_div(p.chunks, 256 / G), y), dim3(256), 0, st, s, dout, out, G);
-  if (p.chunks > 1) hipLaunchKernelGGL((join_runs<E, W>), dim3(p.chunks, y), dim3(256), 0, st, s, out, G);
+  if (p.chunks > 1) hipLaunchKernelGGL((join_runs<E, W>), dim3(p.chunks, y), dim3(kJoin), 0, st, s, out, G);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
 }

@@ -4,6 +4,7 @@
 #include "wn_internal.h"
 #include "wn_teach.h"
 #include "wn_tiny.h"
+#include "wn_train.h"
 
 #include <algorithm>
 #include <cmath>
@@ -251,7 +252,7 @@ int check_call(wn_handle* h, int B, int T, const void* cond, const void* a1, con
 
 // Teacher forcing of every step at once, on the state of the family that generates with B streams.
 int launch_teach(wn_handle* h, int B, int T, const float* cond, const int32_t* y_in, float* logits, const WsLayout& l,
-                 char* base, int reset, hipStream_t st) {
+                 char* base, int reset, hipStream_t st, bool features = false) {
   WnTeachArgs g{};
   WnChainPlan plan;
   const int variant = variant_for(h, B);
@@ -269,6 +270,7 @@ int launch_teach(wn_handle* h, int B, int T, const float* cond, const int32_t* y
   g.io.cond = cond;
   g.io.y_in = y_in;
   g.io.logits = logits;
+  g.io.features = features;
   g.io.B = B;
   g.io.T = T;
   g.io.reset = reset;
@@ -413,6 +415,29 @@ int launch(wn_handle* h, int B, int T, const float* cond, const float* u, const 
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return WN_OK;
 }
+
+// Teacher forcing up to the last product's input, which only the kernels that take all steps at once give.
+int launch_features(wn_handle* h, int B, int T, const float* cond, const int32_t* y, float* features, void* ws, size_t ws_bytes,
+                    int reset, void* stream) {
+  const WsLayout l = ws_layout(h, B);
+  if (!teach_ok(h, B)) return fail(WN_EUNSUPPORTED, "teacher forcing of this handle and batch goes step by step");
+  if (ws_bytes < l.total + teach_bytes(h, B)) return fail(WN_EINVAL, "workspace too small");
+  return launch_teach(h, B, T, cond, y, features, l, static_cast<char*>(ws), reset, static_cast<hipStream_t>(stream), true);
+}
+
+// wn_score's scratch: the features of every step, and the loss of kScoreRows rows at a time.
+constexpr int64_t kScoreRows = 1 << 18;
+struct ScoreLayout {
+  size_t lse_off, loss_off, total;
+  ScoreLayout(int64_t rows) {
+    const int64_t part = std::min(rows, kScoreRows);
+    lse_off = align_up((size_t)rows * WN_A * 4, 256);
+    loss_off = align_up(lse_off + (size_t)part * 4, 256);
+    // (the last call of a scoring has fewer rows; a few rows take another plan)
+    total = loss_off + std::max(wn_loss_workspace_bytes(WN_F32, (int32_t)part, WN_A, WN_A),
+                                wn_loss_workspace_bytes(WN_F32, (int32_t)std::min<int64_t>(part, 64), WN_A, WN_A));
+  }
+};
 
 }  // namespace
 
@@ -688,6 +713,43 @@ int wn_teacher_force(wn_handle* h, int32_t B, int32_t T, const float* cond, cons
   int rc = check_call(h, B, T, cond, y, logits, workspace, ws_bytes, reset);
   if (rc != WN_OK || T == 0) return rc;
   return launch(h, B, T, cond, nullptr, y, nullptr, logits, workspace, ws_bytes, reset, stream, true, kDirect);
+}
+
+int wn_teacher_features(wn_handle* h, int32_t B, int32_t T, const float* cond, const int32_t* y, float* features,
+                        void* workspace, size_t ws_bytes, int32_t reset, void* stream) {
+  g_err.clear();
+  int rc = check_call(h, B, T, cond, y, features, workspace, ws_bytes, reset);
+  if (rc != WN_OK || T == 0) return rc;
+  DeviceScope scope(h->device);
+  if (!scope.ok()) return fail(WN_EHIP, "cannot select the handle's device");
+  return launch_features(h, B, T, cond, y, features, workspace, ws_bytes, reset, stream);
+}
+
+size_t wn_score_scratch_bytes(const wn_handle* h, int32_t B, int32_t T) {
+  if (!h || B < 1 || T < 1 || (size_t)B * (size_t)T > (size_t)1 << 40) return 0;
+  return ScoreLayout((int64_t)B * T).total;
+}
+
+int wn_score(wn_handle* h, int32_t B, int32_t T, const float* cond, const int32_t* y, float* nll, void* workspace,
+             size_t ws_bytes, void* scratch, size_t scratch_bytes, int32_t reset, void* stream) {
+  g_err.clear();
+  int rc = check_call(h, B, T, cond, y, nll, workspace, ws_bytes, reset);
+  if (rc != WN_OK || T == 0) return rc;
+  if (!scratch) return fail(WN_EINVAL, "null scratch");
+  if (reinterpret_cast<uintptr_t>(scratch) % 256 != 0) return fail(WN_EINVAL, "scratch must be 256-byte aligned");
+  const int64_t rows = (int64_t)B * T;
+  const ScoreLayout s(rows);
+  if (scratch_bytes < s.total) return fail(WN_EINVAL, "scratch too small");
+  DeviceScope scope(h->device);
+  if (!scope.ok()) return fail(WN_EHIP, "cannot select the handle's device");
+  char* const base = static_cast<char*>(scratch);
+  float* const features = reinterpret_cast<float*>(base);
+  rc = launch_features(h, B, T, cond, y, features, workspace, ws_bytes, reset, stream);
+  const WnDevWeights& w = h->dmem_f32 ? h->w_chain : h->w;
+  for (int64_t r = 0; rc == WN_OK && r < rows; r += kScoreRows)
+    rc = wn_loss(WN_F32, (int32_t)std::min(kScoreRows, rows - r), WN_A, WN_A, features + r * WN_A, w.w_out, w.b_out, y + r,
+                 nll + r, reinterpret_cast<float*>(base + s.lse_off), base + s.loss_off, s.total - s.loss_off, stream);
+  return rc;
 }
 
 int wn_status(wn_handle* h, const void* workspace, void* stream) {

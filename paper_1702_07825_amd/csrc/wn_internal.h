@@ -56,7 +56,8 @@ struct WnIO {
   const float* u;       // [B][T]            (generation)
   const int32_t* y_in;  // [B][T]            (teacher forcing)
   int32_t* y_out;       // [B][T]            (generation)
-  float* logits;        // [B][T][A]         (teacher forcing)
+  float* logits;        // [B][T][A]         (teacher forcing); with `features` what W_out would multiply
+  int features;         // teacher forcing at once: 1 = stop before the last product
   int B, T, reset, init_sample;
   // how a step's distribution becomes its sample (generation): wn_sample_mode_t, 1 / temperature,
   // k of top-k sampling

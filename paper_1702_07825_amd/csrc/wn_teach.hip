@@ -391,7 +391,7 @@ __device__ __forceinline__ void head_product(f32x4 (&acc)[A / 16 / W][NC], const
 }
 
 // The head of a tile: Z [16 NC][pitch(S)] holds relu(q); ZA [16 NC][pitch(A)] takes z_a.  out(m, c, v)
-// takes the logits c .. c + 3 of row m.  The caller's barrier orders Z.
+// takes the logits (with io.features z_a itself) c .. c + 3 of row m.  The caller's barrier orders Z.
 template <int S, int NC, int W, class Out>
 __device__ __forceinline__ void head_tile(const WnTeachArgs& g, const float* Z, float* ZA, Out out) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, quad = lane >> 4;
@@ -411,9 +411,11 @@ __device__ __forceinline__ void head_tile(const WnTeachArgs& g, const float* Z, 
       f32x4 v = acc[i][k] + br[i];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], 0.f);
-      st4(ZA + (16 * k + n) * pitch(A) + c, v);
+      if (g.io.features) out(16 * k + n, c, v);
+      else st4(ZA + (16 * k + n) * pitch(A) + c, v);
     }
   }
+  if (g.io.features) return;
   lds_barrier();
   head_product<A, NC, W>(acc, g.p.out, ZA, wave);
 #pragma unroll
@@ -985,13 +987,15 @@ __global__ __launch_bounds__(64) void small_head(const WnTeachArgs g, const Smal
   issued();
   mma_rows<K>(acc, w, x);
   f32x4 v = acc + b;
-  if (LAST) {
+  if (!LAST) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], 0.f);
+  }
+  if (LAST || g.io.features) {
     const SmallTile st(g, tile);
     const int T = g.io.T;
     if (n < st.M) st4(g.io.logits + ((size_t)(st.b0 + n / T) * T + n % T) * A + c, v);
   } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], 0.f);
     st4(s.za + ((size_t)tile * 16 + n) * A + c, v);
   }
 }
@@ -1173,7 +1177,7 @@ hipError_t run_small(const WnTeachArgs& g, Small s, hipStream_t st) {
   else hipLaunchKernelGGL((small_chain<R, AX, false>), dim3(s.tiles), dim3(64 * small_waves(R)), lds, st, g, s);
   hipLaunchKernelGGL((small_skip<R, S>), dim3(S / 16, s.tiles), dim3(1024), 0, st, g, s);
   hipLaunchKernelGGL((small_head<S, false>), dim3(A / 16, s.tiles), dim3(64), 0, st, g, s);
-  hipLaunchKernelGGL((small_head<A, true>), dim3(A / 16, s.tiles), dim3(64), 0, st, g, s);
+  if (!g.io.features) hipLaunchKernelGGL((small_head<A, true>), dim3(A / 16, s.tiles), dim3(64), 0, st, g, s);
   return hipGetLastError();
 }
 
