@@ -68,8 +68,8 @@ size_t wn_loss_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V);
  *   g     fp32 [N] upstream gradients (1 / rows for a mean)
  *   dx    [N][D] out, or NULL if not wanted; 0 in rows without a target, whatever x, lse and g hold there
  *   dw    [V][D] out, or NULL;   db fp32 [V] out, or NULL (with b NULL it is the gradient at b = 0)
- * With dtype WN_BF16 q enters the last two products rounded to bf16 (db sums it in fp32); with
- * WN_F32 as fp16 parts, as in wn_loss.  Sizes and errors as wn_loss; all three outputs NULL is
+ * With dtype WN_BF16 q / g (dx) and q / max |g| (dw) enter the last two products rounded to bf16 (db sums q in
+ * fp32); with WN_F32 as fp16 parts, as in wn_loss.  Sizes and errors as wn_loss; all three outputs NULL is
  * an error.  N = 0: dw and db are zeroed.
  */
 int wn_loss_backward(int32_t dtype, int32_t N, int32_t D, int32_t V, const void* x, const void* w, const float* b,

@@ -201,6 +201,14 @@ __device__ __forceinline__ float quads_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
+// Over the 16 lanes of a row of lanes.
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, wnk::dpp<0xB1>(v));
+  v = fmaxf(v, wnk::dpp<0x4E>(v));
+  v = fmaxf(v, wnk::dpp<0x141>(v));
+  return fmaxf(v, wnk::dpp<0x140>(v));
+}
+
 struct FewStats {
   float2* part;
   float* target;
@@ -241,7 +249,8 @@ struct FewStats {
   }
 };
 
-// g q as the operands of dx ([n][v]) and dw ([v][n]), and db, all of whose rows are here.
+// q as the operand of dx ([n][v]; its rows take g where their parts are joined), q g / max |g| as that of dw ([v][n]), so
+// that rounding to bf16 leaves the targets' entries near -1 alone; and db, all of whose rows are here.
 template <class E>
 struct FewGrad {
   const float *lse, *g;
@@ -250,7 +259,7 @@ struct FewGrad {
   float* db;  // or null
   template <int T, int NB>
   __device__ void operator()(const WnFew& f, f32x4 (&acc)[T][NB], int first, int n, int quad, int) const {
-    float ln[NB], gn[NB];
+    float ln[NB], gn[NB], most = 0.f;
     int y[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -259,7 +268,9 @@ struct FewGrad {
       if (y[j] >= f.V) y[j] = -1;
       ln[j] = y[j] >= 0 ? lse[r] : 0.f;
       gn[j] = y[j] >= 0 ? g[r] : 0.f;
+      most = fmaxf(most, fabsf(gn[j]));
     }
+    most = row16_max(most);
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int v = first + 16 * t;
@@ -271,18 +282,19 @@ struct FewGrad {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           p[e] = wnk::expf_fast(acc[t][j][e] - ln[j]) - (v + e == y[j] ? 1.f : 0.f);
-          p[e] = y[j] >= 0 && v + e < f.V ? p[e] * gn[j] : 0.f;
+          p[e] = y[j] >= 0 && v + e < f.V ? p[e] : 0.f;
         }
-        sum += p;
+        sum += p * gn[j];
         if (q && r < f.N && v < vpad) {
           E* d = q + (size_t)r * vpad + v;
           if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4*>(d) = p;
           else *reinterpret_cast<u32x2*>(d) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
         }
         if (qt) {
+          const float gh = most != 0.f ? gn[j] / most : 0.f;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (v + e < f.V) put(qt + (size_t)(v + e) * npad + r, p[e]);
+            if (v + e < f.V) put(qt + (size_t)(v + e) * npad + r, p[e] * gh);
         }
       }
       if (NB == 1 && qt) {  // (bf16 takes 32 rows at a time)
@@ -408,10 +420,17 @@ __global__ __launch_bounds__(256, 2) void few_dx(const WnFew f, const E* q, int 
 
 // dw: a wave keeps its slab of x's columns in registers and goes over its classes, 16 at a time.
 template <class E, int NB>
-__global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int npad, E* dw) {
+__global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int npad, const float* g, E* dw) {
   constexpr int W = Piece<E>::n, S = kStep<E>, K = (16 * NB + S - 1) / S, kTiles = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
   const int c0 = blockIdx.x * kSlab<E>, c = min(c0 + W * n, f.D - 1);
+  float most = 0.f;  // max |g|, which q was divided by
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int r = 16 * j + n, t = r < f.N ? f.y[r] : -1;
+    if (t >= 0 && t < f.V) most = fmaxf(most, fabsf(g[r]));
+  }
+  most = row16_max(most);
   __shared__ __align__(16) char stage[4][16 * 256];
   char* const mine = stage[wave];
   P<E> a[K][W];
@@ -448,7 +467,7 @@ __global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int
 #pragma unroll
       for (int u = 0; u < W; ++u) {
         E e;
-        put(&e, acc[u][i]);
+        put(&e, acc[u][i] * most);
         o[u] = e;
       }
       const int p = 4 * quad + i;
@@ -522,7 +541,7 @@ hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, co
                          p.each, sum);
     if (dw)
       hipLaunchKernelGGL((few_dw<E, NB>), dim3(p.slabs, (unsigned)ceil_div(f.V, 256)), dim3(256), 0, st, f, static_cast<const E*>(qt),
-                         p.npad, static_cast<E*>(dw));
+                         p.npad, g, static_cast<E*>(dw));
   });
   return hipGetLastError();
 }

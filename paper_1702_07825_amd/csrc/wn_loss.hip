@@ -3,7 +3,7 @@
 //
 // Everything heavy is one product C[b][a] = sum_k A[a][k] B[b][k] with different ends (product):
 //   logits   A = w, B = x           the tile's largest logit and sum of exponentials of each row (forward), or
-//                                   q = g (exp(l - lse) - [v = y]) as the next products' operand (backward)
+//                                   q = exp(l - lse) - [v = y] as the next products' operand (backward)
 //   dx       A = w transposed, B = q
 //   dw       A = x transposed, B = q transposed
 // Both operands lie along k in memory, so the transposed ones are copies (pack_cols); the backward pass takes
@@ -334,7 +334,26 @@ struct StatsEnd {
   }
 };
 
-// 16-bit operand units of q (three forms: bf16, or the fp16 parts of q 2^14).
+// Largest |g| of the rows with a target: parts[blockIdx.x] of each block's, joined by whoever needs it.
+constexpr int kGParts = 64;
+__global__ __launch_bounds__(256) void largest_g(const float* g, const int32_t* y, int N, int V, float* parts) {
+  __shared__ float s[4];
+  float m = 0.f;
+  for (int n = blockIdx.x * 256 + threadIdx.x; n < N; n += gridDim.x * 256) {
+    const int t = y[n];
+    if (t >= 0 && t < V) m = fmaxf(m, fabsf(g[n]));
+  }
+  m = wnk::wave_max(m);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) parts[blockIdx.x] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+}
+__device__ __forceinline__ float join_largest(const float* parts, int n) {
+  const int lane = threadIdx.x & 63;
+  return wnk::wave_max(lane < n ? parts[lane] : 0.f);
+}
+
+// 16-bit operand units of q (bf16, or the fp16 parts of q 2^14).
 constexpr int kQScale = 14;
 __device__ __forceinline__ void split(float v, u16& hi, u16& lo) {
   const _Float16 h = (_Float16)v;
@@ -344,19 +363,26 @@ __device__ __forceinline__ void split(float v, u16& hi, u16& lo) {
 }
 
 // Backward: q of the tile's rows and classes as the operands of dx ([n][v]) and dw ([v][n]), and the sums of g q
-// over the tile's rows.  fp32: q without g (|q| <= 1); bf16: g q.  A lane holds four classes of a row, so [n][v] is
+// over the tile's rows.  q enters the products without g (|q| <= 1): dx's rows take their g afterwards, and so does dw:
+// fp32 arrays with x's rows, bf16 ones as g / max |g| here and max |g| afterwards.  So the target's entry, -1 and a
+// probability, is hardly touched by q's rounding to bf16: with g in q all rows of a mean shared the rounding
+// error of -1 / N, which was off by 0.38 % in both gradients (4096 rows of text; now 0.17 %, what the
+// gradients' own rounding costs).  A lane holds four classes of a row, so [n][v] is
 // stored from the registers (32-byte runs); [v][n] goes through LDS, a wave's classes by 64 rows (fp32: 32 rows,
 // hi and lo parts) at a time, so that its stores are runs of 128 bytes.
 template <bool SP>
 struct GradEnd {
   Logits l;
   const float *lse, *g;
+  const float* gmax;  // bf16: parts of max |g| (largest_g); null without qt
+  int gparts;
   u16 *q, *qt;     // or null
   int ldq, ldqt;
   float* db;       // [tiles of rows][V], or null
   template <class T>
   __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
     l.take<T>(acc, pl);
+    const float most = !SP && qt ? join_largest(gmax, gparts) : 1.f;
     constexpr int RA = 16 * T::NA, RB = 16 * T::NB;  // the wave's classes and rows
     static_assert(RB == 64, "a row of the transposed tile is 128 bytes");
     char* const tr = lds + (pl.wa * T::WB + pl.wb) * RA * 128;
@@ -398,6 +424,7 @@ struct GradEnd {
       const bool ok = yn >= 0 && yn < l.V_all;
       const int t = ok ? yn - l.v0 : -1;
       const float ln = take_off_far<T>(acc, j, ok ? lse[n] : 0.f), gn = ok ? g[n] : 0.f;
+      const float gh = most != 0.f ? gn / most : 0.f;  // (1 where all rows weigh alike)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
@@ -425,13 +452,14 @@ struct GradEnd {
             put_pair(i, 32 + 16 * (j & 1) + (pl.n & ~1), lo);
           }
         } else {
-          u16 h[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = bf16_bits(acc[i][j][e]);
           if (q && n < l.N && v < ldq)
-            *reinterpret_cast<u32x2*>(q + (size_t)n * ldq + v) =
-                u32x2{(unsigned)h[0] | (unsigned)h[1] << 16, (unsigned)h[2] | (unsigned)h[3] << 16};
-          if (qt) put_pair(i, 16 * j + (pl.n & ~1), h);
+            *reinterpret_cast<u32x2*>(q + (size_t)n * ldq + v) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+          if (qt) {
+            u16 h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = bf16_bits(p[e] * gh);
+            put_pair(i, 16 * j + (pl.n & ~1), h);
+          }
         }
       }
       if (SP && qt && j & 1) store_rows((pl.b0 + 16 * (j - 1)) * 2);
@@ -467,7 +495,9 @@ struct OutEnd {
   int A, B;           // D, rows
   const int* ea;      // fp32: scales of operand A's rows; the product is acc 2^-(ea[a] + kQScale)
   const int32_t* y;   // dx: rows whose y is outside 0 .. V-1 are 0; or null
-  const float* g;     // fp32 dx: the row's factor; or null
+  const float* g;     // dx: the row's factor; or null
+  const float* gmax;  // bf16 dw: parts of the factor of all (largest_g); or null
+  int gparts;
   int V;
   float* sum;         // [splits][B][A], set (add = 0) or added to; or null
   int add;
@@ -484,11 +514,12 @@ struct OutEnd {
           for (int j = 0; j < T::NB; ++j) acc[i][j][e] = ldexpf(acc[i][j][e], s);
         }
     }
+    const float all = gmax ? join_largest(gmax, gparts) : 1.f;
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
       const int b = pl.b0 + 16 * j + pl.n;
       const bool in = b < B;
-      float f = 1.f;
+      float f = all;
       bool ok = true;
       if (y) {
         const int yb = in ? y[b] : -1;
@@ -760,9 +791,9 @@ __global__ __launch_bounds__(256) void join_loss_few(const float2* part, int til
 }
 
 // out[i] = sum over the parts: 64 places of four values by 4 runs of parts per block, then the runs in order.
-// With y the values are rows of D, and those without a target are 0 whatever the parts hold.
+// With y the values are rows of D that take the factors g, and those without a target are 0 whatever the parts hold.
 template <class E>
-__global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out, const int32_t* y, int V, unsigned D) {
+__global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out, const int32_t* y, int V, unsigned D, const float* g) {
   __shared__ f32x4 s[3][64];
   const int c = threadIdx.x & 63, w = threadIdx.x >> 6, each = (parts + 3) / 4;
   const size_t i = ((size_t)blockIdx.x * 64 + c) * 4;
@@ -785,8 +816,9 @@ __global__ __launch_bounds__(256) void join_parts(const float* part, int parts, 
   if (y) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int t = i + e < n ? y[(unsigned)(i + e) / D] : -1;
-      if (t < 0 || t >= V) v[e] = 0.f;
+      const unsigned r = (unsigned)(i + e) / D;
+      const int t = i + e < n ? y[r] : -1;
+      v[e] = t < 0 || t >= V ? 0.f : v[e] * g[r];
     }
   }
   if (i + 3 < n) {
@@ -884,7 +916,7 @@ struct Forward {
 struct Backward {
   int piece;
   Shape logits, dxs, dws;  // of a whole piece
-  size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, db, cmax, dx, dw, total;
+  size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, db, cmax, gmax, dx, dw, total;
   WnFewPlan few;
   void plan(bool sp, int N, int D, int p) {
     piece = p;
@@ -935,6 +967,7 @@ struct Backward {
     qt = c.take((size_t)piece * un * 2);
     db = c.take(ceil_div(N, 128) * piece * 4);
     cmax = c.take((size_t)kColumnParts * D * 4);
+    gmax = c.take(kGParts * 4);
     dx = c.take(piece == V && dxs.splits == 1 ? 0 : (size_t)dxs.splits * N * D * 4);
     dw = c.take(dws.splits == 1 ? 0 : (size_t)dws.splits * piece * D * 4);
     total = c.at;
@@ -1026,8 +1059,9 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
 }
 
 template <class E>
-hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st, const int32_t* y = nullptr, int V = 0, int D = 1) {
-  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out, y, V, (unsigned)D);
+hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st, const int32_t* y = nullptr, int V = 0, int D = 1,
+                const float* g = nullptr) {
+  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out, y, V, (unsigned)D, g);
   return hipGetLastError();
 }
 
@@ -1041,12 +1075,17 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   if (N <= kFewRows) {
     hipError_t e = wn_few_grads<E>({N, D, V, x, w, b, y}, f.few, lse, g, dx != nullptr, dw, db, ws + f.q, ws + f.qt, floats(f.dx), st);
-    if (e == hipSuccess && dx) e = join(floats(f.dx), f.few.parts, (size_t)N * D, dx, st, y, V, D);
+    if (e == hipSuccess && dx) e = join(floats(f.dx), f.few.parts, (size_t)N * D, dx, st, y, V, D, g);
     return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
   }
   const Operand ox = rows_operand(x, N, D, units(f.x), ints(f.ex), st);
   Operand oxt{};
-  // (bf16: q holds g; fp32: x transposed does, so that q stays within its scale)
+  const float* gmax = nullptr;
+  const int gparts = (int)std::min<size_t>(kGParts, ceil_div(N, 1024));
+  if (dw && !sp) {
+    hipLaunchKernelGGL(largest_g, dim3(gparts), dim3(256), 0, st, g, y, N, V, floats(f.gmax));
+    gmax = floats(f.gmax);
+  }
   if (dw) oxt = cols_operand(x, N, D, RowFactor{y, sp ? g : nullptr, V}, units(f.xt), floats(f.cmax), ints(f.ext), st);
   hipError_t e = hipGetLastError();
   for (int v0 = 0; v0 < V && e == hipSuccess; v0 += f.piece) {
@@ -1056,19 +1095,19 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
     const Operand ow = rows_operand(wv, n, D, units(f.w), ints(f.ew), st);
     const bool big = f.logits.big;
     GradEnd<sp> end{{sp ? ints(f.ex) : nullptr, sp ? ints(f.ew) : nullptr, b ? b + v0 : nullptr, y, N, n, v0, V},
-                    lse, g, dx ? units(f.q) : nullptr, dw ? units(f.qt) : nullptr, ldq, ldqt, db ? floats(f.db) : nullptr};
+                    lse, g, gmax, gparts, dx ? units(f.q) : nullptr, dw ? units(f.qt) : nullptr, ldq, ldqt, db ? floats(f.db) : nullptr};
     e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
     if (e == hipSuccess && db) e = join(floats(f.db), (int)ceil_div(N, big ? 256 : 128), n, db + v0, st);
     if (e == hipSuccess && dx) {
       const Operand owt = cols_operand(wv, n, D, RowFactor{nullptr, nullptr, 0}, units(f.wt), floats(f.cmax), ints(f.ewt), st);
       const bool whole = f.piece == V && f.dxs.splits == 1;
-      const OutEnd<E> o{D, N, ints(f.ewt), y, sp ? g : nullptr, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
+      const OutEnd<E> o{D, N, ints(f.ewt), y, g, nullptr, 0, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
       e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.dxs.splits, 0}, f.dxs.big, o, st);
       if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.dxs.splits, (size_t)N * D, dx, st);
     }
     if (e == hipSuccess && dw) {
       E* const out = dw + (size_t)v0 * D;
-      const OutEnd<E> o{D, n, ints(f.ext), nullptr, nullptr, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
+      const OutEnd<E> o{D, n, ints(f.ext), nullptr, nullptr, gmax, gparts, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
       e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.dws.splits, 0}, f.dws.big, o, st);
       if (e == hipSuccess && f.dws.splits > 1) e = join(floats(f.dw), f.dws.splits, (size_t)n * D, out, st);
     }
