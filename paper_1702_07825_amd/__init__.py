@@ -524,26 +524,31 @@ def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None,
     outs = grads if outs is None else list(outs)
     if len(outs) != len(grads):
         raise ValueError("%d outs for %d grads" % (len(outs), len(grads)))
-    # (whole lists at a time: a model has hundreds of gradients)
+    # (whole lists at a time, and the cheapest question of each kind: a model has hundreds of gradients)
     both = grads if outs is grads else grads + outs
-    for t in both:
-        if not isinstance(t, torch.Tensor):
-            raise TypeError("gradients must be torch tensors")
-    if not {t.dtype for t in both} <= {torch.float32, torch.bfloat16}:
+    try:
+        dtypes = [t.dtype for t in both]
+        devices = {t.get_device() for t in both}
+        sizes = [t.numel() for t in both]
+        dense = all([t.is_contiguous() for t in both])
+    except AttributeError:
+        raise TypeError("gradients must be torch tensors") from None
+    if not set(dtypes) <= {torch.float32, torch.bfloat16}:
         raise ValueError("gradients must be float32 or bfloat16")
     on = _On(grads[0], stream)
-    if {t.device for t in both} != {on.device}:
+    if devices != {on.device.index}:
         raise ValueError("gradients must all be on %s" % on.device)
-    if not all([t.is_contiguous() for t in both]):
+    if not dense:
         raise ValueError("gradients must be contiguous")
-    if outs is not grads and [(t.shape, t.dtype) for t in grads] != [(t.shape, t.dtype) for t in outs]:
-        raise ValueError("outs must have the shapes and dtypes of grads")
-    arrays = np.zeros(len(grads), dtype=_CLIP_ARRAY)
+    n = len(grads)
+    if outs is not grads and (sizes[:n] != sizes[n:] or dtypes[:n] != dtypes[n:]):
+        raise ValueError("outs must have the sizes and dtypes of grads")
+    arrays = np.zeros(n, dtype=_CLIP_ARRAY)
     arrays["g"] = [t.data_ptr() for t in grads]
     arrays["out"] = arrays["g"] if outs is grads else [t.data_ptr() for t in outs]
-    arrays["n"] = [t.numel() for t in grads]
-    arrays["dtype"] = [WN_F32 if t.dtype == torch.float32 else WN_BF16 for t in grads]
+    arrays["n"] = sizes[:n]
+    arrays["dtype"] = [WN_F32 if t is torch.float32 else WN_BF16 for t in dtypes[:n]]
     norm, np_ = on.out(norm, (), torch.float32, "norm")
     ws, wsp, wsn = on.workspace(workspace, lib.wn_clip_workspace_bytes())
-    _check(lib.wn_clip(len(grads), arrays.ctypes.data_as(ctypes.POINTER(ClipArray)), float(max_norm), np_, wsp, wsn, on.handle), "wn_clip")
+    _check(lib.wn_clip(n, arrays.ctypes.data_as(ctypes.POINTER(ClipArray)), float(max_norm), np_, wsp, wsn, on.handle), "wn_clip")
     return norm

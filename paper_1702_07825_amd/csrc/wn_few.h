@@ -5,8 +5,17 @@
 // Calls of up to this many rows read w from memory straight into registers, once each pass, instead of through tiles
 // in LDS.
 constexpr int kFewRows = 64;
+// Whether a block's four waves share its classes: where a run of classes each would leave too few blocks, and the rows
+// are long enough to cut in four.  A forward pass with classes of its own for each wave and with shared ones: 64 rows x
+// 8000 x 4096, fp32 162 and 65 us, bf16 44 and 30; x 32000 x 1024 49 and 74, 26 and 34; 16 rows x 8000 x 4096, fp32 63
+// and 37, x 32000 x 1024 38 and 39.
+inline bool wn_few_shared(bool f32, int N, int D, int V) {
+  return V <= (N <= 16 ? 1 << 15 : 1 << 14) && D * (f32 ? 4 : 2) >= 2048;
+}
 // Classes of a block: a place in `part`.
-inline int wn_few_classes(int N) { return N <= 16 ? 64 : 128; }
+inline int wn_few_classes(bool f32, int N, int D, int V) {
+  return (N <= 16 ? 16 : 32) * (wn_few_shared(f32, N, D, V) ? 1 : 4);
+}
 
 struct WnFew {
   int N, D, V;
@@ -15,7 +24,7 @@ struct WnFew {
   const int32_t* y;
 };
 
-// Forward: (largest logit, sum of exponentials) of each row in each run of wn_few_classes(N) classes, part[run][N], and the
+// Forward: (largest logit, sum of exponentials) of each row in each run of wn_few_classes() classes, part[run][N], and the
 // targets' logits.
 template <class E>
 hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st);

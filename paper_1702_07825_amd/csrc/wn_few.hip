@@ -87,13 +87,17 @@ template <int NB>
 constexpr int kTilesOf = NB == 1 ? 1 : 2;  // T (wn_few_classes: 64 T a block)
 constexpr int kRowBytes = 256, kPitch = kRowBytes + 16;  // of a chunk of x in LDS: 16 rows' pieces on different banks
 
-template <class E, int NB, class End>
+//
+// Few classes of long rows (wn_few_shared) leave most CUs idle so: there the block's four waves share their classes,
+// a quarter of each row each, and the first adds the others' sums (16 rows x 3906 classes x 3398, fp32: 46 us a pass
+// without, 19 so; 37 rows x 50021 x 777 stay at 38, and would take 61).
+template <class E, int NB, bool kShared, class End>
 __global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End end) {
   constexpr int W = Piece<E>::n, K = 4 * W, T = kTilesOf<NB>, U = NB == 1 ? 8 : kRowBytes / 64;
-  constexpr bool kStaged = NB > 1;
-  __shared__ __align__(16) char xs[kStaged ? 2 * 16 * NB * kPitch : 16];
+  constexpr bool kStaged = NB > 1 && !kShared;
+  __shared__ __align__(16) char xs[kStaged ? 2 * 16 * NB * kPitch : kShared ? 3 * T * NB * 64 * 16 : 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
-  const int v0 = (blockIdx.x * 4 + wave) * 16 * T;
+  int v0 = (kShared ? blockIdx.x : blockIdx.x * 4 + wave) * 16 * T;
   // rows behind the last one repeat it: what they give is not used
   const E* w[T];
 #pragma unroll
@@ -114,7 +118,8 @@ __global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End en
         to[t][u] = c < whole ? whole_piece(w[t] + k) : piece_at(w[t] + k, f.D - k - quad * W);
       }
   };
-  fetch(a, 0);
+  const int c0 = kShared ? chunks * wave / 4 : 0, c1 = kShared ? chunks * (wave + 1) / 4 : chunks;
+  if (!kShared || c0 < c1) fetch(a, c0);
   if constexpr (kStaged) {
     constexpr int kPieces = 16 * NB * (kRowBytes / 16) / 256;  // of a chunk of x per thread
     P<E> xv[kPieces];
@@ -160,24 +165,47 @@ __global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End en
       }
     }
   } else {
-    const E* const x = static_cast<const E*>(f.x) + (size_t)min(n, f.N - 1) * f.D + quad * W;
-    for (int c = 0; c < chunks; ++c) {
-      P<E> b[U];
+    const E* x[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) x[j] = static_cast<const E*>(f.x) + (size_t)min(16 * j + n, f.N - 1) * f.D + quad * W;
+    for (int c = c0; c < c1; ++c) {
+      P<E> b[U][NB];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int k = (c * U + u) * K;
-        b[u] = c < whole ? whole_piece(x + k) : piece_at(x + k, f.D - k - quad * W);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) b[u][j] = c < whole ? whole_piece(x[j] + k) : piece_at(x[j] + k, f.D - k - quad * W);
       }
-      if (c + 1 < chunks) fetch(next, c + 1);
+      if (c + 1 < c1) fetch(next, c + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int t = 0; t < T; ++t) acc[t][0] = mma(a[t][u], b[u], acc[t][0]);
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[t][j] = mma(a[t][u], b[u][j], acc[t][j]);
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int u = 0; u < U; ++u) a[t][u] = next[t][u];
+    }
+  }
+  if constexpr (kShared) {
+    f32x4* const s = reinterpret_cast<f32x4*>(xs);
+    if (wave)
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) s[((wave - 1) * T * NB + t * NB + j) * 64 + lane] = acc[t][j];
+    __syncthreads();
+    if (wave == 0) {
+      for (int w4 = 0; w4 < 3; ++w4)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[t][j] += s[(w4 * T * NB + t * NB + j) * 64 + lane];
+    } else {
+      v0 = 1 << 29;  // no classes: the first wave has them
     }
   }
 #pragma unroll
@@ -502,13 +530,20 @@ void by_tiles(int N, F f) {
   else f(std::integral_constant<int, 4>{});
 }
 
+template <class E, int NB, class End>
+void launch_logits(const WnFew& f, int classes, const End& end, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(classes, wn_few_classes(sizeof(E) == 4, f.N, f.D, f.V)));
+  if (wn_few_shared(sizeof(E) == 4, f.N, f.D, f.V)) hipLaunchKernelGGL((few_logits<E, NB, true, End>), grid, dim3(256), 0, st, f, end);
+  else hipLaunchKernelGGL((few_logits<E, NB, false, End>), grid, dim3(256), 0, st, f, end);
+}
+
 }  // namespace
 
 template <class E>
 hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st) {
   by_tiles(f.N, [&](auto nb) {
     const FewStats end{part, target};
-    hipLaunchKernelGGL((few_logits<E, decltype(nb)::value, FewStats>), dim3((unsigned)ceil_div(f.V, wn_few_classes(f.N))), dim3(256), 0, st, f, end);
+    launch_logits<E, decltype(nb)::value>(f, f.V, end, st);
   });
   return hipGetLastError();
 }
@@ -516,7 +551,7 @@ hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t 
 WnFewPlan wn_few_plan(bool f32, int N, int D, int V) {
   WnFewPlan p;
   const int step = f32 ? 16 : 32, e = f32 ? 4 : 2, slab = f32 ? 64 : 128;
-  // q's rows hold zeros from V to the last block's end, past which no step reads; each block of dx takes 4 quarters of whole steps, some 512 blocks
+  // q's rows hold zeros from V to vpad, past which no step reads; each block of dx takes 4 quarters of whole steps, some 512 blocks
   p.vpad = (int)ceil_div(V, 64) * 64;
   p.npad = N <= 32 ? 32 : 64;
   p.slabs = (int)ceil_div(D, slab);
@@ -535,7 +570,7 @@ hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, co
   by_tiles(f.N, [&](auto nb) {
     constexpr int NB = decltype(nb)::value, W = Piece<E>::n;
     const FewGrad<E> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad, p.npad, db};
-    hipLaunchKernelGGL((few_logits<E, NB, FewGrad<E>>), dim3((unsigned)ceil_div(f.V, wn_few_classes(f.N))), dim3(256), 0, st, f, end);
+    launch_logits<E, NB>(f, p.vpad, end, st);  // (q holds zeros behind V)
     if (dx)
       hipLaunchKernelGGL((few_dx<E, NB>), dim3(p.slabs, p.parts), dim3(256), W * NB * 64 * 16, st, f, static_cast<const E*>(q), p.vpad,
                          p.each, sum);

@@ -897,7 +897,7 @@ struct Forward {
     const size_t units = padded_units(D, sp);
     Carve c;
     if (N <= kFewRows) {
-      part = c.take(ceil_div(V, wn_few_classes(N)) * N * sizeof(float2));
+      part = c.take(ceil_div(V, wn_few_classes(sp, N, D, V)) * N * sizeof(float2));
       target = c.take((size_t)N * 4);
       total = c.at;
       return;
@@ -1030,7 +1030,7 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
     float* const target = reinterpret_cast<float*>(ws + f.target);
     hipError_t e = wn_few_loss<E>({N, D, V, x, w, b, y}, part, target, st);
     if (e == hipSuccess) {
-      hipLaunchKernelGGL(join_loss_few, dim3(N), dim3(256), 0, st, part, (int)ceil_div(V, wn_few_classes(N)), target, y, N, V, loss, lse);
+      hipLaunchKernelGGL(join_loss_few, dim3(N), dim3(256), 0, st, part, (int)ceil_div(V, wn_few_classes(sp, N, D, V)), target, y, N, V, loss, lse);
       e = hipGetLastError();
     }
     return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
