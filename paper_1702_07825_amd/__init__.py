@@ -433,10 +433,18 @@ class _On:
         return t, t.data_ptr(), t.numel() * t.element_size()
 
 
+def _i32(n, name):
+    """A size as the C ABI takes it (ctypes would wrap a larger one)."""
+    n = int(n)
+    if not -(1 << 31) <= n < 1 << 31:
+        raise ValueError("%s is out of range: %d" % (name, n))
+    return n
+
+
 def _matrix(t, name):
     if t.dim() != 2:
         raise ValueError("%s must have two dimensions, got %s" % (name, tuple(t.shape)))
-    return int(t.shape[0]), int(t.shape[1])
+    return _i32(t.shape[0], name), _i32(t.shape[1], name)
 
 
 def head_loss(x, w, y, b=None, loss=None, lse=None, workspace=None, stream=None):
@@ -485,7 +493,7 @@ def embed(table, tokens, scale: float = 1.0, out=None, stream=None):
     V, D = _matrix(table, "table")
     on = _On(table, stream)
     shape = tuple(tokens.shape)
-    N = int(tokens.numel())
+    N = _i32(tokens.numel(), "tokens")
     tp, kp = on.ptr(table, table.dtype, (V, D), "table"), on.ptr(tokens, torch.int32, shape, "tokens")
     out, op = on.out(out, shape + (D,), table.dtype, "out")
     _check(lib.wn_embed(dt, N, D, V, tp, kp, float(scale), op, on.handle), "wn_embed")
@@ -498,8 +506,8 @@ def embed_backward(dout, tokens, V: int, scale: float = 1.0, dtable=None, worksp
     dt, lib = _train_dtype(dout, "dout"), load_library()
     if dout.dim() < 1:
         raise ValueError("dout must have a dimension of the table's columns")
-    shape, D, V = tuple(tokens.shape), int(dout.shape[-1]), int(V)
-    N = int(tokens.numel())
+    shape, D, V = tuple(tokens.shape), _i32(dout.shape[-1], "dout"), _i32(V, "V")
+    N = _i32(tokens.numel(), "tokens")
     on = _On(dout, stream)
     dp, kp = on.ptr(dout, dout.dtype, shape + (D,), "dout"), on.ptr(tokens, torch.int32, shape, "tokens")
     dtable, tp = on.out(dtable, (V, D), dout.dtype, "dtable")

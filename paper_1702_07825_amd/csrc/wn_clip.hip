@@ -6,6 +6,9 @@
 // into chunks of equal length that the blocks take in turn, so that one launch serves arrays of any
 // sizes.  Squares are summed in fp64: a chunk's sum of fp32 squares would overflow from gradients of 1e19 on
 // and vanish below 1e-23.
+//
+// Bound: two reads and a write of the arrays (a second read of what does not stay in the caches).  Measured: 0.91 GB in
+// 295 arrays, squares 167 us (5.4 TB/s), scaling 349 us (5.2 TB/s); 3.6 MB in 127 arrays 6.5 us each.
 #include "wn_arrays.h"
 
 #include "wn_wave.h"

@@ -6,6 +6,10 @@
 // the tokens are sorted first, stably, and the sorted rows cut into chunks of equal length: a
 // chunk sums each run of equal tokens in it; runs that lie within a chunk are done, the others leave a
 // partial sum per chunk, which the last kernel joins in order.
+//
+// Bound: reading dout and writing the table.  Measured: 512000 rows of 64 fp32 into 256 (131 MB, runs of up to 100,000
+// rows): sort 28 us, sums 26, join 21; 8191 bf16 rows of 2048 into 65536 (302 MB): the sort beside the table's zeros 44 us
+// (6.1 TB/s), sums 23, join 8.  The lookups 25 us (5.2 TB/s) and 16 us.
 #include "wn_arrays.h"
 
 #include "wn_wave.h"

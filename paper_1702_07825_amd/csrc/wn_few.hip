@@ -379,6 +379,8 @@ struct Columns {
   }
 };
 
+// Bound: reading w (dx) and writing as much (dw).  Measured, 37 rows x 50021 classes x 777 (odd rows of 78 MB), bf16: dx
+// 43 us, dw 36, the logits 38; 1 row x 32000 x 2048 (131 MB): logits 24 us, 5.4 TB/s.
 // dx's parts: a block takes a slab of columns and a run of classes, its waves a quarter of the run each, and adds the
 // quarters up.
 template <class E, int NB>
@@ -451,7 +453,7 @@ template <class E, int NB>
 __global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int npad, const float* g, E* dw) {
   constexpr int W = Piece<E>::n, S = kStep<E>, K = (16 * NB + S - 1) / S, kTiles = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quad = lane >> 4;
-  const int c0 = blockIdx.x * kSlab<E>, c = min(c0 + W * n, f.D - 1);
+  const int c0 = blockIdx.y * kSlab<E>, c = min(c0 + W * n, f.D - 1);
   float most = 0.f;  // max |g|, which q was divided by
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
@@ -475,7 +477,7 @@ __global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int
     for (int u = 0; u < W; ++u) a[k][u] = t.fragment(u);
   }
   for (int t = 0; t < kTiles; ++t) {
-    const int v0 = ((blockIdx.y * 4 + wave) * kTiles + t) * 16;
+    const int v0 = ((blockIdx.x * 4 + wave) * kTiles + t) * 16;
     if (v0 >= f.V) return;
     const int v = v0 + n;
     f32x4 acc[W];
@@ -575,7 +577,7 @@ hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, co
       hipLaunchKernelGGL((few_dx<E, NB>), dim3(p.slabs, p.parts), dim3(256), W * NB * 64 * 16, st, f, static_cast<const E*>(q), p.vpad,
                          p.each, sum);
     if (dw)
-      hipLaunchKernelGGL((few_dw<E, NB>), dim3(p.slabs, (unsigned)ceil_div(f.V, 256)), dim3(256), 0, st, f, static_cast<const E*>(qt),
+      hipLaunchKernelGGL((few_dw<E, NB>), dim3((unsigned)ceil_div(f.V, 256), p.slabs), dim3(256), 0, st, f, static_cast<const E*>(qt),
                          p.npad, g, static_cast<E*>(dw));
   });
   return hipGetLastError();

@@ -154,7 +154,7 @@ def test_no_rows_and_refusals():
     assert wn.embed(table, none).shape == (0, 4)
     assert not bool(wn.embed_backward(torch.empty((0, 4), device="cuda"), none, 5).any())
     for f in (lambda: wn.embed(table.half(), t), lambda: wn.embed(table, t.long()), lambda: wn.embed(table.t(), t),
-              lambda: wn.embed(table, t.cpu()), lambda: wn.embed(table[0], t),
+              lambda: wn.embed_backward(torch.ones((3, 4), device="cuda"), t, (1 << 32) + 5), lambda: wn.embed(table, t.cpu()), lambda: wn.embed(table[0], t),
               lambda: wn.embed_backward(torch.ones((2, 4), device="cuda"), t, 5),
               lambda: wn.embed_backward(torch.ones((3, 4), device="cuda"), t, 5, dtable=torch.ones((4, 4), device="cuda"))):
         with pytest.raises((ValueError, TypeError)):

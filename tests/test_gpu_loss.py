@@ -294,6 +294,36 @@ def test_runs_on_another_stream_and_in_a_graph(dtype):
         assert all(torch.equal(a, c) for a, c in zip(outs, want[k])), k
 
 
+@pytest.mark.parametrize("N", [40, 200])
+def test_targets_at_the_ends_of_int32(N):
+    """Any value outside the classes is padding, the types' ends among them."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(N, 24, 90, torch.float32, seed=19, ignored=0)
+    y[0], y[1], y[2], y[3] = -2 ** 31, 2 ** 31 - 1, 90, -1
+    _check(x, w, b, y, grad)
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own: the results of one after the other."""
+    import paper_1702_07825_amd as wn
+    sets = [[t.cuda() for t in _inputs(700, 96, 3000, torch.bfloat16, seed=30 + k)] for k in range(2)]
+
+    def both(s, stream=None):
+        x, w, b, y, g = s
+        loss, lse = wn.head_loss(x, w, y, b=b, stream=stream)
+        return [loss, lse, *wn.head_loss_backward(x, w, y, lse, g, b=b, stream=stream)]
+
+    want = [both(s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[both(s, st) for s, st in zip(sets, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for r in got:
+        for a, c in zip(r, want):
+            assert all(torch.equal(p, q) for p, q in zip(a, c))
+
+
 def test_gradient_against_differences():
     """sum g loss along a direction in x, w and b, from the losses themselves.  The function's third derivative
     along it is at most 8 max|dl|^3 sum|g| with |dl| the logits' change per unit, so the central difference is off by
