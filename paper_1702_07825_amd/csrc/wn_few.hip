@@ -80,7 +80,7 @@ __device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
 
 // ------------------------------------------------------------------------------------------------
 // Logits: a wave takes T tiles of 16 classes.  The next U pieces of w are in flight during the current ones'
-// products.  Up to 16 rows of x come from the caches as operands; more go through LDS, once for the block's four
+// products.  One tile of x's rows comes from the caches as an operand; more go through LDS, once for the block's four
 // waves (straight from the caches, 37 rows x 50021 classes x 777, the reads of x took the pass from 40 to 92 us).
 // ------------------------------------------------------------------------------------------------
 template <int NB>
@@ -90,7 +90,7 @@ constexpr int kRowBytes = 256, kPitch = kRowBytes + 16;  // of a chunk of x in L
 //
 // Few classes of long rows (wn_few_shared) leave most CUs idle so: there the block's four waves share their classes,
 // a quarter of each row each, and the first adds the others' sums (16 rows x 3906 classes x 3398, fp32: 46 us a pass
-// without, 19 so; 37 rows x 50021 x 777 stay at 38, and would take 61).
+// without, 19 so).
 template <class E, int NB, bool kShared, class End>
 __global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End end) {
   constexpr int W = Piece<E>::n, K = 4 * W, T = kTilesOf<NB>, U = NB == 1 ? 8 : kRowBytes / 64;
@@ -526,16 +526,16 @@ __global__ __launch_bounds__(256, 2) void few_dw(const WnFew f, const E* qt, int
 }
 
 template <class F>
-void by_tiles(int N, F f) {
-  if (N <= 16) f(std::integral_constant<int, 1>{});
-  else if (N <= 32) f(std::integral_constant<int, 2>{});
+void by_tiles(int tiles, F f) {
+  if (tiles == 1) f(std::integral_constant<int, 1>{});
+  else if (tiles == 2) f(std::integral_constant<int, 2>{});
   else f(std::integral_constant<int, 4>{});
 }
 
 template <class E, int NB, class End>
 void launch_logits(const WnFew& f, int classes, const End& end, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(classes, wn_few_classes(sizeof(E) == 4, f.N, f.D, f.V)));
-  if (wn_few_shared(sizeof(E) == 4, f.N, f.D, f.V)) hipLaunchKernelGGL((few_logits<E, NB, true, End>), grid, dim3(256), 0, st, f, end);
+  if (wn_few_shared(sizeof(E) == 4, f.D, f.V)) hipLaunchKernelGGL((few_logits<E, NB, true, End>), grid, dim3(256), 0, st, f, end);
   else hipLaunchKernelGGL((few_logits<E, NB, false, End>), grid, dim3(256), 0, st, f, end);
 }
 
@@ -543,7 +543,7 @@ void launch_logits(const WnFew& f, int classes, const End& end, hipStream_t st) 
 
 template <class E>
 hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t st) {
-  by_tiles(f.N, [&](auto nb) {
+  by_tiles(wn_few_tiles(sizeof(E) == 4, f.N, f.D, f.V), [&](auto nb) {
     const FewStats end{part, target};
     launch_logits<E, decltype(nb)::value>(f, f.V, end, st);
   });
@@ -569,10 +569,11 @@ WnFewPlan wn_few_plan(bool f32, int N, int D, int V) {
 template <class E>
 hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, const float* g, bool dx, void* dw, float* db, void* q,
                         void* qt, float* sum, hipStream_t st) {
-  by_tiles(f.N, [&](auto nb) {
+  const FewGrad<E> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad, p.npad, db};
+  by_tiles(wn_few_tiles(sizeof(E) == 4, f.N, f.D, f.V),
+           [&](auto nb) { launch_logits<E, decltype(nb)::value>(f, p.vpad, end, st); });  // (q holds zeros behind V)
+  by_tiles(f.N <= 16 ? 1 : f.N <= 32 ? 2 : 4, [&](auto nb) {
     constexpr int NB = decltype(nb)::value, W = Piece<E>::n;
-    const FewGrad<E> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad, p.npad, db};
-    launch_logits<E, NB>(f, p.vpad, end, st);  // (q holds zeros behind V)
     if (dx)
       hipLaunchKernelGGL((few_dx<E, NB>), dim3(p.slabs, p.parts), dim3(256), W * NB * 64 * 16, st, f, static_cast<const E*>(q), p.vpad,
                          p.each, sum);

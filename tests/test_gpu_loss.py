@@ -105,7 +105,7 @@ def _check(x, w, b, y, grad, need=("dx", "dw", "db"), device="cuda"):
 
 
 SIZES = [(1, 1, 1), (1, 64, 256), (1, 1000, 777), (2, 7, 5), (15, 64, 100), (16, 64, 256), (17, 65, 129), (33, 8, 2000),
-         (64, 32, 1000), (64, 1025, 65), (31, 300, 4000), (5, 1100, 300), (16, 2500, 70), (30, 1030, 100), (64, 1999, 33), (1, 5000, 1), (48, 513, 2049), (65, 64, 70), (100, 100, 127), (127, 72, 128), (128, 128, 128), (129, 256, 257), (200, 100, 3001), (256, 256, 256),
+         (64, 32, 1000), (64, 1025, 65), (31, 300, 4000), (5, 1100, 300), (4, 100, 17000), (5, 100, 17000), (16, 520, 16400), (16, 2500, 70), (30, 1030, 100), (64, 1999, 33), (1, 5000, 1), (48, 513, 2049), (65, 64, 70), (100, 100, 127), (127, 72, 128), (128, 128, 128), (129, 256, 257), (200, 100, 3001), (256, 256, 256),
          (300, 513, 777), (1000, 64, 300), (2111, 40, 64)]
 
 
