@@ -48,8 +48,9 @@ extern "C" {
  * A class of bias -inf is masked: it has probability 0 (a row whose target is masked has loss +inf;
  * if every class is masked, or a logit is NaN or +inf, the loss is NaN or infinite).  An infinity in
  * x or w itself may leave a row that meets it NaN.
- * fp32 products are taken as three products of fp16 parts that hold each value to 2^-22 of itself
- * (and to 2^-39 of the largest value of its row).
+ * From 65 rows on fp32 products are taken as three products of fp16 parts that hold each value to 2^-22 of
+ * itself (or to 2^-39 of the largest value of its row); fewer rows take them in fp32.  lse of a row
+ * without a target is that of what x holds.
  * N 0 .. 2^20 (0: nothing to do), D 1 .. 2^16, V 1 .. 2^24.
  * Errors: WN_EINVAL (a size out of range, a null pointer, memory that is not on a device or on
  * different ones, a short or misaligned workspace); WN_EUNSUPPORTED (dtype WN_I8); WN_EHIP.
@@ -69,7 +70,7 @@ size_t wn_loss_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V);
  *   dx    [N][D] out, or NULL if not wanted; 0 in rows without a target, whatever x, lse and g hold there
  *   dw    [V][D] out, or NULL;   db fp32 [V] out, or NULL (with b NULL it is the gradient at b = 0)
  * With dtype WN_BF16 q / g (dx) and q / max |g| (dw) enter the last two products rounded to bf16 (db sums q in
- * fp32); with WN_F32 as fp16 parts, as in wn_loss.  Sizes and errors as wn_loss; all three outputs NULL is
+ * fp32); with WN_F32 as wn_loss takes its products.  Sizes and errors as wn_loss; all three outputs NULL is
  * an error.  N = 0: dw and db are zeroed.
  */
 int wn_loss_backward(int32_t dtype, int32_t N, int32_t D, int32_t V, const void* x, const void* w, const float* b,

@@ -147,6 +147,22 @@ def test_gradient_against_differences():
     assert float((diff * g).double().sum()) == float((d * wn.embed_backward(g, t, 30, 2.0)).double().sum())
 
 
+def test_offsets_beyond_32_bits():
+    """A table of 4.6 GB: rows on both sides of 2^32 bytes."""
+    import paper_1702_07825_amd as wn
+    V, D = (1 << 20) + 70000, 2048
+    table = torch.zeros((V, D), dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 5, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, V - 1], device="cuda")
+    table[rows] = torch.randn((6, D), device="cuda").bfloat16()
+    t = rows.to(torch.int32).repeat(3)
+    assert torch.equal(wn.embed(table, t), table[rows].repeat(3, 1))
+    d = torch.randint(-4, 5, (18, D), device="cuda").bfloat16()
+    got = wn.embed_backward(d, t, V)
+    assert torch.equal(got[rows], d.view(3, 6, D).float().sum(dim=0).bfloat16())
+    got[rows] = 0
+    assert not bool(got.any())
+
+
 def test_no_rows_and_refusals():
     import paper_1702_07825_amd as wn
     none = torch.empty((0,), dtype=torch.int32, device="cuda")
