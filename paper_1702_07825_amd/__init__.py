@@ -430,6 +430,8 @@ class _On:
         import torch
         if t is None:
             t = self.empty(max(nbytes, 1), torch.uint8)
+        elif t.device != self.device or not t.is_contiguous():
+            raise ValueError("workspaces must be contiguous and on %s" % self.device)
         return t, t.data_ptr(), t.numel() * t.element_size()
 
 

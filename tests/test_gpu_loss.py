@@ -423,3 +423,6 @@ def test_refusals():
             wn.head_loss_backward(x, w, y, a["lse"], a["grad"], b=b, need=a["need"], dx=a["dx"])
     with pytest.raises(wn.WnError):
         wn.head_loss(x, w, y, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    for ws in (torch.empty(1 << 26, dtype=torch.uint8), torch.empty((1 << 26, 2), dtype=torch.uint8, device="cuda")[:, 0]):
+        with pytest.raises(ValueError):
+            wn.head_loss(x, w, y, workspace=ws)
