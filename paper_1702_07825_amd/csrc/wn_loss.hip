@@ -13,6 +13,9 @@
 // row is scaled by a power of two so that its largest value lies in [2^14, 2^15), hi = fp16(v),
 // lo = fp16(v - hi), which holds v to 2^-22 of itself or 2^-39 of the row's largest, and a product takes
 // hi hi + hi lo + lo hi (lo lo is below 2^-22 of it), summed in fp32.
+//
+// Up to kFewRows rows go to wn_few.hip, which is bound by reading w once (64 and 65 rows x 50021 classes x 777: forward 40
+// and 72 us in bf16, 74 and 135 in fp32).
 #include "wn_few.h"
 
 #include "wn_wave.h"
