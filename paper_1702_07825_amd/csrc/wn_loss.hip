@@ -278,20 +278,6 @@ struct Logits {
   }
 };
 
-// exp(l - at) as 2^(l log2 e - at log2 e): the product of `at` is the row's.  Where `at` is so large that it would
-// overflow (every class of the row masked by fp32's lowest value), `at` is taken off the logits first.
-constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float exp_from(float l, float at_log2e) { return __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -at_log2e)); }
-template <class T>
-__device__ __forceinline__ float take_off_far(f32x4 (&acc)[T::NA][T::NB], int j, float at) {
-  const bool far = fabsf(at) > 1e37f && fabsf(at) < INFINITY;
-  if (__any(far)) {
-#pragma unroll
-    for (int i = 0; i < T::NA; ++i) acc[i][j] -= far ? at : 0.f;
-  }
-  return far ? 0.f : at * kLog2e;
-}
-
 __device__ __forceinline__ float across_quads_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
@@ -301,7 +287,10 @@ __device__ __forceinline__ float across_quads_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-// Forward: (largest logit, sum of exp(l - largest)) of each row in the tile's classes, and the target's logit.
+// Forward: (largest logit, sum of exp(l - largest)) of each row in the tile's classes, and the target's logit.  The largest
+// is taken off a logit before the product with log2 e: l - largest is exact near it, so the largest class counts 1 wherever the
+// logits lie and no loss is negative.  (fma(l, log2 e, -largest log2 e) is one operation shorter, but the rounding of
+// its last term moves every exponential of the row: by 1e-6 at logits of 20, a factor of 3e5 at -1e9.)
 struct StatsEnd {
   Logits l;
   float2* part;   // [tiles of all pieces][N]
@@ -321,11 +310,11 @@ struct StatsEnd {
       m = across_quads_max(m);
       Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { target[n] = acc[i][j][e]; });
       // (a row without a class yet: every exponential is 0, not exp(-inf + inf))
-      const float at = take_off_far<T>(acc, j, m == -INFINITY ? 0.f : m);
+      const float at = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += exp_from(acc[i][j][e], at);
+        for (int e = 0; e < 4; ++e) sum += wnk::expf_fast(acc[i][j][e] - at);
       sum = across_quads_sum(sum);
       if (pl.quad == 0) s[pl.wa * T::TB + pl.wb * (T::TB / T::WB) + 16 * j + pl.n] = make_float2(m, sum);
     }
@@ -433,13 +422,13 @@ struct GradEnd {
       const int yn = n < l.N ? l.y[n] : -1;
       const bool ok = yn >= 0 && yn < l.V_all;
       const int t = ok ? yn - l.v0 : -1;
-      const float ln = take_off_far<T>(acc, j, ok ? lse[n] : 0.f), gn = ok ? g[n] : 0.f;
+      const float ln = ok ? lse[n] : 0.f, gn = ok ? g[n] : 0.f;
       const float gh = most != 0.f ? gn / most : 0.f;  // (1 where all rows weigh alike)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = exp_from(acc[i][j][e], ln);
+          const float p = wnk::expf_fast(acc[i][j][e] - ln);
           acc[i][j][e] = ok ? p : 0.f;  // (whatever a row without a target holds)
         }
       Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { acc[i][j][e] -= 1.f; });

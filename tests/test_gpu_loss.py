@@ -426,3 +426,68 @@ def test_refusals():
     for ws in (torch.empty(1 << 26, dtype=torch.uint8), torch.empty((1 << 26, 2), dtype=torch.uint8, device="cuda")[:, 0]):
         with pytest.raises(ValueError):
             wn.head_loss(x, w, y, workspace=ws)
+
+
+def _whole(N, D, V, dtype, seed):
+    """Inputs whose products are whole numbers of at most D, so a logit is rounded once, where the bias is added."""
+    g = torch.Generator().manual_seed(seed)
+    x, w = (torch.randint(-1, 2, s, generator=g).to(dtype).cuda() for s in ((N, D), (V, D)))
+    y = torch.randint(0, V, (N,), generator=g, dtype=torch.int32).cuda()
+    grad = ((torch.rand((N,), generator=g) - 0.2) / N).cuda()
+    return x, w, y, grad
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("offset", [100.0, -1e4, 1e6, -1e6, -1e9, 1e9, -1e30, 1e30, torch.finfo(torch.float32).min])
+@pytest.mark.parametrize("N", [1, 30, 65, 300])
+def test_all_logits_far_from_zero(N, offset, dtype):
+    """A bias of one value on every class: logits are rounded beside it (from 1e9 on all to the bias itself), and the
+    loss is that of the rounded ones, whose differences are exact.  Each exponential is off by a relative
+    2^-22 (1 + |l - m|), their sum also by (V / 2048 + 128) u.  The gradients take the lse that the loss returned."""
+    import paper_1702_07825_amd as wn
+    D, V = 24, 700
+    x, w, y, grad = _whole(N, D, V, dtype, seed=31)
+    b = torch.full((V,), offset, device="cuda")
+    print("far", N, offset, dtype, flush=True)
+    l = ((x.double() @ w.double().t().contiguous()) + b.double()).float().double()
+    at = y.long()[:, None]
+    m = l.max(dim=1, keepdim=True).values
+    spread = float((l - m).abs().max())
+    want = (l - m).exp().sum(dim=1).log() + (m - l.gather(1, at))[:, 0]
+    loss, lse = wn.head_loss(x, w, y, b=b)
+    tol = (V / 2048 + 128) * U + 2.0 ** -22 * (1 + spread) + U * want
+    assert bool(((loss.double() - want).abs() <= tol).all())
+    assert bool(((lse.double() - torch.logsumexp(l - m, dim=1) - m[:, 0]).abs() <= tol + U * lse.double().abs()).all())
+    p = (l - lse.double()[:, None]).exp()
+    e = 2.0 ** -22 * (1 + (l - lse.double()[:, None]).abs()) * p
+    hot = torch.zeros_like(p).scatter_(1, at, 1.0)
+    G = grad.double()[:, None]
+    got = wn.head_loss_backward(x, w, y, lse, grad, b=b)
+    q, e = (p - hot) * G, (e + U * hot) * G.abs()
+    for t, a, ea, c in ((got[0], q, e, w), (got[1], q.t().contiguous(), e.t().contiguous(), x)):
+        c, K = c.double(), a.shape[1]
+        v, A = a @ c, a.abs() @ c.abs()
+        if dtype == torch.float32:
+            err = (3 * 2.0 ** -22 + 3 * K * U) * A + 2.0 ** -38 * K * float(G.abs().max()) + 4 * U * v.abs()
+        else:
+            err = (2.0 ** -8 + K * U) * A + 2.0 ** -8 * v.abs()
+        assert bool(((t.double() - v).abs() <= err + ea @ c.abs() + K * 2.0 ** -126).all())
+    assert bool(((got[2].double() - q.sum(dim=0)).abs() <= e.sum(dim=0) + N * U * q.abs().sum(dim=0) + N * 2.0 ** -126).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 40, 65, 300])
+@pytest.mark.parametrize("size", [1.0, 20.0, 300.0, 1e4])
+def test_losses_are_not_negative(N, size, dtype):
+    """Rows whose target has the largest logit, by enough that the others hardly count: the sum of exponentials holds a 1,
+    so its log is never below 0, and nor is the loss; above it by the others' 2^-24 and less at most."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = (t.cuda() for t in _inputs(N, 64, 500, dtype, seed=32, ignored=0))
+    x = (x.float() * size).to(dtype)
+    l = x.double() @ w.double().t().contiguous() + b.double()
+    top = l.topk(2, dim=1)
+    y = top.indices[:, 0].to(torch.int32).contiguous()
+    loss = wn.head_loss(x, w, y, b=b)[0]
+    assert bool((loss >= 0).all())
+    sure = top.values[:, 0] - top.values[:, 1] > 30 + 1e-2 * size  # (beyond the logits' own rounding)
+    assert not bool((loss[sure] > 500 * 2.0 ** -40).any())
