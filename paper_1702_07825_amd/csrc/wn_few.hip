@@ -319,7 +319,7 @@ struct FewGrad {
           else *reinterpret_cast<u32x2*>(d) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
         }
         if (qt) {
-          const float gh = most != 0.f ? gn[j] / most : 0.f;
+          const float gh = most != 0.f ? gn[j] / most : gn[j];  // (a NaN, which max |g| passes over, stays)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (v + e < f.V) put(qt + (size_t)(v + e) * npad + r, p[e] * gh);

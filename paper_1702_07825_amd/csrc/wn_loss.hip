@@ -423,7 +423,7 @@ struct GradEnd {
       const bool ok = yn >= 0 && yn < l.V_all;
       const int t = ok ? yn - l.v0 : -1;
       const float ln = ok ? lse[n] : 0.f, gn = ok ? g[n] : 0.f;
-      const float gh = most != 0.f ? gn / most : 0.f;  // (1 where all rows weigh alike)
+      const float gh = most != 0.f ? gn / most : gn;  // (1 where all rows weigh alike; a NaN, which max |g| passes over, stays)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll

@@ -491,3 +491,22 @@ def test_losses_are_not_negative(N, size, dtype):
     assert bool((loss >= 0).all())
     sure = top.values[:, 0] - top.values[:, 1] > 30 + 1e-2 * size  # (beyond the logits' own rounding)
     assert not bool((loss[sure] > 500 * 2.0 ** -40).any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 40, 100])
+@pytest.mark.parametrize("rest", ["nan", "zero", "some"])
+def test_upstream_gradients_that_are_nan_show(N, rest, dtype):
+    """NaN in every row's g, in one row's beside zeros, or beside others: dw and db hold it throughout (each entry adds
+    up a q of that row that is not 0), and dx in those rows alone."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = (t.cuda() for t in _inputs(N, 40, 90, dtype, seed=33, ignored=0))
+    bad = torch.ones(N, dtype=torch.bool, device="cuda")
+    if rest != "nan":
+        bad[1:] = False
+        grad = grad * (rest == "some")
+    grad[bad] = float("nan")
+    loss, lse = wn.head_loss(x, w, y, b=b)
+    dx, dw, db = wn.head_loss_backward(x, w, y, lse, grad, b=b)
+    assert bool(torch.isnan(dw).all()) and bool(torch.isnan(db).all())
+    assert bool(torch.isnan(dx[bad]).all()) and bool(torch.isfinite(dx[~bad]).all())
