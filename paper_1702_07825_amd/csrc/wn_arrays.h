@@ -35,6 +35,13 @@ __device__ __forceinline__ void put(u16* p, float v) { *p = bf16_bits(v); }
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 inline size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
 
+// A launch takes fewer than 2^32 threads in a dimension: more than 2^20 blocks go on in grid.y (the last ones behind the end).
+inline dim3 many_blocks(size_t blocks) {
+  const size_t x = std::min<size_t>(blocks, (size_t)1 << 20);
+  return dim3((unsigned)x, (unsigned)ceil_div(blocks, x));
+}
+__device__ __forceinline__ long long block_of_many() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Makes the device that the call's arrays live on current until the end of the scope.  check() an array before the
 // scope is entered: WN_EINVAL for memory that is not on a device (or on another one than the others).
 class ArrayScope {

@@ -78,7 +78,7 @@ __device__ __forceinline__ void put_piece(E* p, int left, const float (&v)[W]) {
 template <class E, int W>
 __global__ __launch_bounds__(256) void embed_rows(const E* table, const int32_t* t, int N, int D, int V, float scale, E* out, int G) {
   const int lane = threadIdx.x & (G - 1);
-  const long long n = (long long)blockIdx.x * (256 / G) + threadIdx.x / G;
+  const long long n = block_of_many() * (256 / G) + threadIdx.x / G;
   if (n >= N) return;
   const int v = t[n];
   const bool ok = v >= 0 && v < V;
@@ -539,7 +539,7 @@ template <class E>
 int run_forward(int N, int D, int V, const E* table, const int32_t* t, float scale, E* out, hipStream_t st) {
   constexpr int W = 16 / sizeof(E);
   const int G = lanes_of(D, W);
-  hipLaunchKernelGGL((embed_rows<E, W>), dim3((unsigned)ceil_div(N, 256 / G)), dim3(256), 0, st, table, t, N, D, V, scale, out, G);
+  hipLaunchKernelGGL((embed_rows<E, W>), many_blocks(ceil_div(N, 256 / G)), dim3(256), 0, st, table, t, N, D, V, scale, out, G);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
 }

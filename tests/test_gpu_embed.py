@@ -179,3 +179,14 @@ def test_no_rows_and_refusals():
               lambda: wn.embed_backward(torch.ones((3, 4), device="cuda"), t, 5, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(wn.WnError):
             f()
+
+
+def test_lookup_of_more_threads_than_a_launch_takes():
+    """2^24 rows by a block each (34 GB): beyond 2^32 threads in all."""
+    import paper_1702_07825_amd as wn
+    N, V, D = (1 << 24) + 5, 300, 1032
+    table = torch.randn((V, D), generator=torch.Generator().manual_seed(9)).bfloat16().cuda()
+    t = torch.randint(0, V, (N,), generator=torch.Generator(device="cuda").manual_seed(9), device="cuda", dtype=torch.int32)
+    out = wn.embed(table, t)
+    for a in range(0, N, 1 << 20):
+        assert torch.equal(out[a:a + (1 << 20)], table[t[a:a + (1 << 20)].long()]), a
