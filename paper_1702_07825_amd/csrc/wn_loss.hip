@@ -809,7 +809,7 @@ template <class E>
 __global__ __launch_bounds__(256) void join_parts(const float* part, int parts, size_t n, E* out, const int32_t* y, int V, unsigned D, const float* g) {
   __shared__ f32x4 s[3][64];
   const int c = threadIdx.x & 63, w = threadIdx.x >> 6, each = (parts + 3) / 4;
-  const size_t i = ((size_t)blockIdx.x * 64 + c) * 4;
+  const size_t i = ((size_t)block_of_many() * 64 + c) * 4;
   f32x4 v{0.f, 0.f, 0.f, 0.f};
   if (i + 3 < n) {
 #pragma unroll 8
@@ -1086,7 +1086,7 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
 template <class E>
 hipError_t join(const float* part, int parts, size_t n, E* out, hipStream_t st, const int32_t* y = nullptr, int V = 0, int D = 1,
                 const float* g = nullptr) {
-  hipLaunchKernelGGL(join_parts<E>, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out, y, V, (unsigned)D, g);
+  hipLaunchKernelGGL(join_parts<E>, many_blocks(ceil_div(n, 256)), dim3(256), 0, st, part, parts, n, out, y, V, (unsigned)D, g);
   return hipGetLastError();
 }
 

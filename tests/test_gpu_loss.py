@@ -510,3 +510,25 @@ def test_upstream_gradients_that_are_nan_show(N, rest, dtype):
     dx, dw, db = wn.head_loss_backward(x, w, y, lse, grad, b=b)
     assert bool(torch.isnan(dw).all()) and bool(torch.isnan(db).all())
     assert bool(torch.isnan(dx[bad]).all()) and bool(torch.isfinite(dx[~bad]).all())
+
+
+def test_gradient_of_more_values_than_a_launch_takes_threads():
+    """dx of 2^32 values, summed over two pieces of the vocabulary."""
+    import paper_1702_07825_amd as wn
+    N, D, V = 1 << 20, 4096, 300
+    g = torch.Generator(device="cuda").manual_seed(34)
+    x = torch.empty((N, D), dtype=torch.bfloat16, device="cuda")
+    for a in range(0, N, 1 << 17):
+        x[a:a + (1 << 17)] = torch.randn((1 << 17, D), generator=g, device="cuda").bfloat16()
+    w = (torch.randn((V, D), generator=g, device="cuda") / D ** 0.5).bfloat16()
+    y = torch.randint(0, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    y[1::7] = -1
+    grad = torch.rand((N,), generator=g, device="cuda")
+    loss, lse = wn.head_loss(x, w, y)
+    dx = wn.head_loss_backward(x, w, y, lse, grad, need=("dx",))[0]
+    rows = torch.cat([torch.arange(300), torch.randint(0, N, (500,), generator=torch.Generator().manual_seed(35)),
+                      torch.arange(N - 300, N)]).cuda()
+    want = _formulas(x[rows], w, None, y[rows], grad[rows])
+    _near(loss[rows], want["loss"], "loss")
+    _near(dx[rows], want["dx"], "dx")
+    assert not bool(dx[1::7].any())
