@@ -887,9 +887,12 @@ Shape shape_for(size_t a, size_t b, int units, bool sp, bool may_split) {
   return best;
 }
 
-// Classes of a forward piece: a multiple of 256, pieces alike.
-int forward_piece(int V, size_t each) {
-  const size_t most = std::max<size_t>(256, kForwardPiece / each / 256 * 256), pieces = ceil_div(V, most);
+// Classes of a forward piece: a multiple of 256, pieces alike.  `each`: bytes of a packed class, 0 where w stays as it is.  A
+// launch takes fewer than 2^32 threads: 256 for 128 x 128 outputs, half as many for 256 x 256.
+int forward_piece(int N, int V, size_t each) {
+  const size_t launch = (((size_t)1 << 24) - 1) / ceil_div(N, 128) * 128;
+  const size_t most = std::max<size_t>(256, (each ? std::min(launch, kForwardPiece / each) : launch) / 256 * 256);
+  const size_t pieces = ceil_div(V, most);
   return (int)std::min<size_t>(V, ceil_div(ceil_div(V, pieces), 256) * 256);
 }
 
@@ -915,7 +918,7 @@ struct Forward {
       total = c.at;
       return;
     }
-    piece = forward_piece(V, units * 2 + 4);
+    piece = forward_piece(N, V, units * 2 + 4);
     part = c.take(ceil_div(V, 128) * N * sizeof(float2));
     target = c.take((size_t)N * 4);
     x = c.take((size_t)N * units * 2);
@@ -1064,7 +1067,7 @@ int run_forward(int N, int D, int V, const E* x, const E* w, const float* b, con
   RowPacker<E> pack;
   const Operand ox = pack.add(x, N, D, reinterpret_cast<u16*>(ws + f.x), ex);
   const bool direct = !sp && D % 8 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
-  const int piece = direct ? V : f.piece;
+  const int piece = direct ? forward_piece(N, V, 0) : f.piece;
   int tiles = 0;
   for (int v0 = 0; v0 < V; v0 += piece) {
     const int n = std::min(piece, V - v0);

@@ -532,3 +532,18 @@ def test_gradient_of_more_values_than_a_launch_takes_threads():
     _near(loss[rows], want["loss"], "loss")
     _near(dx[rows], want["dx"], "dx")
     assert not bool(dx[1::7].any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_logits_of_more_tiles_than_a_launch_takes(dtype):
+    """2^20 rows of 8 values under 2^19 classes and some: beyond 2^32 threads for all tiles."""
+    import paper_1702_07825_amd as wn
+    N, D, V = 1 << 20, 8, (1 << 19) + 77
+    x, w, b, y, grad = (t.cuda() for t in _inputs(N, D, V, dtype, seed=36))
+    print("tiles", N, V, dtype, flush=True)
+    loss, lse = wn.head_loss(x, w, y, b=b)
+    rows = torch.cat([torch.arange(40), torch.randint(0, N, (80,), generator=torch.Generator().manual_seed(37)),
+                      torch.arange(N - 40, N)]).cuda()
+    want = _formulas(x[rows], w, b, y[rows], grad[rows])
+    _near(loss[rows], want["loss"], "loss")
+    _near(lse[rows], want["lse"], "lse")
