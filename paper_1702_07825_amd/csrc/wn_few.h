@@ -2,6 +2,30 @@
 #pragma once
 #include "wn_arrays.h"
 
+#include "wn_wave.h"
+
+namespace wnt {
+
+// Over a lane's place in the four rows of 16 lanes.
+__device__ __forceinline__ float quads_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float quads_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// Over the 16 lanes of a row of lanes.
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, wnk::dpp<0xB1>(v));
+  v = fmaxf(v, wnk::dpp<0x4E>(v));
+  v = fmaxf(v, wnk::dpp<0x141>(v));
+  return fmaxf(v, wnk::dpp<0x140>(v));
+}
+
+}  // namespace wnt
+
 // Calls of up to this many rows read w from memory straight into registers, once each pass, instead of through tiles
 // in LDS.
 constexpr int kFewRows = 64;

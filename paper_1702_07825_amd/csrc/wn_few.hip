@@ -8,8 +8,6 @@
 // operand B's the rows, NB tiles of 16.
 #include "wn_few.h"
 
-#include "wn_wave.h"
-
 namespace {
 
 using namespace wnt;
@@ -218,23 +216,6 @@ __global__ __launch_bounds__(256, 2) void few_logits(const WnFew f, const End en
       for (int j = 0; j < NB; ++j) acc[t][j][e] = v < f.V ? acc[t][j][e] + bv : -INFINITY;
     }
   end(f, acc, v0 + 4 * quad, n, quad, wave);
-}
-
-__device__ __forceinline__ float quads_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-__device__ __forceinline__ float quads_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
-
-// Over the 16 lanes of a row of lanes.
-__device__ __forceinline__ float row16_max(float v) {
-  v = fmaxf(v, wnk::dpp<0xB1>(v));
-  v = fmaxf(v, wnk::dpp<0x4E>(v));
-  v = fmaxf(v, wnk::dpp<0x141>(v));
-  return fmaxf(v, wnk::dpp<0x140>(v));
 }
 
 struct FewStats {

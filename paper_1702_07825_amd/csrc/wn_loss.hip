@@ -18,8 +18,6 @@
 // and 72 us in bf16, 74 and 135 in fp32).
 #include "wn_few.h"
 
-#include "wn_wave.h"
-
 namespace {
 
 using namespace wnt;
@@ -66,6 +64,7 @@ using Small = Tile<128, 128, 2, 2>;
 // row b = b0 + 16 j + n.
 struct Place {
   int ta, tb, split;  // tile
+  int last;           // the last chunk of the sum
   int a0, b0;         // this wave's first output
   int wa, wb, n, quad;
 };
@@ -122,6 +121,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
   const int va = (tid >> 3) * g.a.ld * 2 + piece * 16, vb = (tid >> 3) * g.b.ld * 2 + piece * 16;
   const int kc = (max(g.a.k, g.b.k) + kChunk - 1) / kChunk;
   const int c0 = pl.split * g.cps, c1 = min(kc, c0 + g.cps);
+  pl.last = c1 - 1;
   auto stage_piece = [&](int c, char* to, int i) {
     const bool isa = i < T::IA;
     const int k = isa ? i : i - T::IA;
@@ -175,6 +175,8 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Prod
   for (int c = c0; c < c1; ++c) {
     const char* at = buffer(c);
     char* const to = buffer(c);
+    if constexpr (End::kScaledByTile)
+      if (c > c0) end.template to_chunk<T>(acc, pl, c);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < T::NA; ++i) {
@@ -278,20 +280,12 @@ struct Logits {
   }
 };
 
-__device__ __forceinline__ float across_quads_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-__device__ __forceinline__ float across_quads_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
-
 // Forward: (largest logit, sum of exp(l - largest)) of each row in the tile's classes, and the target's logit.  The largest
 // is taken off a logit before the product with log2 e: l - largest is exact near it, so the largest class counts 1 wherever the
 // logits lie and no loss is negative.  (fma(l, log2 e, -largest log2 e) is one operation shorter, but the rounding of
 // its last term moves every exponential of the row: by 1e-6 at logits of 20, a factor of 3e5 at -1e9.)
 struct StatsEnd {
+  static constexpr bool kScaledByTile = false;
   Logits l;
   float2* part;   // [tiles of all pieces][N]
   int tile0;      // the piece's first
@@ -307,7 +301,7 @@ struct StatsEnd {
       float m = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) m = fmaxf(fmaxf(fmaxf(m, acc[i][j][0]), acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
-      m = across_quads_max(m);
+      m = quads_max(m);
       Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { target[n] = acc[i][j][e]; });
       // (a row without a class yet: every exponential is 0, not exp(-inf + inf))
       const float at = m == -INFINITY ? 0.f : m;
@@ -315,7 +309,7 @@ struct StatsEnd {
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += wnk::expf_fast(acc[i][j][e] - at);
-      sum = across_quads_sum(sum);
+      sum = quads_sum(sum);
       if (pl.quad == 0) s[pl.wa * T::TB + pl.wb * (T::TB / T::WB) + 16 * j + pl.n] = make_float2(m, sum);
     }
     __syncthreads();
@@ -352,8 +346,12 @@ __device__ __forceinline__ float join_largest(const float* parts, int n) {
   return wnk::wave_max(lane < n ? parts[lane] : 0.f);
 }
 
-// 16-bit operand units of q (bf16, or the fp16 parts of q 2^14).
-constexpr int kQScale = 14;
+// 16-bit operand units of q: bf16, or fp16 parts of q 2^e.  As dx's operand e is 14: a row's largest q is off by 2^-24 as
+// 1 - p, so what 2^-39 cuts off is not seen.  As dw's operand a row is a class, which no row may target and whose
+// probabilities may all be small: there e is the class's own within a tile of rows, so that the tile's
+// largest p (1 if a row targets the class) lies in [2^14, 2^15), up to kQMost (a tile all below 2^-66 is held to 2^-105).  dw's sums change from one tile's
+// scale to the next by at most 2^66: below 2^116 with 2^20 rows of products below 2^30.
+constexpr int kQScale = 14, kQMost = 80;
 __device__ __forceinline__ void split(float v, u16& hi, u16& lo) {
   const _Float16 h = (_Float16)v;
   const float r = v - (float)h;
@@ -371,13 +369,53 @@ __device__ __forceinline__ void split(float v, u16& hi, u16& lo) {
 // hi and lo parts) at a time, so that its stores are runs of 128 bytes.
 template <bool SP>
 struct GradEnd {
+  static constexpr bool kScaledByTile = false;
   Logits l;
   const float *lse, *g;
   const float* gmax;  // bf16: parts of max |g| (largest_g); null without qt
   int gparts;
   u16 *q, *qt;     // or null
   int ldq, ldqt;
+  int* eq;         // fp32: qt's scales, [tiles of rows][V]
   float* db;       // [tiles of rows][V], or null
+  // 2^e of this lane's classes over the tile's rows, whose log p are in acc: a class's rows lie in 16 lanes of each of WB
+  // waves.  A class that a row of the tile targets may have a q near -1.
+  template <class T>
+  __device__ __forceinline__ void class_scales(const f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds, f32x4 (&by)[T::NA]) const {
+    float* const s = reinterpret_cast<float*>(lds);  // [WB][TA], and [TA]: 0 for a target, -inf
+    for (int k = threadIdx.x; k < T::TA; k += T::kThreads) s[T::WB * T::TA + k] = -INFINITY;
+    __syncthreads();
+    for (int k = threadIdx.x; k < T::TB; k += T::kThreads) {
+      const int n = pl.tb * T::TB + k, yn = n < l.N ? l.y[n] : -1, a = yn < 0 ? -1 : yn - l.v0 - pl.ta * T::TA;
+      if (a >= 0 && a < T::TA) s[T::WB * T::TA + a] = 0.f;
+    }
+    const int at = pl.wa * 16 * T::NA + 4 * pl.quad;
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i) {
+      f32x4 m;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        m[e] = acc[i][0][e];
+#pragma unroll
+        for (int j = 1; j < T::NB; ++j) m[e] = fmaxf(m[e], acc[i][j][e]);
+        m[e] = row16_max(m[e]);
+      }
+      if (pl.n == 0) *reinterpret_cast<f32x4*>(s + pl.wb * T::TA + at + 16 * i) = m;
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < T::TA; k += T::kThreads) {
+      float m = s[k];
+#pragma unroll
+      for (int w = 1; w <= T::WB; ++w) m = fmaxf(m, s[w * T::TA + k]);
+      const int e = kQScale - (int)fminf(fmaxf(floorf(m * 1.4426950408889634f), kQScale - kQMost), 0.f), v = pl.ta * T::TA + k;
+      s[k] = __uint_as_float((unsigned)(127 + e) << 23);
+      if (v < l.V) eq[(size_t)pl.tb * l.V + v] = e;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i) by[i] = *reinterpret_cast<const f32x4*>(s + at + 16 * i);
+    __syncthreads();  // (what follows writes where s lies)
+  }
   template <class T>
   __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
     l.take<T>(acc, pl);
@@ -416,37 +454,53 @@ struct GradEnd {
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
-#pragma unroll
-    for (int j = 0; j < T::NB; ++j) {
+    float gn[T::NB];
+    int t[T::NB];
+    auto less_lse = [&](int j) {  // acc: log p (p is 0 in a row without a target, whatever it holds)
       const int n = pl.b0 + 16 * j + pl.n;
       const int yn = n < l.N ? l.y[n] : -1;
       const bool ok = yn >= 0 && yn < l.V_all;
-      const int t = ok ? yn - l.v0 : -1;
-      const float ln = ok ? lse[n] : 0.f, gn = ok ? g[n] : 0.f;
-      const float gh = most != 0.f ? gn / most : gn;  // (1 where all rows weigh alike; a NaN, which max |g| passes over, stays)
+      const float ln = ok ? lse[n] : 0.f;
+      gn[j] = ok ? g[n] : 0.f;
+      t[j] = ok && yn - l.v0 < l.V ? yn - l.v0 : -1;
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = wnk::expf_fast(acc[i][j][e] - ln);
-          acc[i][j][e] = ok ? p : 0.f;  // (whatever a row without a target holds)
-        }
-      Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { acc[i][j][e] -= 1.f; });
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = ok ? acc[i][j][e] - ln : -INFINITY;
+    };
+    f32x4 by[SP ? T::NA : 1];
+    if constexpr (SP) {
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) less_lse(j);
+      if (qt) class_scales<T>(acc, pl, lds, by);
+    }
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      if constexpr (!SP) less_lse(j);
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = wnk::expf_fast(acc[i][j][e]);
+      Logits::at_target<T>(pl, t[j], [&](int i, int e) { acc[i][j][e] -= 1.f; });
+      const int n = pl.b0 + 16 * j + pl.n;
+      const float gh = most != 0.f ? gn[j] / most : gn[j];  // (1 where all rows weigh alike; a NaN, which max |g| passes over, stays)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
         const int v = pl.a0 + 16 * i + 4 * pl.quad;
         const f32x4 p = acc[i][j];
-        acc[i][j] = p * gn;
+        acc[i][j] = p * gn[j];
         if constexpr (SP) {
           u16 hi[4], lo[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) split(ldexpf(p[e], kQScale), hi[e], lo[e]);
           if (q && n < l.N && v < ldq / 2) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split(p[e] * (1 << kQScale), hi[e], lo[e]);
             u16* d = q + (size_t)n * ldq + v / 32 * kChunk + v % 32;
             *reinterpret_cast<u32x2*>(d) = u32x2{(unsigned)hi[0] | (unsigned)hi[1] << 16, (unsigned)hi[2] | (unsigned)hi[3] << 16};
             *reinterpret_cast<u32x2*>(d + 32) = u32x2{(unsigned)lo[0] | (unsigned)lo[1] << 16, (unsigned)lo[2] | (unsigned)lo[3] << 16};
           }
           if (qt) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split(p[e] * by[i][e], hi[e], lo[e]);
             put_pair(i, 16 * (j & 1) + (pl.n & ~1), hi);
             put_pair(i, 32 + 16 * (j & 1) + (pl.n & ~1), lo);
           }
@@ -491,8 +545,11 @@ struct GradEnd {
 // dx and dw: out[b][a] (rows of D).
 template <class E>
 struct OutEnd {
+  static constexpr bool kScaledByTile = sizeof(E) == 4;
   int A, B;           // D, rows
-  const int* ea;      // fp32: scales of operand A's rows; the product is acc 2^-(ea[a] + kQScale)
+  const int* ea;      // fp32: scales of operand A's rows; the product is acc 2^-(ea[a] + eb)
+  const int* eq;      // fp32 dw: eb of each tile of k, [tiles][B]; or null: kQScale
+  int tile;           // log2 of its chunks
   const int32_t* y;   // dx: rows whose y is outside 0 .. V-1 are 0; or null
   const float* g;     // dx: the row's factor; or null
   const float* gmax;  // bf16 dw: parts of the factor of all (largest_g); or null
@@ -501,16 +558,32 @@ struct OutEnd {
   float* sum;         // [splits][B][A], set (add = 0) or added to; or null
   int add;
   E* out;             // where sum is null
+  // The sums before chunk c in the units of its tile, where it is the first of one.
+  template <class T>
+  __device__ __forceinline__ void to_chunk(f32x4 (&acc)[T::NA][T::NB], const Place& pl, int c) const {
+    if (!eq || c & ((1 << tile) - 1)) return;
+    const int* now = eq + (size_t)(c >> tile) * B;
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      const int b = min(pl.b0 + 16 * j + pl.n, B - 1);
+      const float f = __uint_as_float((unsigned)(127 + now[b] - (now - B)[b]) << 23);  // (at most 2^66 either way)
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) acc[i][j] *= f;
+    }
+  }
   template <class T>
   __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char*) const {
     if constexpr (sizeof(E) == 4) {
+      int eb[T::NB];
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) eb[j] = eq ? eq[(size_t)(pl.last >> tile) * B + min(pl.b0 + 16 * j + pl.n, B - 1)] : kQScale;
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int s = -(ea[min(pl.a0 + 16 * i + 4 * pl.quad + e, A - 1)] + kQScale);
+          const int s = ea[min(pl.a0 + 16 * i + 4 * pl.quad + e, A - 1)];
 #pragma unroll
-          for (int j = 0; j < T::NB; ++j) acc[i][j][e] = ldexpf(acc[i][j][e], s);
+          for (int j = 0; j < T::NB; ++j) acc[i][j][e] = ldexpf(acc[i][j][e], -(s + eb[j]));
         }
     }
     const float all = gmax ? join_largest(gmax, gparts) : 1.f;
@@ -932,7 +1005,7 @@ struct Forward {
 struct Backward {
   int piece;
   Shape logits, dxs, dws;  // of a whole piece
-  size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, db, cmax, gmax, dx, dw, total;
+  size_t x, ex, xt, ext, w, ew, wt, ewt, q, qt, eq, db, cmax, gmax, dx, dw, total;
   WnFewPlan few;
   void plan(bool sp, int N, int D, int p) {
     piece = p;
@@ -981,6 +1054,7 @@ struct Backward {
     ewt = c.take((size_t)D * 4);
     q = c.take((size_t)N * uv * 2);
     qt = c.take((size_t)piece * un * 2);
+    eq = c.take(sp ? ceil_div(N, 128) * piece * 4 : 0);
     db = c.take(ceil_div(N, 128) * piece * 4);
     cmax = c.take((size_t)kColumnParts * D * 4);
     gmax = c.take(kGParts * 4);
@@ -1125,19 +1199,20 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
     pack.launch(st);
     const bool big = f.logits.big;
     GradEnd<sp> end{{sp ? ints(f.ex) : nullptr, sp ? ints(f.ew) : nullptr, b ? b + v0 : nullptr, y, N, n, v0, V},
-                    lse, g, gmax, gparts, dx ? units(f.q) : nullptr, dw ? units(f.qt) : nullptr, ldq, ldqt, db ? floats(f.db) : nullptr};
+                    lse, g, gmax, gparts, dx ? units(f.q) : nullptr, dw ? units(f.qt) : nullptr, ldq, ldqt,
+                    ints(f.eq), db ? floats(f.db) : nullptr};
     e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
     if (e == hipSuccess && db) e = join(floats(f.db), (int)ceil_div(N, big ? 256 : 128), n, db + v0, st);
     if (e == hipSuccess && dx) {
       const Operand owt = cols_operand(wv, n, D, RowFactor{nullptr, nullptr, 0}, units(f.wt), floats(f.cmax), ints(f.ewt), st);
       const bool whole = f.piece == V && f.dxs.splits == 1;
-      const OutEnd<E> o{D, N, ints(f.ewt), y, g, nullptr, 0, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
+      const OutEnd<E> o{D, N, ints(f.ewt), nullptr, 0, y, g, nullptr, 0, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
       e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.dxs.splits, 0}, f.dxs.big, o, st);
       if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.dxs.splits, (size_t)N * D, dx, st);
     }
     if (e == hipSuccess && dw) {
       E* const out = dw + (size_t)v0 * D;
-      const OutEnd<E> o{D, n, ints(f.ext), nullptr, nullptr, gmax, gparts, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
+      const OutEnd<E> o{D, n, ints(f.ext), sp ? ints(f.eq) : nullptr, big ? 3 : 2, nullptr, nullptr, gmax, gparts, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
       e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.dws.splits, 0}, f.dws.big, o, st);
       if (e == hipSuccess && f.dws.splits > 1) e = join(floats(f.dw), f.dws.splits, (size_t)n * D, out, st);
     }
