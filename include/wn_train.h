@@ -116,7 +116,8 @@ typedef struct {
  * The norm over all elements of n_arrays gradient arrays (`arrays` is a HOST array, read before the call
  * returns), and the arrays scaled so that the norm is at most max_norm:
  *   norm = sqrt(sum g^2)  (summed in fp64: fp32 gradients neither overflow nor vanish)
- *   out  = g * min(1, max_norm / norm), rounded once; a copy where norm <= max_norm
+ *   out  = g * (max_norm / norm): the factor rounded to 24 bits, however small it is, then the product to fp32, and
+ *          that to bf16 in arrays of bf16; a copy where norm <= max_norm
  *   norm     fp32 [1] device, out
  * Where the norm is not finite (an infinity or NaN among the gradients, or a norm beyond fp32),
  * out is a copy of g: the caller sees it in *norm and can skip the step.  max_norm >= 0 (inf:

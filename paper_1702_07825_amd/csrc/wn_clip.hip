@@ -127,12 +127,24 @@ __global__ __launch_bounds__(kThreads) void clip_squares(const Arrays a, double*
   if (threadIdx.x == 0) slot[blockIdx.x] = add ? slot[blockIdx.x] + v : v;
 }
 
-__device__ __forceinline__ u32x4u times(u32x4u w, float f, bool bf) {
+// The factor max_norm / norm as f 2^k: k is 0 unless fp32 would hold the factor in fewer bits (below its smallest normal value,
+// for norms near its largest) or not at all.
+struct Factor {
+  float f;
+  int k;
+  __device__ __forceinline__ float operator()(float v) const { return k ? ldexpf(v * f, k) : v * f; }
+};
+__device__ __forceinline__ Factor factor_of(double r) {
+  const int k = r > 0.0 && r < 0x1p-126 ? ilogb(r) + 1 : 0;  // f in [1/2, 1): no product overflows
+  return {(float)ldexp(r, -k), k};
+}
+
+__device__ __forceinline__ u32x4u times(u32x4u w, Factor f, bool bf) {
   u32x4u r;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    r[e] = bf ? bf16_pair(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f)
-              : __float_as_uint(__uint_as_float(w[e]) * f);
+    r[e] = bf ? bf16_pair(f(__uint_as_float(w[e] << 16)), f(__uint_as_float(w[e] & 0xffff0000u)))
+              : __float_as_uint(f(__uint_as_float(w[e])));
   return r;
 }
 
@@ -146,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const dou
   if (first && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
   // (max_norm = 0: 0 times each element)
   const bool scaled = norm > max_norm && norm < INFINITY;
-  const float f = scaled ? (float)(max_norm / wide) : 1.f;
+  const Factor f = factor_of(scaled ? max_norm / wide : 1.0);
   for_share(a, true, [&](int k, long long at, int n) {
     if (!scaled && a.out[k] == a.g[k]) return;
     const bool bf = a.last[k] & kBf16;
@@ -171,10 +183,10 @@ __global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const dou
     if (rest < n) {
       if (bf) {
         const u16 v = reinterpret_cast<const u16*>(p)[rest];
-        reinterpret_cast<u16*>(o)[rest] = scaled ? bf16_bits(bf16_val(v) * f) : v;
+        reinterpret_cast<u16*>(o)[rest] = scaled ? bf16_bits(f(bf16_val(v))) : v;
       } else {
         const float v = reinterpret_cast<const float*>(p)[rest];
-        reinterpret_cast<float*>(o)[rest] = scaled ? v * f : v;
+        reinterpret_cast<float*>(o)[rest] = scaled ? f(v) : v;
       }
     }
   });

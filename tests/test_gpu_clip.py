@@ -151,3 +151,11 @@ def test_refusals():
     for m in (-1.0, float("nan")):
         with pytest.raises(wn.WnError):
             wn.clip_gradients([g], m)
+
+
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-7, 1e-20, 1e-30])
+@pytest.mark.parametrize("place", [True, False])
+def test_factors_below_fp32(max_norm, place):
+    """Norms near fp32's largest: max_norm / norm is subnormal in fp32 or 0 there, the clipped gradients are not."""
+    grads = _grads((3000, 77, 40000), (F, H), std=5e35)
+    _check(grads, max_norm, outs=None if place else [torch.empty_like(t) for t in grads])
