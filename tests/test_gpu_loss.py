@@ -590,3 +590,92 @@ def test_gradients_of_classes_that_no_row_targets(N, D, V, dtype):
         err += (2.0 ** -8 + N * U) * A + 2.0 ** -8 * v.abs()
     _near(dw, (v, err), "dw")
     assert bool((dw != 0).any(dim=1)[q.abs().amax(dim=1) > 2.0 ** -100].all())
+
+
+# Calls of up to 64 rows have kernels of their own: the same questions on the other side.
+@pytest.mark.parametrize("N,D,V,dtype", [(70, 2048, 20000, torch.float32), (300, 1023, 40000, torch.float32),
+                                         (70, 2047, 40000, torch.bfloat16), (300, 1999, 33000, torch.bfloat16)])
+def test_several_pieces_of_the_vocabulary_forwards(N, D, V, dtype):
+    """Packed classes of more than 64 MB: three pieces, which share their place, with targets and biases in each."""
+    _check(*_inputs(N, D, V, dtype, seed=40), device="cuda")
+
+
+@pytest.mark.parametrize("N", [65, 130, 600])
+def test_fp32_rows_of_unlike_sizes_from_65_rows_on(N):
+    x, w, b, y, grad = _inputs(N, 48, 200, torch.float32, seed=41)
+    x *= 10.0 ** torch.linspace(-8, 0, N)[:, None]
+    w *= 10.0 ** torch.linspace(-8, 0, 200)[:, None]
+    grad *= 10.0 ** torch.linspace(-6, 6, N)
+    _check(x, w, b, y, grad)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,D,V", [(100, 64, 300), (100, 33, 150), (300, 72, 1001), (1000, 7, 65)])
+def test_arrays_that_start_anywhere_from_65_rows_on(dtype, N, D, V):
+    """One element into their allocations, rows of whole 16-byte pieces among them; what lies around the outputs stays."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = _inputs(N, D, V, dtype, seed=42)
+    loss, lse, want = _check(x, w, b, y, grad)
+
+    def at1(t):
+        s = torch.full((t.numel() + 2,), 7, dtype=t.dtype, device="cuda")
+        v = s[1:-1].view(t.shape)
+        v.copy_(t)
+        return s, v
+
+    (_, X), (_, W), (_, B), (_, Y), (_, G) = (at1(t) for t in (x, w, b, y, grad))
+    outs = [at1(torch.zeros_like(t)) for t in (loss, lse, *want)]
+    wn.head_loss(X, W, Y, b=B, loss=outs[0][1], lse=outs[1][1])
+    wn.head_loss_backward(X, W, Y, outs[1][1], G, b=B, dx=outs[2][1], dw=outs[3][1], db=outs[4][1])
+    for (s, v), t in zip(outs, (loss, lse, *want)):
+        assert torch.equal(v, t)
+        assert float(s[0]) == 7 and float(s[-1]) == 7
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N", [20, 100])
+def test_masked_targets_and_values_that_are_not_finite(N, dtype):
+    """A masked target's loss is infinite, its gradients finite; a NaN in x shows in its row's loss alone and in dw; an
+    infinity in w in every loss whose logit it raises."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, grad = (t.cuda() for t in _inputs(N, 40, 300, dtype, seed=43, ignored=0))
+    masked = b.clone()
+    masked[7] = -float("inf")
+    y = torch.where(y == 7, 8, y).to(torch.int32)
+    y[3] = 7
+    loss, lse = wn.head_loss(x, w, y, b=masked)
+    assert float(loss[3]) == float("inf") and int(torch.isfinite(loss).sum()) == N - 1
+    for t in wn.head_loss_backward(x, w, y, lse, grad, b=masked):
+        assert bool(torch.isfinite(t).all())
+    x[4, 5] = float("nan")
+    loss, lse = wn.head_loss(x, w, y, b=b)
+    assert bool(torch.isnan(loss[4])) and int(torch.isnan(loss).sum()) == 1
+    assert bool(torch.isnan(wn.head_loss_backward(x, w, y, lse, grad, b=b)[1]).any())
+    w[9, 0] = float("inf")
+    assert not bool(torch.isfinite(wn.head_loss(x, w, y, b=b)[0][x[:, 0] > 0]).any())
+
+
+def test_gradient_against_differences_from_65_rows_on():
+    """As for few rows: the central difference is off by h^2 / 6 of the third derivative, at most 8 max|dl|^3 sum|g|, and by
+    the losses' tolerance over h; the gradient along the direction by its entries' tolerances."""
+    import paper_1702_07825_amd as wn
+    args = _inputs(150, 32, 120, torch.float32, seed=44)
+    g = torch.Generator().manual_seed(45)
+    dirs = [torch.randn(t.shape, generator=g) / t.numel() ** 0.5 for t in args[:3]]
+    X, W, B, Y, G = (t.cuda() for t in args)
+    tols = _formulas(X, W, B, Y, G)
+    loss, lse = wn.head_loss(X, W, Y, b=B)
+    grads = wn.head_loss_backward(X, W, Y, lse, G, b=B)
+    for k, (t, d, got, name) in enumerate(zip((X, W, B), dirs, grads, ("dx", "dw", "db"))):
+        d, h = d.cuda(), 2.0 ** -6
+        f = []
+        for s in (h, -h):
+            a = [X, W, B]
+            a[k] = t + s * d
+            f.append(float((G.double() * wn.head_loss(a[0], a[1], Y, b=a[2])[0].double()).sum()))
+        dl = float((d @ W.t().contiguous() if k == 0 else X @ d.t().contiguous() if k == 1 else d).abs().max())
+        weight = float(G.abs().sum())
+        # (the moved arrays are rounded to fp32 once more: 2^-24 of the logits' terms, within the losses' own tolerance)
+        tol = h * h / 6 * 8 * dl ** 3 * weight + 2 * float(tols["loss"][1].max()) * weight / h
+        tol += float((tols[name][1] * d.double().abs()).sum())
+        assert abs((f[0] - f[1]) / (2 * h) - float((got.double() * d.double()).sum())) <= tol, name

@@ -213,3 +213,26 @@ def test_a_training_step_of_the_two_ends():
         torch.cuda.synchronize()
         near(outs, want[k])
         step(sets[(k + 1) % 3][:-1].contiguous(), sets[(k + 1) % 3][1:].contiguous())
+
+
+def test_scores_of_more_rows_than_the_loss_takes_at_a_time():
+    """2^18 rows a call of the loss: three streams of 87500 steps take two.  The scores are those of the loss on both parts,
+    and on both sides of the cut and at the ends those of 64 bits, within the tolerance above."""
+    import paper_1702_07825_amd as wn
+    B, T = 3, 87500
+    w, net = _model(4, 16, 32)
+    cond, y = _inputs(4, 16, B, T)
+    y[2, -3:] = -1
+    z = net.teacher_features(cond, y).view(-1, 256)
+    nll = net.score(cond, y).view(-1)
+    wo, b, t = torch.tensor(w["w_out"]).cuda(), torch.tensor(w["b_out"]).cuda(), y.view(-1)
+    for a, e in ((0, 1 << 18), (1 << 18, B * T)):
+        assert torch.equal(nll[a:e], wn.head_loss(z[a:e], wo, t[a:e], b=b)[0])
+    for a in (0, (1 << 18) - 40, B * T - 80):
+        zd, ta = z[a:a + 80].double(), t[a:a + 80]
+        S = zd.abs() @ wo.double().abs().t().contiguous()
+        l = zd @ wo.double().t().contiguous() + b.double()
+        want = torch.where(ta >= 0, torch.logsumexp(l, dim=1) - l.gather(1, ta.clamp(min=0).long()[:, None])[:, 0], 0.0)
+        tol = 2 * (3 * 2.0 ** -22 + 3 * 256 * 2.0 ** -24) * S.amax(dim=1) + 2.0 ** -20 * (1 + want.abs() + l.abs().amax(dim=1))
+        assert bool(((nll[a:a + 80].double() - want).abs() <= tol).all())
+    net.close()
