@@ -234,7 +234,8 @@ int wn_teacher_features(wn_handle* h, int32_t B, int32_t T, const float* cond, c
  *   nll      device fp32 [B][T] out
  *   scratch  device, >= wn_score_scratch_bytes(h, B, T) bytes, 256-byte aligned; it holds nothing between calls
  * The workspace is wn_teacher_force's and its state continues as there.  Errors as wn_teacher_features, and WN_EINVAL for
- * a null, misaligned or short scratch.  A call that wn_abort ends leaves nll undefined from that step on (wn_status).
+ * a null, misaligned or short scratch, or a y, nll or scratch that is not memory of the handle's device.  A call that
+ * wn_abort ends leaves nll undefined from that step on (wn_status).
  */
 int wn_score(wn_handle* h, int32_t B, int32_t T, const float* cond, const int32_t* y, float* nll, void* workspace,
              size_t ws_bytes, void* scratch, size_t scratch_bytes, int32_t reset, void* stream);

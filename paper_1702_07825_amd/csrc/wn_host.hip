@@ -4,7 +4,7 @@
 #include "wn_internal.h"
 #include "wn_teach.h"
 #include "wn_tiny.h"
-#include "wn_train.h"
+#include "wn_arrays.h"
 
 #include <algorithm>
 #include <cmath>
@@ -740,12 +740,17 @@ int wn_score(wn_handle* h, int32_t B, int32_t T, const float* cond, const int32_
   const int64_t rows = (int64_t)B * T;
   const ScoreLayout s(rows);
   if (scratch_bytes < s.total) return fail(WN_EINVAL, "scratch too small");
+  const WnDevWeights& w = h->dmem_f32 ? h->w_chain : h->w;
+  // What wn_loss asks of its arrays, before the features' launch moves the state.
+  wnt::ArrayScope arrays;
+  if ((rc = arrays.check(w.w_out, "the handle's memory")) != WN_OK || (rc = arrays.check(y, "y")) != WN_OK ||
+      (rc = arrays.check(nll, "nll")) != WN_OK || (rc = arrays.check(scratch, "scratch")) != WN_OK)
+    return rc;
   DeviceScope scope(h->device);
   if (!scope.ok()) return fail(WN_EHIP, "cannot select the handle's device");
   char* const base = static_cast<char*>(scratch);
   float* const features = reinterpret_cast<float*>(base);
   rc = launch_features(h, B, T, cond, y, features, workspace, ws_bytes, reset, stream);
-  const WnDevWeights& w = h->dmem_f32 ? h->w_chain : h->w;
   for (int64_t r = 0; rc == WN_OK && r < rows; r += kScoreRows)
     rc = wn_loss(WN_F32, (int32_t)std::min(kScoreRows, rows - r), WN_A, WN_A, features + r * WN_A, w.w_out, w.b_out, y + r,
                  nll + r, reinterpret_cast<float*>(base + s.lse_off), base + s.loss_off, s.total - s.loss_off, stream);

@@ -236,3 +236,25 @@ def test_scores_of_more_rows_than_the_loss_takes_at_a_time():
         tol = 2 * (3 * 2.0 ** -22 + 3 * 256 * 2.0 ** -24) * S.amax(dim=1) + 2.0 ** -20 * (1 + want.abs() + l.abs().amax(dim=1))
         assert bool(((nll[a:a + 80].double() - want).abs() <= tol).all())
     net.close()
+
+
+@pytest.mark.parametrize("what", ["y", "nll"])
+def test_refused_memory_leaves_the_state(what):
+    """y or nll in host memory is refused before anything runs: the call after it gives what it would have given."""
+    import paper_1702_07825_amd as wn
+    w, net = _model(4, 16, 32)
+    cond, y = _inputs(4, 16, 2, 60)
+    ws = net.new_workspace(2)
+    first, rest = [(cond[:, a:b].contiguous(), y[:, a:b].contiguous()) for a, b in ((0, 30), (30, 60))]
+    net.score(*first, workspace=ws)
+    want = net.score(*rest, workspace=ws, reset=False)
+    net.score(*first, workspace=ws)
+    scratch = torch.empty(int(net._lib.wn_score_scratch_bytes(net._h, 2, 30)), dtype=torch.uint8, device="cuda")
+    host = torch.zeros((2, 30), dtype=torch.int32 if what == "y" else torch.float32, pin_memory=True)
+    nll = torch.empty((2, 30), device="cuda")
+    args = {"y": rest[1].data_ptr(), "nll": nll.data_ptr(), what: host.data_ptr()}
+    rc = net._lib.wn_score(net._h, 2, 30, rest[0].data_ptr(), args["y"], args["nll"], ws.data_ptr(), ws.numel(), scratch.data_ptr(),
+                           scratch.numel(), 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == wn.WN_EINVAL and what in net._lib.wn_last_error().decode()
+    assert torch.equal(net.score(*rest, workspace=ws, reset=False), want)
+    net.close()
