@@ -375,7 +375,10 @@ class Conditioner:
 # The operators at the ends of a training step (include/wn_train.h).  Matrices are float32 or
 # bfloat16, dense; a row whose target or token lies outside the classes (-1, say) is padding.
 # ``stream`` is a torch stream of the tensors' device (default: the current one there); tensors made
-# here (outputs, workspaces) belong to that stream.
+# here (outputs, workspaces) belong to that stream, and those given are recorded on it, so they may be
+# dropped before the call has run.
+# Gradients come from the *_backward calls: no call here is differentiable by torch's autograd, whether
+# its tensors require a gradient or not, and tensors written in place keep their version.
 # ------------------------------------------------------------------------------------------------
 def _train_dtype(t, name):
     import torch
@@ -409,6 +412,12 @@ class _On:
         with torch.cuda.stream(self.other):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
+    def used(self, *tensors):
+        """Keeps tensors of other streams from being handed out again before the call has run."""
+        if self.other is not None:
+            for t in tensors:
+                t.record_stream(self.other)
+
     def out(self, t, shape, dtype, name):
         if t is None:
             t = self.empty(shape, dtype)
@@ -418,12 +427,14 @@ class _On:
     def ptr(self, t, dtype, shape, name):
         try:
             if t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
+                self.used(t)
                 return t.data_ptr()
         except AttributeError:
             pass
         p = _dev_ptr(t, dtype, shape, name)  # (says what is wrong)
         if t.device != self.device:
             raise ValueError("%s is on %s, not on %s" % (name, t.device, self.device))
+        self.used(t)
         return p
 
     def workspace(self, t, nbytes):
@@ -432,6 +443,8 @@ class _On:
             t = self.empty(max(nbytes, 1), torch.uint8)
         elif t.device != self.device or not t.is_contiguous():
             raise ValueError("workspaces must be contiguous and on %s" % self.device)
+        else:
+            self.used(t)
         return t, t.data_ptr(), t.numel() * t.element_size()
 
 
@@ -550,6 +563,7 @@ def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None,
         raise ValueError("gradients must all be on %s" % on.device)
     if not dense:
         raise ValueError("gradients must be contiguous")
+    on.used(*both)
     n = len(grads)
     if outs is not grads and (sizes[:n] != sizes[n:] or dtypes[:n] != dtypes[n:]):
         raise ValueError("outs must have the sizes and dtypes of grads")

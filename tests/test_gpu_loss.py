@@ -679,3 +679,48 @@ def test_gradient_against_differences_from_65_rows_on():
         tol = h * h / 6 * 8 * dl ** 3 * weight + 2 * float(tols["loss"][1].max()) * weight / h
         tol += float((tols[name][1] * d.double().abs()).sum())
         assert abs((f[0] - f[1]) / (2 * h) - float((got.double() * d.double()).sum())) <= tol, name
+
+
+def _late(call, make):
+    """call(stream, *tensors) on a stream that is busy; its inputs are dropped and their memory asked for again meanwhile."""
+    tensors = make()
+    sizes = [(t.shape, t.dtype) for t in tensors]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)
+    got = call(stream, *tensors)
+    del tensors
+    others = [torch.ones(s, dtype=d, device="cuda") for s, d in sizes for _ in range(2)]
+    torch.cuda.synchronize()
+    del others
+    return got
+
+
+def test_inputs_dropped_before_another_stream_has_run():
+    """Memory of inputs (and of workspaces given) that a call on another stream still has to read is not handed out."""
+    import paper_1702_07825_amd as wn
+    g = torch.Generator(device="cuda").manual_seed(46)
+
+    def make():
+        g.manual_seed(46)
+        x, w = (torch.randn(s, generator=g, device="cuda") for s in ((300, 64), (500, 64)))
+        y = torch.randint(0, 500, (300,), generator=g, device="cuda", dtype=torch.int32)
+        return x, w, y, torch.rand((300,), generator=g, device="cuda")
+
+    def loss(stream, x, w, y, grad):
+        l, lse = wn.head_loss(x, w, y, stream=stream)
+        return [l, lse, *wn.head_loss_backward(x, w, y, lse, grad, stream=stream)]
+
+    def tables(stream, x, w, y, grad):
+        return [wn.embed(w, y, stream=stream), wn.embed_backward(x, y, 500, stream=stream)]
+
+    def clip(stream, x, w, y, grad):
+        outs = [torch.empty_like(x), torch.empty_like(w)]
+        return [wn.clip_gradients([x, w], 1.0, outs=outs, stream=stream), *outs]
+
+    for call in (loss, tables, clip):
+        want = call(None, *make())
+        torch.cuda.synchronize()
+        got = _late(call, make)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), call.__name__
