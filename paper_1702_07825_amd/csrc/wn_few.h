@@ -30,20 +30,24 @@ __device__ __forceinline__ float row16_max(float v) {
 // in LDS.
 constexpr int kFewRows = 64;
 // Whether a block's four waves share its classes: where a run of classes each would leave too few blocks, and the rows
-// are long enough to cut in four.  A forward pass with classes of its own for each wave and with shared ones: 64 rows x
-// 8000 x 4096, fp32 162 and 65 us, bf16 44 and 30; x 32000 x 1024 49 and 74, 26 and 34; 16 rows x 8000 x 4096, fp32 63
-// and 37.
-inline bool wn_few_shared(bool f32, int D, int V) { return V <= 1 << 14 && D * (f32 ? 4 : 2) >= 2048; }
+// are long enough to cut in four.  A forward pass with classes of its own for each wave and with shared ones (us), rows of 1000
+// values: 64 rows, fp32 51 and 24 at 8000 classes, 51 and 42 at 16384, 51 and 55 at 20000; 17 rows 32 and 16, 32 and 26,
+// 33 and 35; 16 rows 32 and 13, 32 and 21, 33 and 24, 33 and 31 at 26000; bf16, 32 rows 13 and 10, 14 and 13, 15 and 17;
+// 64 rows 16 and 13, 17 and 17 at 12000 (of 2048 values 27 and 30), 18 and 18 at 16384.  Of 200 values at 8000 classes: 64
+// rows, fp32 18 and 13, bf16 11 and 11.
+inline bool wn_few_shared(bool f32, int N, int D, int V) {
+  return V <= (f32 || N <= 32 ? 1 << 14 : 1 << 13) && D * (f32 ? 4 : 2) >= 800;
+}
 // Tiles of 16 rows in the logits: 1, 2 or 4.  One tile takes x from the caches and two or more through LDS, which is faster
 // from a few rows on (50021 classes x 777, bf16: 4 rows 48 and 35 us, 16 rows 60 and 36); shared classes take it from
 // the caches anyway.
 inline int wn_few_tiles(bool f32, int N, int D, int V) {
-  if (N <= 16 && (N == 1 || wn_few_shared(f32, D, V))) return 1;
+  if (N <= 16 && (N == 1 || wn_few_shared(f32, N, D, V))) return 1;
   return N <= 32 ? 2 : 4;
 }
 // Classes of a block: a place in `part`.
 inline int wn_few_classes(bool f32, int N, int D, int V) {
-  return (wn_few_tiles(f32, N, D, V) == 1 ? 16 : 32) * (wn_few_shared(f32, D, V) ? 1 : 4);
+  return (wn_few_tiles(f32, N, D, V) == 1 ? 16 : 32) * (wn_few_shared(f32, N, D, V) ? 1 : 4);
 }
 
 struct WnFew {

@@ -516,7 +516,7 @@ void by_tiles(int tiles, F f) {
 template <class E, int NB, class End>
 void launch_logits(const WnFew& f, int classes, const End& end, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(classes, wn_few_classes(sizeof(E) == 4, f.N, f.D, f.V)));
-  if (wn_few_shared(sizeof(E) == 4, f.D, f.V)) hipLaunchKernelGGL((few_logits<E, NB, true, End>), grid, dim3(256), 0, st, f, end);
+  if (wn_few_shared(sizeof(E) == 4, f.N, f.D, f.V)) hipLaunchKernelGGL((few_logits<E, NB, true, End>), grid, dim3(256), 0, st, f, end);
   else hipLaunchKernelGGL((few_logits<E, NB, false, End>), grid, dim3(256), 0, st, f, end);
 }
 

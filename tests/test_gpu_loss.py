@@ -724,3 +724,10 @@ def test_inputs_dropped_before_another_stream_has_run():
         torch.cuda.synchronize()
         got = _late(call, make)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), call.__name__
+
+
+@pytest.mark.parametrize("N,D,V,dtype", [(64, 200, 16384, torch.float32), (64, 200, 16385, torch.float32), (17, 199, 900, torch.float32),
+                                         (9, 201, 1003, torch.float32), (33, 400, 8192, torch.bfloat16), (33, 400, 8193, torch.bfloat16),
+                                         (32, 401, 9000, torch.bfloat16), (20, 399, 500, torch.bfloat16), (1, 403, 257, torch.bfloat16)])
+def test_few_rows_where_waves_begin_to_share_classes(N, D, V, dtype):
+    _check(*_inputs(N, D, V, dtype, seed=47), device="cuda")
