@@ -21,10 +21,11 @@ using namespace wnt;
 
 constexpr int kArrays = 168;   // arrays of a launch: the arguments stay under 4 KB
 constexpr int kThreads = 256;
-// Elements of a chunk: long ones keep more loads in flight, short ones spread small models over the chip (127 arrays of
-// 890,000 elements: 6.8 and 6.6 us with chunks of 8192, 11.7 and 10.2 with 16384; 0.9 GB: 218 and 163 us for the squares).
+// Elements of a chunk: long ones keep more loads in flight, short ones spread small models over the chip.  Both passes in us,
+// short and long, 127 arrays of 2^20 fp32 elements in all 10.2 and 10.4 (bf16 9.4, 10.7), of 2^22 21.6 and 14.4 (18.7, 12.4),
+// of 2^26 138 and 132 (81, 70); 16 arrays 9.4 and 11.2 (8.6, 10.4), 12.7 and 13.6 (11.6, 10.7), 125 and 125 (74, 67).
 constexpr int kLong = 16384, kShort = 4096;
-constexpr long long kShortUpTo = 1LL << 26;
+constexpr long long kShortUpTo = 1LL << 21;
 constexpr int kSlots = 1024;   // blocks of a launch, partial sums
 
 struct Arrays {

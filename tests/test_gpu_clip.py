@@ -159,3 +159,10 @@ def test_factors_below_fp32(max_norm, place):
     """Norms near fp32's largest: max_norm / norm is subnormal in fp32 or 0 there, the clipped gradients are not."""
     grads = _grads((3000, 77, 40000), (F, H), std=5e35)
     _check(grads, max_norm, outs=None if place else [torch.empty_like(t) for t in grads])
+
+
+@pytest.mark.parametrize("extra", [0, 1, 5])
+def test_on_both_sides_of_the_chunks_lengths(extra):
+    sizes = (1 << 20, 12345, 0, (1 << 20) - 12345 - 7, 7 + extra)  # 2^21 elements and some
+    for dtypes in ((F,), (H,), (F, H)):
+        _check(_grads(sizes, dtypes), 300.0)
