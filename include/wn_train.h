@@ -122,8 +122,8 @@ typedef struct {
  * Where the norm is not finite (an infinity or NaN among the gradients, or a norm beyond fp32),
  * out is a copy of g: the caller sees it in *norm and can skip the step.  max_norm >= 0 (inf:
  * only the norm counts).  n_arrays 0 .. 2^20.
- * Errors as wn_loss (of the arrays only the first one's memory is looked at), and WN_EINVAL for a max_norm
- * that is negative or NaN.
+ * Errors as wn_loss (of the arrays only the first one's memory is looked at), WN_EINVAL for a max_norm
+ * that is negative or NaN and for arrays that overlap (the same one listed twice, say), and WN_ENOMEM.
  */
 int wn_clip(int32_t n_arrays, const wn_clip_array* arrays, float max_norm, float* norm, void* workspace,
             size_t ws_bytes, void* stream);

@@ -166,3 +166,15 @@ def test_on_both_sides_of_the_chunks_lengths(extra):
     sizes = (1 << 20, 12345, 0, (1 << 20) - 12345 - 7, 7 + extra)  # 2^21 elements and some
     for dtypes in ((F,), (H,), (F, H)):
         _check(_grads(sizes, dtypes), 300.0)
+
+
+def test_gradients_that_share_memory_are_refused():
+    import paper_1702_07825_amd as wn
+    g = torch.ones(100, device="cuda")
+    for grads, outs in (([g, g], None), ([g[:60], g[50:]], None), ([g[:50], g[50:]], [g[50:], g[:50]])):
+        with pytest.raises(wn.WnError) as e:
+            wn.clip_gradients(grads, 1.0, outs=outs)
+        assert e.value.code == wn.WN_EINVAL and "overlap" in str(e.value)
+    assert bool((g == 1).all())
+    outs = [torch.empty_like(g) for _ in range(2)]
+    assert float(wn.clip_gradients([g, g], 1e9, outs=outs)) == float(torch.tensor(200.0).sqrt())

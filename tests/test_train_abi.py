@@ -116,3 +116,24 @@ def test_workspace_sizes(lib):
     # a fixed multiple of the pieces' budget, whatever the vocabulary: the logits are not kept
     assert lib.wn_loss_backward_workspace_bytes(1, 8192, 2048, 1 << 20) < 4 << 30
     assert lib.wn_clip_workspace_bytes() > 0
+
+
+def test_clip_refuses_arrays_that_overlap(lib):
+    """Found before any device call; arrays that only touch, outputs that are the inputs, and inputs listed twice with
+    outputs of their own go on to the check of the memory."""
+    import paper_1702_07825_amd as wn
+
+    def clip(*arrays):
+        a = (wn.ClipArray * len(arrays))()
+        for k, (g, out, n, dtype) in enumerate(arrays):
+            a[k].g, a[k].out, a[k].n, a[k].dtype = P + g, P + out, n, dtype
+        assert lib.wn_clip(len(arrays), a, 1.0, P, P, 1 << 40, None) == -1
+        return lib.wn_last_error().decode()
+
+    for bad in (((0, 0, 4, 0), (0, 0, 4, 0)), ((0, 0, 4, 0), (12, 12, 4, 0)), ((64, 64, 8, 1), (32, 32, 9, 0)),
+                ((0, 64, 4, 0), (32, 64, 4, 0)), ((0, 8, 4, 0),), ((0, 64, 4, 0), (64, 128, 4, 0)),
+                ((16, 64, 4, 0), (0, 16, 1, 0)), ((0, 256, 4, 0), (64, 512, 4, 0), (128, 264, 4, 1))):
+        assert "overlap" in clip(*bad), bad
+    for good in (((0, 0, 4, 0), (16, 16, 4, 0)), ((32, 32, 8, 1), (0, 0, 8, 0)), ((0, 64, 4, 0), (0, 128, 4, 0)),
+                 ((0, 16, 4, 0),), ((16, 0, 4, 0),), ((0, 0, 4, 0), (4, 4, 0, 0)), ((0, 256, 4, 0), (16, 64, 4, 0), (32, 128, 4, 1))):
+        assert "device memory" in clip(*good), good
