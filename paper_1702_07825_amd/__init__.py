@@ -156,9 +156,15 @@ def _check(rc: int, where: str):
         raise WnError(rc, where, load_library().wn_last_error().decode())
 
 
-def _stream_handle(stream) -> Optional[int]:
+def _stream_handle(stream, *tensors) -> Optional[int]:
+    """The call's stream; tensors of another one are recorded on it, so that they (a workspace made for the call
+    among them) are not handed out again before the call has run."""
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
+    s = torch.cuda.current_stream()
+    if stream is not None and stream != s:
+        s = stream
+        for t in tensors:
+            t.record_stream(s)
     return s.cuda_stream
 
 
@@ -250,13 +256,14 @@ class WaveNet:
         sp = _dev_ptr(samples, torch.int32, (B, T), "samples")
         if workspace is None:
             workspace = self.new_workspace(B, cond.device)
+        on = _stream_handle(stream, cond, uniforms, samples, workspace)
         if sampler is None:
             _check(self._lib.wn_generate(self._h, B, T, cp, up, sp, workspace.data_ptr(), workspace.numel(),
-                                         1 if reset else 0, _stream_handle(stream)), "wn_generate")
+                                         1 if reset else 0, on), "wn_generate")
         else:
             smp = Sampler(int(sampler[0]), float(sampler[1]), int(sampler[2]))
             _check(self._lib.wn_generate_sampled(self._h, B, T, cp, up, sp, workspace.data_ptr(), workspace.numel(),
-                                                 1 if reset else 0, ctypes.byref(smp), _stream_handle(stream)),
+                                                 1 if reset else 0, ctypes.byref(smp), on),
                    "wn_generate_sampled")
         return samples
 
@@ -272,7 +279,8 @@ class WaveNet:
         if workspace is None:
             workspace = self.new_workspace(B, cond.device)
         _check(self._lib.wn_teacher_force(self._h, B, T, cp, yp, lp, workspace.data_ptr(), workspace.numel(),
-                                          1 if reset else 0, _stream_handle(stream)), "wn_teacher_force")
+                                          1 if reset else 0, _stream_handle(stream, cond, y, logits, workspace)),
+               "wn_teacher_force")
         return logits
 
     def teacher_features(self, cond, y, features=None, workspace=None, reset: bool = True, stream=None):
@@ -356,7 +364,7 @@ class Conditioner:
         if workspace is None:
             workspace = torch.empty(max(self.workspace_bytes(B, Tf), 1), dtype=torch.uint8, device=features.device)
         _check(self._lib.wn_condition(self._h, B, Tf, fp, int(T), cp, workspace.data_ptr(), workspace.numel(),
-                                      _stream_handle(stream)), "wn_condition")
+                                      _stream_handle(stream, features, cond, workspace)), "wn_condition")
         return cond
 
     def condition_static(self, features, T: int, cond, stream=None):
@@ -366,7 +374,7 @@ class Conditioner:
         B, Tf = int(features.shape[0]), int(features.shape[1])
         fp = _dev_ptr(features, torch.float32, (B, Tf, self.n_features), "features")
         cp = _dev_ptr(cond, torch.float32, (B, T, self.n_layers, 2 * self.r), "cond")
-        _check(self._lib.wn_condition_static(self._h, B, Tf, fp, int(T), cp, _stream_handle(stream)),
+        _check(self._lib.wn_condition_static(self._h, B, Tf, fp, int(T), cp, _stream_handle(stream, features, cond)),
                "wn_condition_static")
         return cond
 

@@ -258,3 +258,39 @@ def test_refused_memory_leaves_the_state(what):
     assert rc == wn.WN_EINVAL and what in net._lib.wn_last_error().decode()
     assert torch.equal(net.score(*rest, workspace=ws, reset=False), want)
     net.close()
+
+
+def test_generation_on_a_busy_stream_keeps_its_memory():
+    """Generation, teacher forcing, scoring and conditioning on a stream that is busy, with workspaces of their own: what they
+    need is not handed out when the call returns."""
+    import paper_1702_07825_amd as wn
+    w, net = _model(4, 16, 32)
+    g = np.random.default_rng(9)
+    cw = {k: (g.standard_normal(s) * 0.1).astype(np.float32) for k, s in
+          (("w1", (2, 96, 2, 20)), ("b1", (2, 96)), ("w2", (2, 192, 2, 64)), ("b2", (2, 192)))}
+    conditioner = wn.Conditioner(cw, 4, 16, 1, 60)
+
+    def inputs():
+        cond, y = _inputs(4, 16, 2, 100)
+        u = torch.rand((2, 100), generator=torch.Generator().manual_seed(10)).cuda()
+        return cond, y, u, torch.randn((2, 5, 20), generator=torch.Generator().manual_seed(11)).cuda()
+
+    calls = [lambda s, c, y, u, f: net.generate(c, u, stream=s), lambda s, c, y, u, f: net.teacher_force(c, y, stream=s),
+             lambda s, c, y, u, f: net.score(c, y, stream=s), lambda s, c, y, u, f: conditioner(f, 300, stream=s)]
+    for call in calls:
+        want = call(None, *inputs())
+        torch.cuda.synchronize()
+        tensors = inputs()
+        sizes = [t.shape for t in tensors]
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(100_000_000)
+        got = call(stream, *tensors)
+        del tensors
+        # (small numbers and zeros: harmless as a state, if they were to lie in one)
+        others = [torch.zeros(s, device="cuda") for s in sizes] + [torch.zeros(net.workspace_bytes(2), dtype=torch.uint8, device="cuda")]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        del others
+    net.close()
