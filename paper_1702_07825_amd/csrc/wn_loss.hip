@@ -14,8 +14,8 @@
 // lo = fp16(v - hi), which holds v to 2^-22 of itself or 2^-39 of the row's largest, and a product takes
 // hi hi + hi lo + lo hi (lo lo is below 2^-22 of it), summed in fp32.
 //
-// Up to kFewRows rows go to wn_few.hip, which is bound by reading w once (64 and 65 rows x 50021 classes x 777: forward 40
-// and 72 us in bf16, 74 and 135 in fp32).
+// Up to kFewRows rows go to wn_few.hip, which is bound by reading w once (64 and 65 rows x 50021 classes x 777: forward 42
+// and 70 us in bf16, 79 and 134 in fp32).
 #include "wn_few.h"
 
 namespace {
@@ -81,7 +81,7 @@ __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __built
 // matrix units at the clock that the card holds under them.  Measured, bf16: 8192 x 65536 outputs over 2048 with the
 // forward end 1.69 ms, 1.30 PFLOP/s (a plain library product of this shape 1.58 ms), dw of 65536 x 2048 over 8192 and
 // dx over pieces of 22016 classes 1.27 PFLOP/s (library 1.24); the matrix units are busy 55 % of the cycles at 2.1 GHz,
-// no LDS bank conflicts.  256 x 128 tiles with two blocks a CU, so that one's ends run beside the other's products,
+// on another card 66 % at 1.8, no LDS bank conflicts.  256 x 128 tiles with two blocks a CU, so that one's ends run beside the other's products,
 // reached 1.18 PFLOP/s where these reach 1.5 (their operands come from L2 half as often again).
 template <class T, bool SP, class End>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void product(const Product g, const End end) {
