@@ -70,9 +70,9 @@ size_t wn_loss_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V);
  *   dx    [N][D] out, or NULL if not wanted; 0 in rows without a target, whatever x, lse and g hold there
  *   dw    [V][D] out, or NULL;   db fp32 [V] out, or NULL (with b NULL it is the gradient at b = 0)
  * With dtype WN_BF16 q / g (dx) and q / max |g| (dw) enter the last two products rounded to bf16 (db sums q in
- * fp32); with WN_F32 as wn_loss takes its products, q / g in dw's held to 2^-22 of itself, to 2^-39 of its class's
- * largest (of 1 if a row targets the class) or to 2^-105, in dx's to 2^-22 of itself or to 2^-39.  Sizes and errors as wn_loss; all three outputs
- * NULL is an error.  N = 0: dw and db are zeroed.
+ * fp32); with WN_F32 as wn_loss takes its products, from 65 rows on with q / g in dw's held to 2^-22 of itself, to 2^-39
+ * of its class's largest (of 1 if a row targets the class) or to 2^-105, in dx's to 2^-22 of itself or to 2^-39.  Sizes
+ * and errors as wn_loss; all three outputs NULL is an error.  N = 0: dw and db are zeroed.
  */
 int wn_loss_backward(int32_t dtype, int32_t N, int32_t D, int32_t V, const void* x, const void* w, const float* b,
                      const int32_t* y, const float* lse, const float* g, void* dx, void* dw, float* db,

@@ -547,7 +547,8 @@ _CLIP_ARRAY = np.dtype({"names": ["g", "out", "n", "dtype"], "formats": [np.uint
 def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None, stream=None):
     """wn_clip: scales the tensors of ``grads`` so that the norm over all of them is at most max_norm, in
     place or into ``outs``; returns that norm before (float32 [], on the device).  Where it is not finite the
-    tensors are left as they are.  No two may share memory (a gradient that is listed twice is refused)."""
+    tensors are left as they are.  One that is written may not share memory with another (a gradient listed twice, in
+    place, is refused)."""
     import torch
     grads, lib = list(grads), load_library()
     if not grads:
