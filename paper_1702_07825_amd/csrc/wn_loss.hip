@@ -542,13 +542,13 @@ struct GradEnd {
   }
 };
 
-// dx and dw: out[b][a] (rows of D).
-template <class E>
+// dx and dw: out[b][a] (rows of D).  DW in fp32: operand B's scales change from tile to tile of k.
+template <class E, bool DW>
 struct OutEnd {
-  static constexpr bool kScaledByTile = sizeof(E) == 4;
+  static constexpr bool kScaledByTile = sizeof(E) == 4 && DW;
   int A, B;           // D, rows
   const int* ea;      // fp32: scales of operand A's rows; the product is acc 2^-(ea[a] + eb)
-  const int* eq;      // fp32 dw: eb of each tile of k, [tiles][B]; or null: kQScale
+  const int* eq;      // fp32 dw: eb of each tile of k, [tiles][B] (dx: kQScale)
   int tile;           // log2 of its chunks
   const int32_t* y;   // dx: rows whose y is outside 0 .. V-1 are 0; or null
   const float* g;     // dx: the row's factor; or null
@@ -561,7 +561,7 @@ struct OutEnd {
   // The sums before chunk c in the units of its tile, where it is the first of one.
   template <class T>
   __device__ __forceinline__ void to_chunk(f32x4 (&acc)[T::NA][T::NB], const Place& pl, int c) const {
-    if (!eq || c & ((1 << tile) - 1)) return;
+    if (c & ((1 << tile) - 1)) return;
     const int* now = eq + (size_t)(c >> tile) * B;
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
@@ -576,7 +576,7 @@ struct OutEnd {
     if constexpr (sizeof(E) == 4) {
       int eb[T::NB];
 #pragma unroll
-      for (int j = 0; j < T::NB; ++j) eb[j] = eq ? eq[(size_t)(pl.last >> tile) * B + min(pl.b0 + 16 * j + pl.n, B - 1)] : kQScale;
+      for (int j = 0; j < T::NB; ++j) eb[j] = kScaledByTile ? eq[(size_t)(pl.last >> tile) * B + min(pl.b0 + 16 * j + pl.n, B - 1)] : kQScale;
 #pragma unroll
       for (int i = 0; i < T::NA; ++i)
 #pragma unroll
@@ -1206,13 +1206,13 @@ int run_backward(int N, int D, int V, const E* x, const E* w, const float* b, co
     if (e == hipSuccess && dx) {
       const Operand owt = cols_operand(wv, n, D, RowFactor{nullptr, nullptr, 0}, units(f.wt), floats(f.cmax), ints(f.ewt), st);
       const bool whole = f.piece == V && f.dxs.splits == 1;
-      const OutEnd<E> o{D, N, ints(f.ewt), nullptr, 0, y, g, nullptr, 0, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
+      const OutEnd<E, false> o{D, N, ints(f.ewt), nullptr, 0, y, g, nullptr, 0, V, whole ? nullptr : floats(f.dx), v0 > 0, dx};
       e = run_product<sp>({owt, {units(f.q), N, ldq, ldq}, 0, 0, f.dxs.splits, 0}, f.dxs.big, o, st);
       if (e == hipSuccess && !whole && v0 + n == V) e = join(floats(f.dx), f.dxs.splits, (size_t)N * D, dx, st);
     }
     if (e == hipSuccess && dw) {
       E* const out = dw + (size_t)v0 * D;
-      const OutEnd<E> o{D, n, ints(f.ext), sp ? ints(f.eq) : nullptr, big ? 3 : 2, nullptr, nullptr, gmax, gparts, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
+      const OutEnd<E, true> o{D, n, ints(f.ext), sp ? ints(f.eq) : nullptr, big ? 3 : 2, nullptr, nullptr, gmax, gparts, 1, f.dws.splits == 1 ? nullptr : floats(f.dw), 0, out};
       e = run_product<sp>({oxt, {units(f.qt), n, ldqt, ldqt}, 0, 0, f.dws.splits, 0}, f.dws.big, o, st);
       if (e == hipSuccess && f.dws.splits > 1) e = join(floats(f.dw), f.dws.splits, (size_t)n * D, out, st);
     }
