@@ -1,6 +1,7 @@
 /*
  * wn_train.h -- C ABI of libwn's operators at the ends of a training step on an
  * AMD Instinct MI355X (gfx950): the loss of an output layer and its gradients,
+ * log probabilities with entropies and alternatives and their gradients,
  * an embedding and its gradient, and the clip of all gradients.
  *
  * A voice's two ends (the embedding of the samples before, and the softmax over
@@ -80,6 +81,44 @@ int wn_loss_backward(int32_t dtype, int32_t N, int32_t D, int32_t V, const void*
 
 /* Bytes of workspace wn_loss_backward needs, whichever outputs are wanted (0 for sizes out of range). */
 size_t wn_loss_backward_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V);
+
+/*
+ * Log probabilities of given tokens under an output layer (l and lse as in wn_loss), the entropies of the rows'
+ * distributions p[n][v] = exp(l[n][v] - lse[n]), and the `top` likeliest classes of each, without keeping the logits:
+ *   logprob[n] = l[n][y[n]] - lse[n],  entropy[n] = lse[n] - sum_v p[n][v] l[n][v]
+ *   y             int32 [N]; a row whose y is outside 0 .. V-1 has no token: its logprob is 0 (the rest is as of any row)
+ *   logprob, entropy, lse   fp32 [N] out
+ *   top_ids       int32 [N][top] out, the classes of the largest logits in falling order, of equal ones the lowest first;
+ *   top_logprobs  fp32 [N][top] out, their log probabilities.  Both may be NULL where top is 0.
+ * The alternatives' logits are summed in 64 bits, so classes closer to each other than the other logits' rounding are in
+ * order; one that that rounding moves behind more than two others (and one more for each 8 of top) in other groups of 8
+ * classes may be missed.  A class of bias -inf is masked: it adds nothing to the entropy and is an alternative (of log
+ * probability -inf) only where fewer than top are left.  If every class is masked, or a logit is NaN or +inf, the row's logprob,
+ * entropy, lse and top_logprobs are NaN or infinite and its top_ids any classes.
+ * Sizes and errors as wn_loss; top 0 .. 32 and at most V.
+ */
+int wn_logprobs(int32_t dtype, int32_t N, int32_t D, int32_t V, int32_t top, const void* x, const void* w, const float* b,
+                const int32_t* y, float* logprob, float* entropy, float* lse, int32_t* top_ids, float* top_logprobs,
+                void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace wn_logprobs needs (0 for sizes out of range or N = 0). */
+size_t wn_logprobs_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V, int32_t top);
+
+/*
+ * Gradients of sum_n g[n] logprob[n] + h[n] entropy[n] over the rows with a token (of wn_logprobs with the same x, w, b and
+ * y, whose lse and entropy this takes):
+ *   q[n][v] = g[n] ([v = y[n]] - p[n][v]) - h[n] p[n][v] (log p[n][v] + entropy[n]), 0 in rows without a token
+ *   dx, dw, db  from q as in wn_loss_backward
+ *   g, h        fp32 [N] upstream gradients; either may be NULL (all 0)
+ * With c[n] = max(|g[n]|, |h[n]|), q / c enters the last two products as q / g does in wn_loss_backward, but for one bit:
+ * its fp16 parts for dx are held to 2^-38.  Sizes, NULL outputs and errors as there.
+ */
+int wn_logprobs_backward(int32_t dtype, int32_t N, int32_t D, int32_t V, const void* x, const void* w, const float* b,
+                         const int32_t* y, const float* lse, const float* entropy, const float* g, const float* h, void* dx,
+                         void* dw, float* db, void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace wn_logprobs_backward needs, whichever outputs are wanted (0 for sizes out of range). */
+size_t wn_logprobs_backward_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int32_t V);
 
 /*
  * Embedding: out[n][k] = scale * table[t[n]][k], rounded once to dtype; a row whose token is outside

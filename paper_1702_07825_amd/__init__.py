@@ -27,9 +27,12 @@ EXPORTED = ("wn_create", "wn_workspace_bytes", "wn_generate", "wn_generate_sampl
             "wn_abort", "wn_kernel_variant", "wn_launch_info", "wn_destroy", "wn_error_string", "wn_last_error",
             "wn_cond_create", "wn_cond_workspace_bytes", "wn_condition", "wn_condition_static", "wn_cond_destroy",
             "wn_loss", "wn_loss_workspace_bytes", "wn_loss_backward", "wn_loss_backward_workspace_bytes",
+            "wn_logprobs", "wn_logprobs_workspace_bytes", "wn_logprobs_backward", "wn_logprobs_backward_workspace_bytes",
             "wn_embed", "wn_embed_backward", "wn_embed_backward_workspace_bytes", "wn_clip", "wn_clip_workspace_bytes")
 # WN_COND_SCRATCH_BYTES of include/wn_cond.h: the largest scratch wn_condition_static takes
 COND_SCRATCH_BYTES = 64 << 20
+# the most alternatives that wn_logprobs gives (include/wn_train.h)
+TOP_MAX = 32
 # wn_sample_mode_t: how a step's distribution becomes its sample
 SAMPLE_DIRECT, SAMPLE_TEMPERATURE, SAMPLE_TOPK, SAMPLE_MODE, SAMPLE_MEAN = 0, 1, 2, 3, 4
 
@@ -111,6 +114,14 @@ def load_library(path: str = LIB_PATH):
         L.wn_loss_backward.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.wn_loss_backward_workspace_bytes.restype = sz
         L.wn_loss_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.wn_logprobs.restype = ctypes.c_int
+        L.wn_logprobs.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.wn_logprobs_workspace_bytes.restype = sz
+        L.wn_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.wn_logprobs_backward.restype = ctypes.c_int
+        L.wn_logprobs_backward.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.wn_logprobs_backward_workspace_bytes.restype = sz
+        L.wn_logprobs_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.wn_embed.restype = ctypes.c_int
         L.wn_embed.argtypes = [i32, i32, i32, i32, vp, vp, f32, vp, vp]
         L.wn_embed_backward.restype = ctypes.c_int
@@ -486,6 +497,11 @@ def head_loss(x, w, y, b=None, loss=None, lse=None, workspace=None, stream=None)
     return loss, lse
 
 
+def _check_need(need):
+    if not need or any(k not in ("dx", "dw", "db") for k in need):
+        raise ValueError("need must name some of dx, dw, db, got %r" % (need,))
+
+
 def head_loss_backward(x, w, y, lse, grad, b=None, need=("dx", "dw", "db"), dx=None, dw=None, db=None, workspace=None,
                        stream=None):
     """wn_loss_backward: gradients of (grad * loss).sum() for ``need`` of x, w and b -> (dx, dw, db), None
@@ -493,8 +509,7 @@ def head_loss_backward(x, w, y, lse, grad, b=None, need=("dx", "dw", "db"), dx=N
     import torch
     dt, lib = _train_dtype(x, "x"), load_library()
     (N, D), (V, _) = _matrix(x, "x"), _matrix(w, "w")
-    if not need or any(k not in ("dx", "dw", "db") for k in need):
-        raise ValueError("need must name some of dx, dw, db, got %r" % (need,))
+    _check_need(need)
     on = _On(x, stream)
     xp, wp = on.ptr(x, x.dtype, (N, D), "x"), on.ptr(w, x.dtype, (V, D), "w")
     yp, sp = on.ptr(y, torch.int32, (N,), "y"), on.ptr(lse, torch.float32, (N,), "lse")
@@ -506,6 +521,60 @@ def head_loss_backward(x, w, y, lse, grad, b=None, need=("dx", "dw", "db"), dx=N
     ws, wsp, wsn = on.workspace(workspace, lib.wn_loss_backward_workspace_bytes(dt, N, D, V))
     _check(lib.wn_loss_backward(dt, N, D, V, xp, wp, bp, yp, sp, gp, dxp, dwp, dbp, wsp, wsn, on.handle),
            "wn_loss_backward")
+    return dx, dw, db
+
+
+def head_logprobs(x, w, y, b=None, top: int = 0, logprob=None, entropy=None, lse=None, top_ids=None, top_logprobs=None,
+                  workspace=None, stream=None):
+    """wn_logprobs: x [N, D], w [V, D], y int32 [N], b float32 [V] or None -> (logprob, entropy, lse, top_ids, top_logprobs):
+    float32 [N], of the ``top`` likeliest classes int32 and float32 [N, top]; the last two None with top 0."""
+    import torch
+    dt, lib = _train_dtype(x, "x"), load_library()
+    (N, D), (V, _), top = _matrix(x, "x"), _matrix(w, "w"), _i32(top, "top")
+    if not 0 <= top <= min(TOP_MAX, V):
+        raise ValueError("top must be 0..%d and at most the classes, got %d" % (TOP_MAX, top))
+    if not top and (top_ids is not None or top_logprobs is not None):
+        raise ValueError("top_ids and top_logprobs are given, but top is 0")
+    on = _On(x, stream)
+    xp, wp = on.ptr(x, x.dtype, (N, D), "x"), on.ptr(w, x.dtype, (V, D), "w")
+    yp = on.ptr(y, torch.int32, (N,), "y")
+    bp = None if b is None else on.ptr(b, torch.float32, (V,), "b")
+    logprob, pp = on.out(logprob, (N,), torch.float32, "logprob")
+    entropy, ep = on.out(entropy, (N,), torch.float32, "entropy")
+    lse, sp = on.out(lse, (N,), torch.float32, "lse")
+    ip = tp = None
+    if top:
+        top_ids, ip = on.out(top_ids, (N, top), torch.int32, "top_ids")
+        top_logprobs, tp = on.out(top_logprobs, (N, top), torch.float32, "top_logprobs")
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_logprobs_workspace_bytes(dt, N, D, V, top))
+    _check(lib.wn_logprobs(dt, N, D, V, top, xp, wp, bp, yp, pp, ep, sp, ip, tp, wsp, wsn, on.handle), "wn_logprobs")
+    return logprob, entropy, lse, top_ids, top_logprobs
+
+
+def head_logprobs_backward(x, w, y, lse, entropy, grad=None, grad_entropy=None, b=None, need=("dx", "dw", "db"), dx=None, dw=None,
+                           db=None, workspace=None, stream=None):
+    """wn_logprobs_backward: gradients of (grad * logprob + grad_entropy * entropy).sum() over the rows with a token for
+    ``need`` of x, w and b -> (dx, dw, db), None where not needed.  lse, entropy: of head_logprobs on the same x, w, y and
+    b; grad, grad_entropy float32 [N], one of which may be None (0)."""
+    import torch
+    dt, lib = _train_dtype(x, "x"), load_library()
+    (N, D), (V, _) = _matrix(x, "x"), _matrix(w, "w")
+    _check_need(need)
+    if grad is None and grad_entropy is None:
+        raise ValueError("grad or grad_entropy must be given")
+    on = _On(x, stream)
+    xp, wp = on.ptr(x, x.dtype, (N, D), "x"), on.ptr(w, x.dtype, (V, D), "w")
+    yp, sp = on.ptr(y, torch.int32, (N,), "y"), on.ptr(lse, torch.float32, (N,), "lse")
+    ep = on.ptr(entropy, torch.float32, (N,), "entropy")
+    gp = None if grad is None else on.ptr(grad, torch.float32, (N,), "grad")
+    hp = None if grad_entropy is None else on.ptr(grad_entropy, torch.float32, (N,), "grad_entropy")
+    bp = None if b is None else on.ptr(b, torch.float32, (V,), "b")
+    dx, dxp = on.out(dx, (N, D), x.dtype, "dx") if "dx" in need else (None, None)
+    dw, dwp = on.out(dw, (V, D), x.dtype, "dw") if "dw" in need else (None, None)
+    db, dbp = on.out(db, (V,), torch.float32, "db") if "db" in need else (None, None)
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_logprobs_backward_workspace_bytes(dt, N, D, V))
+    _check(lib.wn_logprobs_backward(dt, N, D, V, xp, wp, bp, yp, sp, ep, gp, hp, dxp, dwp, dbp, wsp, wsn, on.handle),
+           "wn_logprobs_backward")
     return dx, dw, db
 
 

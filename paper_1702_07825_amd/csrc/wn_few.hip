@@ -12,51 +12,6 @@ namespace {
 
 using namespace wnt;
 
-typedef u16 u16x8u __attribute__((ext_vector_type(8), aligned(2)));
-typedef u16 u16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-
-// A 16-byte piece of a row: 8 bf16 or 4 fp32 values.
-template <class E>
-struct Piece;
-template <>
-struct Piece<u16> {
-  typedef u16x8 type;
-  typedef u16x8u any;
-  static constexpr int n = 8;
-};
-template <>
-struct Piece<float> {
-  typedef f32x4 type;
-  typedef f32x4u any;
-  static constexpr int n = 4;
-};
-template <class E>
-using P = typename Piece<E>::type;
-
-// Elements k .. of p, of which `left` exist (any number); the rest are 0.
-template <class E>
-__device__ __forceinline__ P<E> piece_at(const E* p, int left) {
-  constexpr int n = Piece<E>::n;
-  P<E> v;
-  if (left >= n) {
-    const typename Piece<E>::any x = *reinterpret_cast<const typename Piece<E>::any*>(p);
-#pragma unroll
-    for (int e = 0; e < n; ++e) v[e] = x[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < n; ++e) v[e] = e < left ? p[e] : (E)0;
-  }
-  return v;
-}
-template <class E>
-__device__ __forceinline__ P<E> whole_piece(const E* p) {
-  const typename Piece<E>::any x = *reinterpret_cast<const typename Piece<E>::any*>(p);
-  P<E> v;
-#pragma unroll
-  for (int e = 0; e < Piece<E>::n; ++e) v[e] = x[e];
-  return v;
-}
 template <class E>
 __device__ __forceinline__ P<E> no_piece() {
   P<E> v;
@@ -258,17 +213,69 @@ struct FewStats {
   }
 };
 
+// The same with the sum that the entropy takes, and the largest logit of every 8 classes: those of an even quad and the odd
+// one behind it.
+struct FewProbe {
+  float2* part;
+  float *spread, *target;
+  float* groups;  // [N][ceil(V / 8)], or null
+  template <int T, int NB>
+  __device__ void operator()(const WnFew& f, f32x4 (&acc)[T][NB], int v, int n, int quad, int wave) const {
+    __shared__ WnStat s[4][16 * NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int r = 16 * j + n;
+      const int y = r < f.N ? f.y[r] : -1;
+      float g[T];
+      WnStat o{-INFINITY, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        g[t] = fmaxf(fmaxf(acc[t][j][0], acc[t][j][1]), fmaxf(acc[t][j][2], acc[t][j][3]));
+        o.m = fmaxf(o.m, g[t]);
+      }
+      o.m = quads_max(o.m);
+      const float at = o.m == -INFINITY ? 0.f : o.m;
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        if (groups) {
+          const float m8 = fmaxf(g[t], __shfl_xor(g[t], 16, 64));
+          const int v8 = v + 16 * t;  // (an even quad's is a multiple of 8)
+          if (!(quad & 1) && r < f.N && v8 < f.V) groups[(size_t)r * ((f.V + 7) / 8) + v8 / 8] = m8;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o.count(acc[t][j][e], at);
+          if (y == v + 16 * t + e && y < f.V) target[r] = acc[t][j][e];
+        }
+      }
+      o.s = quads_sum(o.s);
+      o.t = quads_sum(o.t);
+      if (quad == 0) s[wave][r] = o;
+    }
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r >= f.N) return;
+    WnStat o = s[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) o.add(s[w][r]);
+    part[(size_t)blockIdx.x * f.N + r] = make_float2(o.m, o.s);
+    spread[(size_t)blockIdx.x * f.N + r] = o.t;
+  }
+};
+
 // q as the operand of dx ([n][v]; its rows take g where their parts are joined), q g / max |g| as that of dw ([v][n]), so
 // that rounding to bf16 leaves the targets' entries near -1 alone; and db, all of whose rows are here.
-template <class E>
+template <class E, bool ENT>
 struct FewGrad {
   const float *lse, *g;
   E *q, *qt;  // or null
   int vpad, npad;
   float* db;  // or null
+  WnTerms terms;  // ENT: of log probabilities and entropies
   template <int T, int NB>
   __device__ void operator()(const WnFew& f, f32x4 (&acc)[T][NB], int first, int n, int quad, int) const {
     float ln[NB], gn[NB], most = 0.f;
+    float an[NB], en[NB], hn[NB];
     int y[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -277,6 +284,11 @@ struct FewGrad {
       if (y[j] >= f.V) y[j] = -1;
       ln[j] = y[j] >= 0 ? lse[r] : 0.f;
       gn[j] = y[j] >= 0 ? g[r] : 0.f;
+      if constexpr (ENT) {
+        an[j] = y[j] >= 0 ? terms.target[r] : 0.f;
+        en[j] = y[j] >= 0 ? terms.spread[r] : 0.f;
+        hn[j] = y[j] >= 0 ? terms.entropy[r] : 0.f;
+      }
       most = fmaxf(most, fabsf(gn[j]));
     }
     most = row16_max(most);
@@ -290,7 +302,8 @@ struct FewGrad {
         f32x4 p;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = wnk::expf_fast(acc[t][j][e] - ln[j]) - (v + e == y[j] ? 1.f : 0.f);
+          if constexpr (ENT) p[e] = wn_spread(acc[t][j][e] - ln[j], an[j], en[j], hn[j]) + (v + e == y[j] ? an[j] : 0.f);
+          else p[e] = wnk::expf_fast(acc[t][j][e] - ln[j]) - (v + e == y[j] ? 1.f : 0.f);
           p[e] = y[j] >= 0 && v + e < f.V ? p[e] : 0.f;
         }
         sum += p * gn[j];
@@ -532,6 +545,15 @@ hipError_t wn_few_loss(const WnFew& f, float2* part, float* target, hipStream_t 
   return hipGetLastError();
 }
 
+template <class E>
+hipError_t wn_few_probe(const WnFew& f, float2* part, float* spread, float* target, float* groups, hipStream_t st) {
+  by_tiles(wn_few_tiles(sizeof(E) == 4, f.N, f.D, f.V), [&](auto nb) {
+    const FewProbe end{part, spread, target, groups};
+    launch_logits<E, decltype(nb)::value>(f, f.V, end, st);
+  });
+  return hipGetLastError();
+}
+
 WnFewPlan wn_few_plan(bool f32, int N, int D, int V) {
   WnFewPlan p;
   const int step = f32 ? 16 : 32, e = f32 ? 4 : 2, slab = f32 ? 64 : 128;
@@ -549,11 +571,17 @@ WnFewPlan wn_few_plan(bool f32, int N, int D, int V) {
 }
 
 template <class E>
-hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, const float* g, bool dx, void* dw, float* db, void* q,
-                        void* qt, float* sum, hipStream_t st) {
-  const FewGrad<E> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad, p.npad, db};
-  by_tiles(wn_few_tiles(sizeof(E) == 4, f.N, f.D, f.V),
-           [&](auto nb) { launch_logits<E, decltype(nb)::value>(f, p.vpad, end, st); });  // (q holds zeros behind V)
+hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, const float* g, const WnTerms* terms, bool dx, void* dw,
+                        float* db, void* q, void* qt, float* sum, hipStream_t st) {
+  by_tiles(wn_few_tiles(sizeof(E) == 4, f.N, f.D, f.V), [&](auto nb) {
+    auto grads = [&](auto ent) {
+      const FewGrad<E, decltype(ent)::value> end{lse, g, dx ? static_cast<E*>(q) : nullptr, dw ? static_cast<E*>(qt) : nullptr, p.vpad,
+                                                 p.npad, db, terms ? *terms : WnTerms{}};
+      launch_logits<E, decltype(nb)::value>(f, p.vpad, end, st);  // (q holds zeros behind V)
+    };
+    if (terms) grads(std::true_type{});
+    else grads(std::false_type{});
+  });
   by_tiles(f.N <= 16 ? 1 : f.N <= 32 ? 2 : 4, [&](auto nb) {
     constexpr int NB = decltype(nb)::value, W = Piece<E>::n;
     if (dx)
@@ -568,7 +596,9 @@ hipError_t wn_few_grads(const WnFew& f, const WnFewPlan& p, const float* lse, co
 
 template hipError_t wn_few_loss<float>(const WnFew&, float2*, float*, hipStream_t);
 template hipError_t wn_few_loss<u16>(const WnFew&, float2*, float*, hipStream_t);
-template hipError_t wn_few_grads<float>(const WnFew&, const WnFewPlan&, const float*, const float*, bool, void*, float*, void*, void*,
-                                        float*, hipStream_t);
-template hipError_t wn_few_grads<u16>(const WnFew&, const WnFewPlan&, const float*, const float*, bool, void*, float*, void*, void*,
-                                      float*, hipStream_t);
+template hipError_t wn_few_probe<float>(const WnFew&, float2*, float*, float*, float*, hipStream_t);
+template hipError_t wn_few_probe<u16>(const WnFew&, float2*, float*, float*, float*, hipStream_t);
+template hipError_t wn_few_grads<float>(const WnFew&, const WnFewPlan&, const float*, const float*, const WnTerms*, bool, void*, float*,
+                                        void*, void*, float*, hipStream_t);
+template hipError_t wn_few_grads<u16>(const WnFew&, const WnFewPlan&, const float*, const float*, const WnTerms*, bool, void*, float*,
+                                      void*, void*, float*, hipStream_t);
