@@ -2,7 +2,8 @@
  * wn_train.h -- C ABI of libwn's operators at the ends of a training step on an
  * AMD Instinct MI355X (gfx950): the loss of an output layer and its gradients,
  * log probabilities with entropies and alternatives and their gradients,
- * an embedding and its gradient, and the clip of all gradients.
+ * an embedding and its gradient, the clip of all gradients, and updates orthogonalised by
+ * Newton-Schulz products.
  *
  * A voice's two ends (the embedding of the samples before, and the softmax over
  * the classes of the next one; Deep Voice, arXiv 1702.07825, Appendix A.1) run
@@ -15,7 +16,7 @@
  *  - All pointers are DEVICE pointers owned by the caller, all on one device, and
  *    arrays are dense and row-major.  They may start at any element; a workspace
  *    is 256-byte aligned.  No output overlaps an input or another output, except
- *    where wn_clip says so.
+ *    where wn_clip and wn_orthogonalize say so.
  *  - `dtype` (wn_dtype_t, WN_F32 or WN_BF16) is the type of the matrices: x, w,
  *    dx, dw, an embedding table and its rows.  Biases, losses, and upstream
  *    gradients of losses are fp32.  Every sum is in fp32 or wider.
@@ -169,6 +170,38 @@ int wn_clip(int32_t n_arrays, const wn_clip_array* arrays, float max_norm, float
 
 /* Bytes of workspace wn_clip needs, whatever the arrays. */
 size_t wn_clip_workspace_bytes(void);
+
+/* One matrix of wn_orthogonalize: rows x cols elements of dtype (WN_F32 or WN_BF16) at g; the update goes to out, which may
+ * be g itself.  Nothing else may overlap. */
+typedef struct {
+  const void* g;
+  void* out;
+  int32_t rows, cols;  /* 0 .. 2^18, their product at most 2^32; 0: g and out are not looked at */
+  int32_t dtype;
+  float scale;         /* finite */
+} wn_ortho_array;
+
+/*
+ * Updates orthogonalised by Newton-Schulz products, as the Muon optimizer takes them: every matrix G of `arrays` (a HOST
+ * array, read before the call returns) by itself
+ *   X = G / (norm + eps), norm its Frobenius norm (summed in fp64), transposed if rows > cols;
+ *   `steps` times, with (a, b, c) = coefficients[0], [1], [2] of the step:  A = X X',  X <- a X + (b A + c A A) X
+ *   out = scale X, transposed back
+ * coefficients is a HOST array [steps][3].  With (3.4445, -4.7750, 2.0315) five times the singular values of out / scale
+ * lie about 1 (0.7 to 1.2) where those of X were above 0.003 or so; any others may be given as long as no entry of a step's X, A or
+ * b A + c A A reaches 16, 16 or 64 in size (a matrix where one does ends up not finite).
+ * A zero matrix gives zeros; an infinity or NaN in a matrix makes its update NaN, and no other's.
+ * Products are summed in fp32: of WN_BF16 matrices X, A and b A + c A A are rounded to fp16 between products (2^-11 of a value, and
+ * 2^-37 to 2^-35), of WN_F32 ones held in two fp16 parts (2^-22) and three products of them taken for one.
+ * n_arrays 0 .. 2^16, steps 1 .. 64, eps finite and >= 0.
+ * Errors as wn_loss (of the arrays only the first one's memory is looked at), WN_EINVAL for arrays that overlap, and WN_ENOMEM.
+ */
+int wn_orthogonalize(int32_t n_arrays, const wn_ortho_array* arrays, int32_t steps, const float* coefficients, float eps,
+                     void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace wn_orthogonalize needs for arrays of these sizes and dtypes (0 for sizes out of range): about six times
+ * the arrays in 16 bits (fp32: twelve), of about a GiB of buffers at a time. */
+size_t wn_orthogonalize_workspace_bytes(int32_t n_arrays, const wn_ortho_array* arrays);
 
 #ifdef __cplusplus
 }

@@ -28,7 +28,8 @@ EXPORTED = ("wn_create", "wn_workspace_bytes", "wn_generate", "wn_generate_sampl
             "wn_cond_create", "wn_cond_workspace_bytes", "wn_condition", "wn_condition_static", "wn_cond_destroy",
             "wn_loss", "wn_loss_workspace_bytes", "wn_loss_backward", "wn_loss_backward_workspace_bytes",
             "wn_logprobs", "wn_logprobs_workspace_bytes", "wn_logprobs_backward", "wn_logprobs_backward_workspace_bytes",
-            "wn_embed", "wn_embed_backward", "wn_embed_backward_workspace_bytes", "wn_clip", "wn_clip_workspace_bytes")
+            "wn_embed", "wn_embed_backward", "wn_embed_backward_workspace_bytes", "wn_clip", "wn_clip_workspace_bytes",
+            "wn_orthogonalize", "wn_orthogonalize_workspace_bytes")
 # WN_COND_SCRATCH_BYTES of include/wn_cond.h: the largest scratch wn_condition_static takes
 COND_SCRATCH_BYTES = 64 << 20
 # the most alternatives that wn_logprobs gives (include/wn_train.h)
@@ -67,6 +68,11 @@ class CondWeights(ctypes.Structure):
 
 class ClipArray(ctypes.Structure):
     _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class OrthoArray(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 WEIGHT_FIELDS = ("embed", "b_embed", "w_prev", "w_cur", "b_gate", "w_res", "b_res", "w_skip", "b_skip",
@@ -132,6 +138,10 @@ def load_library(path: str = LIB_PATH):
         L.wn_clip.argtypes = [i32, ctypes.POINTER(ClipArray), f32, vp, vp, sz, vp]
         L.wn_clip_workspace_bytes.restype = sz
         L.wn_clip_workspace_bytes.argtypes = []
+        L.wn_orthogonalize.restype = ctypes.c_int
+        L.wn_orthogonalize.argtypes = [i32, ctypes.POINTER(OrthoArray), i32, ctypes.POINTER(f32), f32, vp, sz, vp]
+        L.wn_orthogonalize_workspace_bytes.restype = sz
+        L.wn_orthogonalize_workspace_bytes.argtypes = [i32, ctypes.POINTER(OrthoArray)]
         L.wn_teacher_force.restype = ctypes.c_int
         L.wn_teacher_force.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, vp]
         L.wn_teacher_features.restype = ctypes.c_int
@@ -608,9 +618,14 @@ def embed_backward(dout, tokens, V: int, scale: float = 1.0, dtable=None, worksp
     return dtable
 
 
-_CLIP_ARRAY = np.dtype({"names": ["g", "out", "n", "dtype"], "formats": [np.uint64, np.uint64, np.int64, np.int32],
-                        "offsets": [getattr(ClipArray, k).offset for k in ("g", "out", "n", "dtype")],
-                        "itemsize": ctypes.sizeof(ClipArray)})
+def _fields_of(struct, **formats):
+    """A numpy dtype of a ctypes structure."""
+    return np.dtype({"names": list(formats), "formats": list(formats.values()),
+                     "offsets": [getattr(struct, k).offset for k in formats], "itemsize": ctypes.sizeof(struct)})
+
+
+_CLIP_ARRAY = _fields_of(ClipArray, g=np.uint64, out=np.uint64, n=np.int64, dtype=np.int32)
+_ORTHO_ARRAY = _fields_of(OrthoArray, g=np.uint64, out=np.uint64, rows=np.int32, cols=np.int32, dtype=np.int32, scale=np.float32)
 
 
 def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None, stream=None):
@@ -654,3 +669,61 @@ def clip_gradients(grads, max_norm: float, outs=None, norm=None, workspace=None,
     ws, wsp, wsn = on.workspace(workspace, lib.wn_clip_workspace_bytes())
     _check(lib.wn_clip(n, arrays.ctypes.data_as(ctypes.POINTER(ClipArray)), float(max_norm), np_, wsp, wsn, on.handle), "wn_clip")
     return norm
+
+
+# five steps of the quintic with which the Muon optimizer is published
+MUON_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def orthogonalize(updates, scales=None, coefficients=MUON_COEFFICIENTS, eps: float = 1e-7, outs=None, workspace=None, stream=None):
+    """wn_orthogonalize: every matrix of ``updates`` by itself, X = G / (norm + eps) through a Newton-Schulz step
+    X <- a X + (b X X' + c (X X')^2) X for each (a, b, c) of ``coefficients``, times its entry of ``scales`` (a number: of
+    all; None: 1) -> ``outs`` (which may be ``updates`` themselves; new tensors if None).  One that is written may not share
+    memory with another."""
+    import torch
+    updates, lib = list(updates), load_library()
+    if not updates:
+        raise ValueError("updates is empty")
+    n = len(updates)
+    steps = np.ascontiguousarray(coefficients, dtype=np.float32)
+    if steps.ndim != 2 or steps.shape[1] != 3:
+        raise ValueError("coefficients must be three numbers for each step")
+    try:
+        dtypes = [t.dtype for t in updates]
+        shapes = [tuple(t.shape) for t in updates]
+        devices = {t.get_device() for t in updates}
+        dense = all([t.is_contiguous() for t in updates])
+    except AttributeError:
+        raise TypeError("updates must be torch tensors") from None
+    if not set(dtypes) <= {torch.float32, torch.bfloat16}:
+        raise ValueError("updates must be float32 or bfloat16")
+    if any([len(s) != 2 for s in shapes]):
+        raise ValueError("updates must have two dimensions")
+    if any([s[0] >= 1 << 31 or s[1] >= 1 << 31 for s in shapes]):
+        raise ValueError("an update is too large")
+    on = _On(updates[0], stream)
+    if devices != {on.device.index}:
+        raise ValueError("updates must all be on %s" % on.device)
+    if not dense:
+        raise ValueError("updates must be contiguous")
+    arrays = np.zeros(n, dtype=_ORTHO_ARRAY)
+    arrays["scale"] = 1.0 if scales is None else scales  # (numpy refuses a list of another length)
+    if outs is None:
+        outs = [on.empty(s, d) for s, d in zip(shapes, dtypes)]
+    else:
+        outs = list(outs)
+        if len(outs) != n:
+            raise ValueError("%d outs for %d updates" % (len(outs), n))
+        for t, s, d in zip(outs, shapes, dtypes):
+            on.ptr(t, d, s, "outs")
+    on.used(*updates)
+    arrays["g"] = [t.data_ptr() for t in updates]
+    arrays["out"] = [t.data_ptr() for t in outs]
+    arrays["rows"] = [s[0] for s in shapes]
+    arrays["cols"] = [s[1] for s in shapes]
+    arrays["dtype"] = [WN_F32 if d is torch.float32 else WN_BF16 for d in dtypes]
+    at = arrays.ctypes.data_as(ctypes.POINTER(OrthoArray))
+    ws, wsp, wsn = on.workspace(workspace, lib.wn_orthogonalize_workspace_bytes(n, at))
+    _check(lib.wn_orthogonalize(n, at, len(steps), steps.ctypes.data_as(ctypes.POINTER(ctypes.c_float)), float(eps), wsp, wsn, on.handle),
+           "wn_orthogonalize")
+    return outs

@@ -7,6 +7,8 @@
 #include <cstdint>
 #include <cstdio>
 #include <type_traits>
+#include <utility>
+#include <vector>
 
 #include "wn_train.h"
 #include "wn.h"
@@ -78,6 +80,31 @@ class ArrayScope {
   }
   int dev_ = -1, prev_ = -1;
 };
+
+// Whether an output (`out`) of a list of arrays overlaps another one, or an input (`g`) that it is not the whole of: blocks
+// would read what others have written.  bytes(array): its size, 0 of one that is not looked at.  Throws std::bad_alloc.
+template <class A, class Bytes>
+bool overlap(int n, const A* arrays, Bytes bytes) {
+  typedef std::pair<uintptr_t, uintptr_t> Span;
+  auto span = [&](const A& a, const void* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return Span(at, at + bytes(a));
+  };
+  std::vector<Span> outs;
+  outs.reserve(n);
+  for (int k = 0; k < n; ++k)
+    if (bytes(arrays[k])) outs.push_back(span(arrays[k], arrays[k].out));
+  if (!std::is_sorted(outs.begin(), outs.end())) std::sort(outs.begin(), outs.end());
+  for (size_t i = 1; i < outs.size(); ++i)
+    if (outs[i].first < outs[i - 1].second) return true;
+  for (int k = 0; k < n; ++k) {
+    if (!bytes(arrays[k]) || arrays[k].g == arrays[k].out) continue;
+    const Span g = span(arrays[k], arrays[k].g);
+    const auto after = std::lower_bound(outs.begin(), outs.end(), Span(g.second, 0));
+    if (after != outs.begin() && (after - 1)->second > g.first) return true;
+  }
+  return false;
+}
 
 inline int bad_workspace(const void* ws, size_t have, size_t need) {
   if (need == 0) return WN_OK;

@@ -15,8 +15,6 @@
 
 #include <cmath>
 #include <new>
-#include <utility>
-#include <vector>
 
 namespace {
 
@@ -196,30 +194,6 @@ __global__ __launch_bounds__(kThreads) void clip_scale(const Arrays a, const dou
   });
 }
 
-// Whether an output overlaps another one, or an input that it is not the whole of: blocks would read what others have
-// scaled.  Throws std::bad_alloc.
-bool overlap(int n, const wn_clip_array* arrays) {
-  typedef std::pair<uintptr_t, uintptr_t> Span;
-  auto span = [](const wn_clip_array& a, const void* p) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    return Span(at, at + (uintptr_t)a.n * (a.dtype == WN_BF16 ? 2 : 4));
-  };
-  std::vector<Span> outs;
-  outs.reserve(n);
-  for (int k = 0; k < n; ++k)
-    if (arrays[k].n) outs.push_back(span(arrays[k], arrays[k].out));
-  if (!std::is_sorted(outs.begin(), outs.end())) std::sort(outs.begin(), outs.end());
-  for (size_t i = 1; i < outs.size(); ++i)
-    if (outs[i].first < outs[i - 1].second) return true;
-  for (int k = 0; k < n; ++k) {
-    if (!arrays[k].n || arrays[k].g == arrays[k].out) continue;
-    const Span g = span(arrays[k], arrays[k].g);
-    const auto after = std::lower_bound(outs.begin(), outs.end(), Span(g.second, 0));
-    if (after != outs.begin() && (after - 1)->second > g.first) return true;
-  }
-  return false;
-}
-
 }  // namespace
 
 extern "C" {
@@ -246,7 +220,8 @@ int wn_clip(int32_t n_arrays, const wn_clip_array* arrays, float max_norm, float
     if (all > 1LL << 44) return wn_set_last_error(WN_EINVAL, "too many elements");
   }
   try {
-    if (overlap(n_arrays, arrays)) return wn_set_last_error(WN_EINVAL, "arrays overlap");
+    if (overlap(n_arrays, arrays, [](const wn_clip_array& a) { return (uintptr_t)a.n * (a.dtype == WN_BF16 ? 2 : 4); }))
+      return wn_set_last_error(WN_EINVAL, "arrays overlap");
   } catch (const std::bad_alloc&) {
     return wn_set_last_error(WN_ENOMEM, "out of host memory");
   }

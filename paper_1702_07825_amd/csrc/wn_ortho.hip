@@ -1,0 +1,576 @@
+// Updates orthogonalised by Newton-Schulz products (gfx950).  Declarations and contracts are in include/wn_train.h.
+//
+// Each matrix is X [m][n] with m <= n (a taller one transposed), its Frobenius norm at most 1.  A step is
+//   A = X X',  B = b A + c A A,  X <- a X + B X
+// three products of 16-bit operands on wn_product.h's tiles, all matrices of a call in one launch each.  A and B are symmetric:
+// their tiles on one side of the diagonal are computed and stored twice.  Both operands of a product lie along its sum, so
+// X is kept in both orders (the end of a step writes both).
+//
+// Values are held as fp16 of a power of two times themselves (kX, kA, kB): no entry exceeds its matrix's largest singular
+// value, which starts at 1 or below and stays near 1.2 with the usual coefficients, so one scale serves all entries, and what
+// fp16 cuts off (2^-37 of 1) is nothing beside the products' own rounding.  Matrices of bf16 take one fp16 value (2^-11 of
+// itself, where their results are rounded to 2^-8), those of fp32 hi and lo parts and three products (2^-22).
+#include "wn_product.h"
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+namespace {
+
+constexpr int kX = 12, kA = 12, kB = 10;  // X 2^kX and so on are held: up to 16, 16 and 64
+constexpr int kMostSteps = 64, kMostSide = 1 << 18;
+constexpr long long kMostElements = 1LL << 32;
+constexpr size_t kGroupBytes = (size_t)1 << 30;  // of the matrices that go through the steps together
+
+using Tiny = Tile<64, 64, 2, 2>;
+
+struct Matrix {
+  const void* g;
+  void* out;
+  u16 *x, *xt[2], *a, *b;  // X [m][ldn], its transpose [n][ldm] of this step and the next, A and B [m][ldm]
+  int m, n, ldm, ldn;      // m <= n; units from row to row
+  int tall;                // g is X transposed
+  float scale;
+  int chunk0, chunks;      // of the array's elements, for its norm
+  long long chunk;         // elements of one
+  int pack0, sym0, step0;  // first blocks of the packing, of the products that give A and B, and of the one that gives X
+  int packs, syms, steps;
+};
+// Matrices of a group, in the workspace; of[block] says which matrix a block of a phase works on.
+struct Group {
+  Matrix* matrices;
+  double* squares;
+  int *of_chunk, *of_pack, *of_sym, *of_step;
+};
+constexpr int kBatch = 20;
+struct Batch {
+  Matrix m[kBatch];
+  int first;
+};
+static_assert(sizeof(Batch) < 3900, "kernel arguments");
+
+// A block for each matrix of a batch.
+__global__ __launch_bounds__(256) void put_matrices(const Batch batch, const Group g) {
+  const Matrix& m = batch.m[blockIdx.x];
+  const int at = batch.first + blockIdx.x;
+  if (threadIdx.x == 0) g.matrices[at] = m;
+  for (int k = threadIdx.x; k < m.chunks; k += 256) g.of_chunk[m.chunk0 + k] = at;
+  for (int k = threadIdx.x; k < m.packs; k += 256) g.of_pack[m.pack0 + k] = at;
+  for (int k = threadIdx.x; k < m.syms; k += 256) g.of_sym[m.sym0 + k] = at;
+  for (int k = threadIdx.x; k < m.steps; k += 256) g.of_step[m.step0 + k] = at;
+}
+
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double s[4];
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// Squares in 64 bits: fp32 values neither overflow nor vanish.  A block for each chunk of a matrix.
+template <class E>
+__global__ __launch_bounds__(256) void squares(const Group g) {
+  const Matrix& m = g.matrices[g.of_chunk[blockIdx.x]];
+  const long long all = (long long)m.m * m.n, at = (blockIdx.x - m.chunk0) * m.chunk, end = at + m.chunk < all ? at + m.chunk : all;
+  constexpr int W = Piece<E>::n;
+  const E* p = static_cast<const E*>(m.g);
+  double sum[2] = {0.0, 0.0};
+  for (long long i = at + threadIdx.x * W; i < end; i += 256 * W) {
+    const P<E> v = piece_at(p + i, (int)(end - i < W ? end - i : W));
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const double d = value(v[e]);
+      sum[e & 1] += d * d;
+    }
+  }
+  const double s = block_sum(sum[0] + sum[1]);
+  if (threadIdx.x == 0) g.squares[blockIdx.x] = s;
+}
+
+// Four values to place k of a row (a multiple of 4), times 2^kX where they are of X.
+template <bool SP>
+__device__ __forceinline__ void put4(u16* row, int k, f32x4 v) {
+  if constexpr (SP) {
+    put_split(row, k, v);
+  } else {
+    u16 h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __builtin_bit_cast(u16, (_Float16)v[e]);
+    *reinterpret_cast<u32x2*>(row + k) = u32x2{(unsigned)h[0] | (unsigned)h[1] << 16, (unsigned)h[2] | (unsigned)h[3] << 16};
+  }
+}
+template <bool SP>
+__device__ __forceinline__ f32x4 get4(const u16* row, int k) {
+  const u16* p = SP ? row + k / 32 * kChunk + k % 32 : row + k;
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  const f16x4 hi = *reinterpret_cast<const f16x4*>(p);
+  f32x4 v{(float)hi[0], (float)hi[1], (float)hi[2], (float)hi[3]};
+  if constexpr (SP) {
+    const f16x4 lo = *reinterpret_cast<const f16x4*>(p + 32);
+    v += f32x4{(float)lo[0], (float)lo[1], (float)lo[2], (float)lo[3]};
+  }
+  return v;
+}
+template <bool SP>
+__device__ __forceinline__ int values_of(int units) { return SP ? units / 2 : units; }
+
+// X = G / (|G| + eps) in both orders, 64 x 64 values per block; zeros behind a row's values.
+template <class E>
+__global__ __launch_bounds__(256) void pack(const Group g, double eps) {
+  constexpr bool SP = sizeof(E) == 4;
+  __shared__ float s[64][65];
+  const Matrix& m = g.matrices[g.of_pack[blockIdx.x]];
+  double sum = 0.0;
+  for (int k = threadIdx.x; k < m.chunks; k += 256) sum += g.squares[m.chunk0 + k];
+  const double norm = sqrt(block_sum(sum)) + eps, f = norm != 0.0 ? (1 << kX) / norm : 0.0;
+  const int rows = m.tall ? m.n : m.m, cols = m.tall ? m.m : m.n, wide = (cols + 63) / 64, t = blockIdx.x - m.pack0;
+  const int r0 = t / wide * 64, c0 = t % wide * 64, tid = threadIdx.x;
+  const E* p = static_cast<const E*>(m.g);
+  u16* const as = m.tall ? m.xt[0] : m.x;
+  u16* const across = m.tall ? m.x : m.xt[0];
+  const int lda = m.tall ? m.ldm : m.ldn, ldc = m.tall ? m.ldn : m.ldm;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int i = 16 * h + (tid >> 4), c = 4 * (tid & 15), r = r0 + i;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    if (r < rows) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c0 + c + e < cols) v[e] = (float)((double)value(p[(size_t)r * cols + c0 + c + e]) * f);
+      if (c0 + c < values_of<SP>(lda)) put4<SP>(as + (size_t)r * lda, c0 + c, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[i][c + e] = v[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int i = 16 * h + (tid >> 4), c = 4 * (tid & 15);
+    if (c0 + i < cols && r0 + c < values_of<SP>(ldc))
+      put4<SP>(across + (size_t)(c0 + i) * ldc, r0 + c, f32x4{s[c][i], s[c + 1][i], s[c + 2][i], s[c + 3][i]});
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Products
+// ------------------------------------------------------------------------------------------------
+enum Phase { kGram, kPoly, kStep, kLast };
+
+// rows[b][a] and cols[a][b] = alpha (sum) + beta with[b][a], in the units of their operands.
+template <bool SP>
+struct Keep {
+  static constexpr bool kScaledByTile = false;
+  float alpha, beta;
+  const u16* with;  // [B][ldr], or null
+  u16 *rows, *cols;  // cols: null on the diagonal of a symmetric product
+  int A, B, ldr, ldc;
+  template <class T>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
+    constexpr int RA = 16 * T::NA, kPer = SP ? 2 : T::NB;  // the wave's a; tiles of b that go through LDS together
+    constexpr int kBytes = SP ? 128 : 32 * T::NB, kPieces = kBytes / 16;
+    static_assert(T::NB % kPer == 0 && T::kWaves * RA * kBytes <= T::kLds, "the transposed tile");
+    char* const tr = lds + (pl.wa * T::WB + pl.wb) * RA * kBytes;
+    const int lane = threadIdx.x & 63;
+    const bool odd = lane & 1;
+    auto place = [](int v, int piece) { return v * kBytes + ((piece ^ (v >> 1 & (kPieces - 1))) << 4); };
+    // Two lanes that hold neighbouring rows of b (n even, n + 1) swap two of their four values: the even lane then holds
+    // values 0 and 1 of both, the odd one 2 and 3, and each writes pairs.
+    auto put_pair = [&](int i, int col, const u16 (&v)[4]) {
+      const unsigned lo = (unsigned)v[0] | (unsigned)v[1] << 16, hi = (unsigned)v[2] | (unsigned)v[3] << 16;
+      const unsigned give = odd ? lo : hi, keep = odd ? hi : lo;
+      const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give, 0xB1, 0xf, 0xf, false);
+      const unsigned e = odd ? got : keep, o = odd ? keep : got;
+      const int r = 16 * i + 4 * pl.quad + (odd ? 2 : 0);
+      *reinterpret_cast<unsigned*>(tr + place(r, col >> 3) + (col & 7) * 2) = (e & 0xffffu) | o << 16;
+      *reinterpret_cast<unsigned*>(tr + place(r + 1, col >> 3) + (col & 7) * 2) = e >> 16 | (o & 0xffff0000u);
+    };
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      const int b = pl.b0 + 16 * j + pl.n;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) {
+        const int a = pl.a0 + 16 * i + 4 * pl.quad;
+        const bool in = b < B && a < values_of<SP>(ldr);
+        f32x4 v = acc[i][j] * alpha;
+        if (with && in) v += get4<SP>(with + (size_t)b * ldr, a) * beta;
+        u16 hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (SP) split(v[e], hi[e], lo[e]);
+          else hi[e] = __builtin_bit_cast(u16, (_Float16)v[e]);
+        }
+        if (in) {
+          u16* d = rows + (size_t)b * ldr + (SP ? a / 32 * kChunk + a % 32 : a);
+          *reinterpret_cast<u32x2*>(d) = u32x2{(unsigned)hi[0] | (unsigned)hi[1] << 16, (unsigned)hi[2] | (unsigned)hi[3] << 16};
+          if constexpr (SP)
+            *reinterpret_cast<u32x2*>(d + 32) = u32x2{(unsigned)lo[0] | (unsigned)lo[1] << 16, (unsigned)lo[2] | (unsigned)lo[3] << 16};
+        }
+        if (cols) {
+          put_pair(i, 16 * (j % kPer) + (pl.n & ~1), hi);
+          if constexpr (SP) put_pair(i, 32 + 16 * (j % kPer) + (pl.n & ~1), lo);
+        }
+      }
+      if (j % kPer != kPer - 1 || !cols) continue;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own part of LDS)
+      const int unit0 = SP ? (pl.b0 + 16 * (j - 1)) * 2 : pl.b0;
+      constexpr int kRows = 64 / kPieces;
+#pragma unroll 4
+      for (int k = 0; k < RA / kRows; ++k) {
+        const int r = kRows * k + lane / kPieces, a = pl.a0 + r, piece = lane % kPieces;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(tr + place(r, piece));
+        if (a < A && unit0 + 8 * piece < ldc) *reinterpret_cast<u32x4*>(cols + (size_t)a * ldc + unit0 + 8 * piece) = x;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+};
+
+// out[b][a] = alpha (sum) + beta with[b][a].
+template <class E>
+struct Result {
+  static constexpr bool kScaledByTile = false;
+  float alpha, beta;
+  const u16* with;  // [B][ldw]
+  E* out;           // [B][A]
+  int A, B, ldw;
+  template <class T>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char*) const {
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      const int b = pl.b0 + 16 * j + pl.n;
+      if (b >= B) continue;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) {
+        const int a = pl.a0 + 16 * i + 4 * pl.quad;
+        if (a >= A) continue;
+        const f32x4 v = acc[i][j] * alpha + get4<sizeof(E) == 4>(with + (size_t)b * ldw, a) * beta;
+        E* d = out + (size_t)b * A + a;
+        if (a + 3 < A) {
+          if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(d) = f32x4u{v[0], v[1], v[2], v[3]};
+          else *reinterpret_cast<u16x4u*>(d) = u16x4u{bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3])};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (a + e < A) put(d + e, v[e]);
+        }
+      }
+    }
+  }
+};
+
+struct Step {
+  float a, b, c;
+  int phase, now;  // now: which of xt is this step's
+};
+
+// Blocks of all matrices of a group.  Each XCD takes a run of them (block b runs on XCD b mod 8), so that the tiles it works
+// on at a time share the operands' rows in its L2.
+template <class T, class E>
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group g, const Step s) {
+  constexpr bool SP = sizeof(E) == 4;
+  extern __shared__ __align__(16) char lds[];
+  const int blocks = gridDim.x, xcd = blockIdx.x & 7, per = blocks >> 3, rem = blocks & 7;
+  const int block = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
+  const bool sym = s.phase <= kPoly;
+  const Matrix& m = g.matrices[(sym ? g.of_sym : g.of_step)[block]];
+  Place pl;
+  Operand oa, ob;
+  if (sym) {
+    const int t = block - m.sym0;
+    int i = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+    while (i * (i + 1) / 2 > t) --i;
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    pl.tb = i;
+    pl.ta = t - i * (i + 1) / 2;
+    oa = s.phase == kGram ? Operand{m.x, m.m, m.ldn, m.ldn} : Operand{m.a, m.m, m.ldm, m.ldm};
+    ob = oa;
+  } else {
+    oa = {m.xt[s.now], m.n, m.ldm, m.ldm};
+    ob = {m.b, m.m, m.ldm, m.ldm};
+    if (s.phase == kLast && m.tall) {
+      const Operand o = oa;
+      oa = ob;
+      ob = o;
+    }
+    const int ta = (int)((oa.rows + T::TA - 1) / T::TA), tb = (int)((ob.rows + T::TB - 1) / T::TB), t = block - m.step0;
+    const int band = t / (kBand * ta), in = t - band * kBand * ta, wide = min(kBand, tb - band * kBand);
+    pl.ta = in / wide;
+    pl.tb = band * kBand + in - pl.ta * wide;
+  }
+  pl.in_tile<T>();
+  f32x4 acc[T::NA][T::NB];
+  auto exp2i = [](int e) { return __uint_as_float((unsigned)(127 + e) << 23); };
+  if (s.phase == kLast) {
+    const Result<E> end{m.scale * exp2i(-kB - kX), s.a * m.scale * exp2i(-kX), m.tall ? m.xt[s.now] : m.x, static_cast<E*>(m.out),
+                        (int)oa.rows, (int)ob.rows, m.tall ? m.ldm : m.ldn};
+    tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
+    end.template operator()<T>(acc, pl, lds);
+    return;
+  }
+  Keep<SP> end{};
+  end.A = (int)oa.rows;
+  end.B = (int)ob.rows;
+  if (s.phase == kGram) {
+    end.alpha = exp2i(kA - 2 * kX);
+    end.rows = m.a;
+    end.ldr = end.ldc = m.ldm;
+  } else if (s.phase == kPoly) {
+    end.alpha = s.c * exp2i(kB - 2 * kA);
+    end.beta = s.b * exp2i(kB - kA);
+    end.with = m.a;
+    end.rows = m.b;
+    end.ldr = end.ldc = m.ldm;
+  } else {
+    end.alpha = exp2i(-kB);
+    end.beta = s.a;
+    end.with = m.x;
+    end.rows = m.x;
+    end.cols = m.xt[s.now ^ 1];
+    end.ldr = m.ldn;
+    end.ldc = m.ldm;
+  }
+  if (sym && pl.ta != pl.tb) end.cols = end.rows;
+  tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
+  end.template operator()<T>(acc, pl, lds);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Host
+// ------------------------------------------------------------------------------------------------
+struct Sides {
+  int m, n, ldm, ldn;
+  bool tall;
+  Sides(const wn_ortho_array& a) : m(std::min(a.rows, a.cols)), n(std::max(a.rows, a.cols)), tall(a.rows > a.cols) {
+    ldm = padded_units(m, a.dtype == WN_F32);
+    ldn = padded_units(n, a.dtype == WN_F32);
+  }
+  size_t bytes() const { return up256((size_t)m * ldn * 2) + 2 * up256((size_t)n * ldm * 2) + 2 * up256((size_t)m * ldm * 2); }
+};
+inline bool empty(const wn_ortho_array& a) { return a.rows == 0 || a.cols == 0; }
+
+// The tiles of a launch: by a model of its time.  A chunk of 256 x 256 outputs takes a CU 1.4 us (three products of fp16
+// parts: 2.1), of 128 x 128 two blocks on a CU 1.2 us, of 64 x 64 four 0.9 us; a tile's start and end 8, 6 and 5 us.
+constexpr int kTileSides[3] = {256, 128, 64};
+struct Plan {
+  double sum[3] = {0, 0, 0}, longest[3] = {0, 0, 0}, blocks[3] = {0, 0, 0};
+  void add(int k, double tiles, int units, bool sp) {
+    static const double kChunkUs[3] = {1.4, 1.2, 0.9}, kEnds[3] = {8.0, 6.0, 5.0};
+    const double us = units / kChunk * kChunkUs[k] * (sp ? 1.5 : 1.0) + kEnds[k];
+    sum[k] += tiles * us;
+    blocks[k] += tiles;
+    longest[k] = std::max(longest[k], us);
+  }
+  int best() const {
+    static const double kRoom[3] = {256, 512, 1024};
+    int at = 0;
+    double least = 1e300;
+    for (int k = 0; k < 3; ++k) {
+      const double us = blocks[k] <= kRoom[k] ? longest[k] : sum[k] / kRoom[k] + longest[k] / 2;
+      if (us < least) least = us, at = k;
+    }
+    return at;
+  }
+};
+inline double side_tiles(int v, int k) { return (double)ceil_div(v, kTileSides[k]); }
+
+// The arrays of one dtype that go together: from `at` on, until their buffers fill kGroupBytes.
+struct GroupPlan {
+  std::vector<int> arrays;
+  int sym = 0, step = 0;  // tiles
+  long long chunks = 0, packs = 0, syms = 0, steps = 0;
+  size_t buffers = 0;
+  // Bytes of all: descriptors, indexes, sums and buffers.
+  size_t total() const {
+    return up256(arrays.size() * sizeof(Matrix)) + up256(chunks * 8) + up256(chunks * 4) + up256(packs * 4) + up256(syms * 4) +
+           up256(steps * 4) + buffers;
+  }
+};
+inline long long chunk_of(long long n) { return std::max<long long>(16384, (long long)ceil_div((size_t)n, 1024 * 8) * 8); }
+
+GroupPlan next_group(int n_arrays, const wn_ortho_array* arrays, int dtype, int& at) {
+  GroupPlan p;
+  Plan sym, step;
+  const bool sp = dtype == WN_F32;
+  for (; at < n_arrays; ++at) {
+    const wn_ortho_array& a = arrays[at];
+    if (a.dtype != dtype || empty(a)) continue;
+    const Sides s(a);
+    if (!p.arrays.empty() && p.buffers + s.bytes() > kGroupBytes) break;
+    p.arrays.push_back(at);
+    p.buffers += s.bytes();
+    for (int k = 0; k < 3; ++k) {
+      const double tm = side_tiles(s.m, k);
+      sym.add(k, tm * (tm + 1) / 2, s.ldn, sp);
+      sym.add(k, tm * (tm + 1) / 2, s.ldm, sp);
+      step.add(k, tm * side_tiles(s.n, k), s.ldm, sp);
+    }
+  }
+  p.sym = sym.best();
+  p.step = step.best();
+  for (int i : p.arrays) {
+    const Sides s(arrays[i]);
+    const long long tm = (long long)side_tiles(s.m, p.sym);
+    p.chunks += (long long)ceil_div((size_t)s.m * s.n, (size_t)chunk_of((long long)s.m * s.n));
+    p.packs += (long long)(ceil_div(s.m, 64) * ceil_div(s.n, 64));
+    p.syms += tm * (tm + 1) / 2;
+    p.steps += (long long)(side_tiles(s.m, p.step) * side_tiles(s.n, p.step));
+  }
+  return p;
+}
+
+template <class T, class E>
+hipError_t launch_newton(const Group& g, const Step& s, long long blocks, hipStream_t st) {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(newton<T, E>), hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((newton<T, E>), dim3((unsigned)blocks), dim3(T::kThreads), T::kLds, st, g, s);
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t run_group(const GroupPlan& p, const wn_ortho_array* arrays, int steps, const float* coefficients, float eps, char* ws,
+                     hipStream_t st) {
+  Carve c;
+  Group g;
+  g.matrices = reinterpret_cast<Matrix*>(ws + c.take(p.arrays.size() * sizeof(Matrix)));
+  g.squares = reinterpret_cast<double*>(ws + c.take(p.chunks * 8));
+  g.of_chunk = reinterpret_cast<int*>(ws + c.take(p.chunks * 4));
+  g.of_pack = reinterpret_cast<int*>(ws + c.take(p.packs * 4));
+  g.of_sym = reinterpret_cast<int*>(ws + c.take(p.syms * 4));
+  g.of_step = reinterpret_cast<int*>(ws + c.take(p.steps * 4));
+  int chunks = 0, packs = 0, syms = 0, products = 0;
+  Batch batch;
+  for (size_t at = 0; at < p.arrays.size();) {
+    batch.first = (int)at;
+    int n = 0;
+    for (; n < kBatch && at < p.arrays.size(); ++n, ++at) {
+      const wn_ortho_array& a = arrays[p.arrays[at]];
+      const Sides s(a);
+      Matrix& m = batch.m[n];
+      auto units = [&](int rows, int ld) { return reinterpret_cast<u16*>(ws + c.take((size_t)rows * ld * 2)); };
+      m.g = a.g;
+      m.out = a.out;
+      m.x = units(s.m, s.ldn);
+      m.xt[0] = units(s.n, s.ldm);
+      m.xt[1] = units(s.n, s.ldm);
+      m.a = units(s.m, s.ldm);
+      m.b = units(s.m, s.ldm);
+      m.m = s.m, m.n = s.n, m.ldm = s.ldm, m.ldn = s.ldn, m.tall = s.tall;
+      m.scale = a.scale;
+      const long long all = (long long)s.m * s.n;
+      m.chunk = chunk_of(all);
+      m.chunk0 = chunks, m.pack0 = packs, m.sym0 = syms, m.step0 = products;
+      m.chunks = (int)ceil_div((size_t)all, (size_t)m.chunk);
+      m.packs = (int)(ceil_div(s.m, 64) * ceil_div(s.n, 64));
+      const int tm = (int)side_tiles(s.m, p.sym);
+      m.syms = tm * (tm + 1) / 2;
+      m.steps = (int)(side_tiles(s.m, p.step) * side_tiles(s.n, p.step));
+      chunks += m.chunks, packs += m.packs, syms += m.syms, products += m.steps;
+    }
+    hipLaunchKernelGGL(put_matrices, dim3(n), dim3(256), 0, st, batch, g);
+  }
+  hipLaunchKernelGGL(squares<E>, dim3(chunks), dim3(256), 0, st, g);
+  hipLaunchKernelGGL(pack<E>, dim3(packs), dim3(256), 0, st, g, (double)eps);
+  hipError_t e = hipGetLastError();
+  auto launch = [&](int tile, const Step& s, long long blocks) {
+    if (e != hipSuccess) return;
+    e = tile == 0 ? launch_newton<Big, E>(g, s, blocks, st) : tile == 1 ? launch_newton<Small, E>(g, s, blocks, st) : launch_newton<Tiny, E>(g, s, blocks, st);
+  };
+  for (int k = 0; k < steps; ++k) {
+    Step s{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], kGram, k & 1};
+    launch(p.sym, s, p.syms);
+    s.phase = kPoly;
+    launch(p.sym, s, p.syms);
+    s.phase = k + 1 < steps ? kStep : kLast;
+    launch(p.step, s, p.steps);
+  }
+  return e;
+}
+
+int check_arrays(int n_arrays, const wn_ortho_array* arrays) {
+  if (n_arrays < 0 || n_arrays > 1 << 16) return wn_set_last_error(WN_EINVAL, "n_arrays must be 0..2^16");
+  if (n_arrays && !arrays) return wn_set_last_error(WN_EINVAL, "null pointer");
+  for (int k = 0; k < n_arrays; ++k) {
+    const wn_ortho_array& a = arrays[k];
+    const int rc = bad_dtype(a.dtype);
+    if (rc != WN_OK) return rc;
+    if (a.rows < 0 || a.rows > kMostSide || a.cols < 0 || a.cols > kMostSide || (long long)a.rows * a.cols > kMostElements)
+      return wn_set_last_error(WN_EINVAL, "an array's rows and cols must be 0..2^18, their product at most 2^32");
+  }
+  return WN_OK;
+}
+
+// Of all groups, which share it one after the other.  Throws std::bad_alloc.
+size_t workspace_bytes(int n_arrays, const wn_ortho_array* arrays) {
+  size_t most = 0;
+  for (int dtype : {WN_F32, WN_BF16})
+    for (int at = 0; at < n_arrays;) {
+      const GroupPlan p = next_group(n_arrays, arrays, dtype, at);
+      if (!p.arrays.empty()) most = std::max(most, p.total());
+    }
+  return most;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wn_orthogonalize_workspace_bytes(int32_t n_arrays, const wn_ortho_array* arrays) {
+  if (check_arrays(n_arrays, arrays) != WN_OK) return 0;
+  try {
+    return workspace_bytes(n_arrays, arrays);
+  } catch (const std::bad_alloc&) {
+    return 0;
+  }
+}
+
+int wn_orthogonalize(int32_t n_arrays, const wn_ortho_array* arrays, int32_t steps, const float* coefficients, float eps,
+                     void* workspace, size_t ws_bytes, void* stream) {
+  wn_clear_last_error();
+  int rc = check_arrays(n_arrays, arrays);
+  if (rc != WN_OK) return rc;
+  if (steps < 1 || steps > kMostSteps) return wn_set_last_error(WN_EINVAL, "steps must be 1..64");
+  if (!coefficients) return wn_set_last_error(WN_EINVAL, "null pointer");
+  for (int k = 0; k < 3 * steps; ++k)
+    if (!std::isfinite(coefficients[k])) return wn_set_last_error(WN_EINVAL, "coefficients must be finite");
+  if (!(eps >= 0.f) || std::isinf(eps)) return wn_set_last_error(WN_EINVAL, "eps must be finite and >= 0");
+  const wn_ortho_array* first = nullptr;
+  for (int k = 0; k < n_arrays; ++k) {
+    const wn_ortho_array& a = arrays[k];
+    if (empty(a)) continue;
+    if (!first) first = &a;
+    if (!a.g || !a.out) return wn_set_last_error(WN_EINVAL, "null pointer");
+    const uintptr_t size = a.dtype == WN_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(a.g) % size || reinterpret_cast<uintptr_t>(a.out) % size)
+      return wn_set_last_error(WN_EINVAL, "an array is not aligned to its elements");
+    if (!std::isfinite(a.scale)) return wn_set_last_error(WN_EINVAL, "scales must be finite");
+  }
+  if (!first) return WN_OK;
+  try {
+    if (overlap(n_arrays, arrays, [](const wn_ortho_array& a) { return (uintptr_t)a.rows * a.cols * (a.dtype == WN_BF16 ? 2 : 4); }))
+      return wn_set_last_error(WN_EINVAL, "arrays overlap");
+    rc = bad_workspace(workspace, ws_bytes, workspace_bytes(n_arrays, arrays));
+    if (rc != WN_OK) return rc;
+    ArrayScope scope;
+    // (the first array stands for all, as in wn_clip)
+    if ((rc = scope.check(workspace, "workspace")) != WN_OK || (rc = scope.check(first->g, "g")) != WN_OK ||
+        (rc = scope.check(first->out, "out")) != WN_OK || (rc = scope.enter()) != WN_OK)
+      return rc;
+    char* const ws = static_cast<char*>(workspace);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    for (int dtype : {WN_F32, WN_BF16})
+      for (int at = 0; at < n_arrays;) {
+        const GroupPlan p = next_group(n_arrays, arrays, dtype, at);
+        if (p.arrays.empty()) continue;
+        const hipError_t e = dtype == WN_F32 ? run_group<float>(p, arrays, steps, coefficients, eps, ws, st)
+                                             : run_group<u16>(p, arrays, steps, coefficients, eps, ws, st);
+        if (e != hipSuccess) return wn_set_last_error(WN_EHIP, hipGetErrorString(e));
+      }
+  } catch (const std::bad_alloc&) {
+    return wn_set_last_error(WN_ENOMEM, "out of host memory");
+  }
+  return WN_OK;
+}
+
+}  // extern "C"
