@@ -89,13 +89,16 @@ struct RowOut {
   int N, V;
   float *logprob, *entropy, *lse;
   float* log_s;  // [N]
-  __device__ __forceinline__ void put(int n, const WnStat& o) const {
+  // (a block's first thread writes; the others get log s too)
+  __device__ __forceinline__ float put(int n, const WnStat& o, bool write = threadIdx.x == 0) const {
     const float z = logf(o.s);
+    if (!write) return z;
     const int t = y[n];
     lse[n] = o.m + z;
     logprob[n] = t >= 0 && t < V ? (target[n] - o.m) - z : 0.f;  // (in this order log s is not lost beside a large m)
     entropy[n] = z - o.t / o.s;
     log_s[n] = z;
+    return z;
   }
 };
 
@@ -113,25 +116,30 @@ __global__ __launch_bounds__(256) void join_probe(const float2* part, const floa
   __syncthreads();
   if (w || n >= r.N) return;
   for (int k = 1; k < 16; ++k) o.add(s[k][c]);
-  r.put(n, o);
+  r.put(n, o, true);
 }
 
-// The same for few rows: a block per row.
-__global__ __launch_bounds__(256) void join_probe_few(const float2* part, const float* spread, int tiles, const RowOut r) {
-  __shared__ WnStat s[4];
-  const int n = blockIdx.x;
+// A row's parts joined by a block; every thread gets them.
+template <int kThreads>
+__device__ __forceinline__ WnStat join_tiles(const float2* part, const float* spread, int tiles, int N, int n) {
+  __shared__ WnStat s[kThreads / 64];
   WnStat o{-INFINITY, 0.f, 0.f};
 #pragma unroll 4
-  for (int t = threadIdx.x; t < tiles; t += 256) {
-    const float2 p = part[(size_t)t * r.N + n];
-    o.add({p.x, p.y, spread[(size_t)t * r.N + n]});
+  for (int t = threadIdx.x; t < tiles; t += kThreads) {
+    const float2 p = part[(size_t)t * N + n];
+    o.add({p.x, p.y, spread[(size_t)t * N + n]});
   }
   for (int d = 32; d; d >>= 1) o.add({__shfl_xor(o.m, d, 64), __shfl_xor(o.s, d, 64), __shfl_xor(o.t, d, 64)});
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = o;
   __syncthreads();
-  if (threadIdx.x) return;
-  for (int w = 1; w < 4; ++w) o.add(s[w]);
-  r.put(n, o);
+  o = s[0];
+  for (int w = 1; w < kThreads / 64; ++w) o.add(s[w]);
+  return o;
+}
+
+// For few rows, without alternatives: a block per row.
+__global__ __launch_bounds__(256) void join_probe_few(const float2* part, const float* spread, int tiles, const RowOut r) {
+  r.put(blockIdx.x, join_tiles<256>(part, spread, tiles, r.N, blockIdx.x));
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -144,6 +152,8 @@ struct Group {
 constexpr int kNone = (1 << 24) - 1;  // (numbers of groups are compared as floats)
 static_assert(kMaxV / 8 < kNone, "groups");
 
+__device__ __forceinline__ bool before(const Group& a, const Group& b) { return a.v > b.v || (a.v == b.v && a.g < b.g); }
+
 // The `want` largest of a wave's R entries a lane, by value and then by the lower number: lane r ends with the r-th.
 template <int R>
 __device__ __forceinline__ Group largest_of(Group (&e)[R], int want) {
@@ -153,7 +163,7 @@ __device__ __forceinline__ Group largest_of(Group (&e)[R], int want) {
     Group b = e[0];
 #pragma unroll
     for (int k = 1; k < R; ++k)
-      if (e[k].v > b.v || (e[k].v == b.v && e[k].g < b.g)) b = e[k];
+      if (before(e[k], b)) b = e[k];
     const float top = wnk::wave_max(b.v);
     const int g = (int)-wnk::wave_max(b.v == top ? -(float)b.g : -(float)kNone);
     if (lane == r) mine = {top, g};
@@ -173,132 +183,243 @@ struct Alternatives {
   const float* log_s;   // [N]
   Group* list;          // [N][kept(top)] from piece to piece
   int seen, last;       // 0: list is empty; the last piece
+  const float2* part;   // few rows: a row's statistics are joined here; or null
+  const float* spread;
+  int tiles;
+  RowOut rows;
   int32_t* ids;         // [N][top]
   float* logprobs;
 };
 constexpr int kSegment = 16;  // groups a lane looks at together
+constexpr int kMostKept = kept(kMostTop);
 
-// The classes of the kept groups: their logits in 64 bits, a wave for each group; lane 8 c of a wave ends with class c's.
-template <class E>
-__device__ __forceinline__ double class_logit(const Alternatives& a, int n, int g) {
+// A wave's segment of up to 64 kSegment groups (v[k] of group first + 64 k + lane, `left` of them) joined with the list `mine`,
+// of which lane r holds the r-th largest.  The want-th largest of the lanes' largest values is one that at least want groups
+// reach, so only groups that reach it are looked at again: a few more than want, unless many are equal.
+__device__ __forceinline__ Group join_segment(const float (&v)[kSegment], int first, int left, Group mine, int want, Group* room) {
+  const int lane = threadIdx.x & 63;
+  float most = v[0];
+#pragma unroll
+  for (int k = 1; k < kSegment; ++k) most = fmaxf(most, v[k]);
+  // (numbers rise from segment to segment, so an equal value comes behind those kept)
+  const Group least{__shfl(mine.v, want - 1, 64), __shfl(mine.g, want - 1, 64)};
+  if (least.g != kNone && !__any(most > least.v)) return mine;
+  const int had = __popcll(__ballot(mine.g != kNone));
+  // the list, then the groups that reach t (with a full list: its least, while few do)
+  float t = least.v;
+  auto reach = [&]() {
+    int n = had;
+#pragma unroll
+    for (int k = 0; k < kSegment; ++k) n += __popcll(__ballot(v[k] >= t && k * 64 + lane < left));
+    return n;
+  };
+  int n = 65;
+  if (least.g != kNone) n = reach();
+  if (n > 64) {
+    for (int r = 0; r < want; ++r) {
+      t = wnk::wave_max(most);
+      if (lane == __ffsll(__ballot(most == t)) - 1) most = -INFINITY;
+    }
+    t = fmaxf(t, least.v);  // (-infinity without a full list)
+    n = reach();
+  }
+  if (n > 64) {  // (many equal ones, or many of one lane)
+    Group e[kSegment + 1];
+#pragma unroll
+    for (int k = 0; k < kSegment; ++k) e[k] = k * 64 + lane < left ? Group{v[k], first + k * 64 + lane} : Group{-INFINITY, kNone};
+    e[kSegment] = mine;
+    return largest_of(e, want);
+  }
+  if (mine.g != kNone) room[lane] = mine;
+  n = had;
+#pragma unroll
+  for (int k = 0; k < kSegment; ++k) {
+    const bool in = v[k] >= t && k * 64 + lane < left;
+    const unsigned long long all = __ballot(in);
+    if (in) room[n + __popcll(all & ((1ull << lane) - 1))] = {v[k], first + k * 64 + lane};
+    n += __popcll(all);
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own part of LDS)
+  const Group e = lane < n ? room[lane] : Group{-INFINITY, kNone};
+  int rank = 0;
+  for (int k = 0; k < n; ++k) {
+    const Group o{__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e.v), k)), __builtin_amdgcn_readlane(e.g, k)};
+    rank += before(o, e);
+  }
+  asm volatile("" ::: "memory");  // (every entry has been read)
+  if (lane < n && rank < want) room[rank] = e;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  return lane < want && lane < n ? room[lane] : Group{-INFINITY, kNone};
+}
+
+// C classes' logits, summed in S by a wave: lanes 64 / C c .. of it end with class v[c]'s.
+template <class E, class S, int C, int kAhead>
+__device__ __forceinline__ S class_logits(const Alternatives& a, int n, const int (&v)[C]) {
   constexpr int W = Piece<E>::n;
   const int lane = threadIdx.x & 63;
   const E* x = static_cast<const E*>(a.x) + (size_t)n * a.D;
-  const E* w = static_cast<const E*>(a.w) + (size_t)g * 8 * a.D;
-  double sum[8];
-  size_t row[8];
+  const E* w[C];
+  S sum[C];
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    sum[c] = 0.0;
-    row[c] = (size_t)min(c, a.V - 1 - g * 8) * a.D;  // (classes behind the last: the last again)
+  for (int c = 0; c < C; ++c) {
+    sum[c] = 0;
+    w[c] = static_cast<const E*>(a.w) + (size_t)v[c] * a.D;
   }
-  auto add = [&](const P<E>& xv, const P<E> (&wv)[8]) {
+  auto add = [&](const P<E>& xv, const P<E> (&wv)[C]) {
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      const double xd = value(xv[k]);
+      const S xs = value(xv[k]);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) sum[c] += xd * (double)value(wv[c][k]);
+      for (int c = 0; c < C; ++c) sum[c] += xs * (S)value(wv[c][k]);
     }
   };
   const int whole = a.D / (64 * W) * (64 * W);
+#pragma unroll kAhead
   for (int k = lane * W; k < whole; k += 64 * W) {
-    P<E> wv[8];
+    P<E> wv[C];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) wv[c] = whole_piece(w + row[c] + k);
+    for (int c = 0; c < C; ++c) wv[c] = whole_piece(w[c] + k);
     add(whole_piece(x + k), wv);
   }
   if (const int k = whole + lane * W; k < a.D) {
-    P<E> wv[8];
+    P<E> wv[C];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) wv[c] = piece_at(w + row[c] + k, a.D - k);
+    for (int c = 0; c < C; ++c) wv[c] = piece_at(w[c] + k, a.D - k);
     add(piece_at(x + k, a.D - k), wv);
   }
-  // halves of the lanes take halves of the classes, three times; then 8 lanes add up
+  // halves of the lanes take halves of the classes until each has one; then the lanes of a class add up
 #pragma unroll
-  for (int h = 4; h; h >>= 1) {
-    const bool up = lane & (h * 8);
+  for (int h = C / 2; h; h >>= 1) {
+    const int d = h * 64 / C;
+    const bool up = lane & d;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < C / 2; ++c)
       if (c < h) {
-        const double give = up ? sum[c] : sum[c + h], keep = up ? sum[c + h] : sum[c];
-        sum[c] = keep + __shfl_xor(give, h * 8, 64);
+        const S give = up ? sum[c] : sum[c + h], keep = up ? sum[c + h] : sum[c];
+        sum[c] = keep + __shfl_xor(give, d, 64);
       }
   }
-  double s = sum[0];
-  for (int d = 4; d; d >>= 1) s += __shfl_xor(s, d, 64);
-  const int v = g * 8 + (lane >> 3);
-  if (a.b && v < a.V) s += (double)a.b[v];
+  S s = sum[0];
+#pragma unroll
+  for (int d = 32 / C; d; d >>= 1) s += __shfl_xor(s, d, 64);
+  int mine = v[0];
+#pragma unroll
+  for (int c = 1; c < C; ++c) mine = lane / (64 / C) == c ? v[c] : mine;
+  if (a.b) s += (S)a.b[mine];
   return s;
 }
 
-// A block per row: each wave finds the largest groups of its segments, the first joins them; in the last piece the
-// waves compute their classes' logits, which are then ranked.
+// A block per row.  The waves find the largest groups of their segments, which are then joined; in the last piece they
+// compute the logits of these groups' classes in 32 bits, of which the largest, as many as groups, are computed in 64 and
+// ranked by counting.  For few rows the block joins its row's statistics first.
 template <class E, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void alternatives(const Alternatives a) {
-  __shared__ Group found[kWaves + 1][64];
-  __shared__ double logit[64 * 8];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = blockIdx.x, want = kept(a.top);
+__global__ __launch_bounds__(64 * kWaves, kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
+  constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
+  __shared__ Group found[(kWaves + 1) * kMostKept], best[kMostKept], room[kWaves][64];
+  __shared__ Group near[kMostKept * 8], pick[kMostKept];  // classes by their logits in 32 bits
+  __shared__ float top_of[kMostKept];
+  __shared__ double logit[kMostKept];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x, want = kept(a.top);
+  float z = 0.f;
+  if (a.part) z = a.rows.put(n, join_tiles<kThreads>(a.part, a.spread, a.tiles, a.N, n));
   const float* groups = a.groups + (size_t)n * a.count;
   Group mine{-INFINITY, kNone};
-  for (int s = wave * 64 * kSegment; s < a.count; s += kWaves * 64 * kSegment) {
-    Group e[kSegment + 1];
-    float most = -INFINITY;
+  for (int s = wave * 64 * kSegment; s < a.count; s += kThreads * kSegment) {
+    float v[kSegment];
 #pragma unroll
     for (int k = 0; k < kSegment; ++k) {
       const int i = s + k * 64 + lane;
-      const float v = i < a.count ? groups[i] : -INFINITY;
-      e[k] = {v == v ? v : -INFINITY, i < a.count ? a.first + i : kNone};  // (a NaN would be neither before nor behind another)
-      most = fmaxf(most, e[k].v);
+      v[k] = fmaxf(i < a.count ? groups[i] : -INFINITY, -INFINITY);  // (a NaN would be neither before nor behind another)
     }
-    // (numbers rise from segment to segment, so an equal value comes behind those kept)
-    const Group least{__shfl(mine.v, want - 1, 64), __shfl(mine.g, want - 1, 64)};
-    if (least.g != kNone && !__any(most > least.v)) continue;
-    e[kSegment] = mine;
-    mine = largest_of(e, want);
+    mine = join_segment(v, a.first + s, a.count - s, mine, want, room[wave]);
   }
-  found[wave][lane] = mine;
-  if (wave == 0) found[kWaves][lane] = a.seen && lane < want ? a.list[(size_t)n * want + lane] : Group{-INFINITY, kNone};
-  __syncthreads();
-  if (wave == 0) {
-    Group e[kWaves + 1];
-#pragma unroll
-    for (int k = 0; k <= kWaves; ++k) e[k] = found[k][lane];
-    mine = largest_of(e, want);
-    found[0][lane] = mine;
-    if (!a.last && lane < want) a.list[(size_t)n * want + lane] = mine;
+  if (a.count <= 64 * kSegment && !a.seen) {
+    if (tid < want) best[tid] = mine;
+  } else {
+    if (lane < want) found[wave * want + lane] = mine;
+    if (tid < want) {
+      found[kWaves * want + tid] = a.seen ? a.list[(size_t)n * want + tid] : Group{-INFINITY, kNone};
+      best[tid] = {-INFINITY, kNone};
+    }
+    __syncthreads();
+    const int all = (kWaves + 1) * want;
+    for (int i = tid; i < all; i += kThreads) {
+      const Group e = found[i];
+      int rank = 0;
+      for (int k = 0; k < all; ++k) rank += before(found[k], e);
+      if (e.g != kNone && rank < want) best[rank] = e;
+    }
   }
-  if (!a.last) return;
   __syncthreads();
+  if (!a.last) {
+    if (tid < want) a.list[(size_t)n * want + tid] = best[tid];
+    return;
+  }
   for (int k = wave; k < want; k += kWaves) {
-    const int g = found[0][k].g;
-    if (g == kNone) continue;
-    const double s = class_logit<E>(a, n, g);
-    if ((lane & 7) == 0) logit[k * 8 + (lane >> 3)] = s;
+    const int g = best[k].g, c = lane >> 3;
+    Group e{-INFINITY, kNone};
+    if (g != kNone) {
+      int v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = min(g * 8 + i, a.V - 1);
+      const float l = class_logits<E, float, 8, kAhead>(a, n, v);
+      if (g * 8 + c < a.V) e = {fmaxf(l, -INFINITY), g * 8 + c};
+    }
+    if ((lane & 7) == 0) near[k * 8 + c] = e;
+    const float m = wnk::wave_max(e.v);
+    if (lane == 0) top_of[k] = m;
   }
   __syncthreads();
-  const float z = a.log_s[n];
-  auto class_of = [&](int i) {  // or -1
-    const int g = found[0][i >> 3].g, v = g * 8 + (i & 7);
-    return g != kNone && v < a.V ? v : -1;
-  };
-  for (int i = threadIdx.x; i < want * 8; i += 64 * kWaves) {
-    const int v = class_of(i);
-    if (v < 0) continue;
-    const double l = logit[i], key = l == l ? l : -INFINITY;
-    int rank = 0;
-    double most = -INFINITY;
-    for (int k = 0; k < want * 8; ++k) {
-      const int o = class_of(k);
-      const double ol = logit[k], okey = ol == ol ? ol : -INFINITY;
-      rank += o >= 0 && (okey > key || (okey == key && o < v));
-      if (o >= 0) most = fmax(most, okey);
+  // the want largest of them reach the least of the groups' largest
+  int picked = 0;
+  if (wave == 0) {
+    const float t = -wnk::wave_max(lane < want ? -top_of[lane] : -INFINITY);
+    int m = 0;
+    for (int i = 0; i < want * 8; i += 64) {
+      const Group e = i + lane < want * 8 ? near[i + lane] : Group{-INFINITY, kNone};
+      const bool in = e.g != kNone && e.v >= t;
+      const unsigned long long all = __ballot(in);
+      asm volatile("" ::: "memory");
+      if (in) near[m + __popcll(all & ((1ull << lane) - 1))] = e;  // (never behind what is still to be read)
+      m += __popcll(all);
     }
-    if (rank < a.top) {
-      a.ids[(size_t)n * a.top + rank] = v;
-      // (the row's largest logit is taken off as it is here, not as the product rounded it: no log probability is above 0)
-      a.logprobs[(size_t)n * a.top + rank] = (float)((l - most) - (double)z);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    for (int i = lane; i < m; i += 64) {
+      const Group e = near[i];
+      int rank = 0;
+      for (int k = 0; k < m; ++k) rank += before(near[k], e);
+      if (rank < want) pick[rank] = e;
     }
+    picked = min(m, want);
+    if (lane == 0) top_of[0] = __int_as_float(picked);
   }
+  __syncthreads();
+  picked = __float_as_int(top_of[0]);
+  for (int k = wave * 4; k < picked; k += kWaves * 4) {
+    int v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pick[min(k + i, picked - 1)].g;
+    const double l = class_logits<E, double, 4, kAhead>(a, n, v);
+    if ((lane & 15) == 0 && k + (lane >> 4) < picked)
+      logit[k + (lane >> 4)] = l == l ? l : -INFINITY;  // (where a logit is a NaN, log s is, and so is what comes out)
+  }
+  __syncthreads();
+  if (tid >= picked) return;  // (of the first wave: it has a lane for each)
+  if (!a.part) z = a.log_s[n];
+  const int v = pick[tid].g;
+  const double l = logit[tid];
+  int rank = 0;
+  double most = -INFINITY;
+  for (int k = 0; k < picked; ++k) {
+    const int o = pick[k].g;
+    const double ol = logit[k];
+    rank += ol > l || (ol == l && o < v);
+    most = fmax(most, ol);
+  }
+  if (rank >= a.top) return;
+  a.ids[(size_t)n * a.top + rank] = v;
+  // (the row's largest logit is taken off as it is here, not as the product rounded it: no log probability is above 0)
+  a.logprobs[(size_t)n * a.top + rank] = (float)((l - most) - (double)z);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -336,12 +457,15 @@ struct Probe {
   }
 };
 
+// Waves of a row.  Few rows leave the chip empty, so a row takes many; many rows of few groups take one each, which has no
+// other to wait for.  Measured with 1, 4 and 8 waves (us beside the call without alternatives): 1 row x 32000 classes x
+// 2048, 5 alternatives 53, 22, 22 and 20 of them 124, 50, 51; 37 x 50021 x 777 in fp32, 20: 142, 59, 49; 300 x 32000 x 1024, 5: 49,
+// 25, 46; 1000 x 32000 x 1024, 20: 117, 95, 205; 4096 x 65536 x 1024, 8: 226, 184, 469; 16000 x 256 x 256 in fp32, 3: 56, 108, 455.
 template <class E>
 hipError_t launch_alternatives(const Alternatives& a, hipStream_t st) {
-  // one wave for each segment, or each kept group
-  const int waves = (int)std::max<size_t>(ceil_div(a.count, 64 * kSegment), a.last ? kept(a.top) : 1);
-  if (waves > 4) hipLaunchKernelGGL((alternatives<E, 8>), dim3(a.N), dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((alternatives<E, 4>), dim3(a.N), dim3(256), 0, st, a);
+  if (a.N <= 128) hipLaunchKernelGGL((alternatives<E, 8>), dim3(a.N), dim3(512), 0, st, a);
+  else if (a.N <= 2048 || a.count > 64 * kSegment) hipLaunchKernelGGL((alternatives<E, 4>), dim3(a.N), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((alternatives<E, 1>), dim3(a.N), dim3(64), 0, st, a);
   return hipGetLastError();
 }
 
@@ -365,16 +489,21 @@ int run_probe(const ProbeCall& c, const E* x, const E* w, char* ws, hipStream_t 
   float* const log_s = reinterpret_cast<float*>(ws + f.log_s);
   float* const groups = c.top ? reinterpret_cast<float*>(ws + f.groups) : nullptr;
   const RowOut rows{target, c.y, N, V, c.logprob, c.entropy, c.lse, log_s};
-  Alternatives alt{groups, 0, 0, N, D, V, c.top, x, w, c.b, log_s, reinterpret_cast<Group*>(ws + f.list), 0, 0, c.ids, c.top_logprobs};
+  Alternatives alt{groups, 0, 0, N, D, V, c.top, x, w, c.b, log_s, reinterpret_cast<Group*>(ws + f.list), 0, 0, nullptr, nullptr, 0, rows,
+                   c.ids, c.top_logprobs};
   if (N <= kFewRows) {
     hipError_t e = wn_few_probe<E>({N, D, V, x, w, c.b, c.y}, part, spread, target, groups, st);
-    if (e == hipSuccess) {
-      hipLaunchKernelGGL(join_probe_few, dim3(N), dim3(256), 0, st, part, spread, (int)ceil_div(V, wn_few_classes(sp, N, D, V)), rows);
+    const int tiles = (int)ceil_div(V, wn_few_classes(sp, N, D, V));
+    if (e == hipSuccess && !c.top) {
+      hipLaunchKernelGGL(join_probe_few, dim3(N), dim3(256), 0, st, part, spread, tiles, rows);
       e = hipGetLastError();
     }
     if (e == hipSuccess && c.top) {
       alt.count = (int)ceil_div(V, 8);
       alt.last = 1;
+      alt.part = part;
+      alt.spread = spread;
+      alt.tiles = tiles;
       e = launch_alternatives<E>(alt, st);
     }
     return e == hipSuccess ? WN_OK : wn_set_last_error(WN_EHIP, hipGetErrorString(e));
