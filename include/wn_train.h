@@ -200,7 +200,7 @@ int wn_orthogonalize(int32_t n_arrays, const wn_ortho_array* arrays, int32_t ste
                      void* workspace, size_t ws_bytes, void* stream);
 
 /* Bytes of workspace wn_orthogonalize needs for arrays of these sizes and dtypes (0 for sizes out of range): about six times
- * the arrays in 16 bits (fp32: twelve), of about a GiB of buffers at a time. */
+ * the arrays in 16 bits (fp32: twelve), of about 4 GiB of buffers at a time. */
 size_t wn_orthogonalize_workspace_bytes(int32_t n_arrays, const wn_ortho_array* arrays);
 
 #ifdef __cplusplus

@@ -24,7 +24,7 @@ __host__ __device__ constexpr int kept(int top) { return top + 2 + top / 8; }
 static_assert(kept(kMostTop) <= 64, "a lane for each");
 
 struct ProbeEnd {
-  static constexpr bool kScaledByTile = false;
+  static constexpr bool kScaledByTile = false, kStarts = false;
   Logits l;
   float2* part;    // [tiles of all pieces][N]: m and s
   float* spread;   // t

@@ -21,9 +21,10 @@ namespace {
 constexpr int kX = 12, kA = 12, kB = 10;  // X 2^kX and so on are held: up to 16, 16 and 64
 constexpr int kMostSteps = 64, kMostSide = 1 << 18;
 constexpr long long kMostElements = 1LL << 32;
-constexpr size_t kGroupBytes = (size_t)1 << 30;  // of the matrices that go through the steps together
+constexpr size_t kGroupBytes = (size_t)4 << 30;  // of the matrices that go through the steps together
 
-using Tiny = Tile<64, 64, 2, 2>;
+// (small products are a chain of a few chunks' loads: room for four)
+using Tiny = Tile<64, 64, 2, 2, 4>;
 
 struct Matrix {
   const void* g;
@@ -77,14 +78,23 @@ __global__ __launch_bounds__(256) void squares(const Group g) {
   constexpr int W = Piece<E>::n;
   const E* p = static_cast<const E*>(m.g);
   double sum[2] = {0.0, 0.0};
-  for (long long i = at + threadIdx.x * W; i < end; i += 256 * W) {
-    const P<E> v = piece_at(p + i, (int)(end - i < W ? end - i : W));
+  auto add = [&](const P<E>& v) {
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       const double d = value(v[e]);
       sum[e & 1] += d * d;
     }
+  };
+  constexpr int kAhead = 8;
+  long long i = at + threadIdx.x * W;
+  for (; i + 256 * W * (kAhead - 1) + W <= end; i += 256 * W * kAhead) {
+    P<E> v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v[k] = whole_piece(p + i + 256 * W * k);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) add(v[k]);
   }
+  for (; i < end; i += 256 * W) add(piece_at(p + i, (int)(end - i < W ? end - i : W)));
   const double s = block_sum(sum[0] + sum[1]);
   if (threadIdx.x == 0) g.squares[blockIdx.x] = s;
 }
@@ -131,25 +141,29 @@ __global__ __launch_bounds__(256) void pack(const Group g, double eps) {
   u16* const as = m.tall ? m.xt[0] : m.x;
   u16* const across = m.tall ? m.x : m.xt[0];
   const int lda = m.tall ? m.ldm : m.ldn, ldc = m.tall ? m.ldn : m.ldm;
+  // a thread has 16 values of a row, then of a column
+  const int i = tid >> 2, c = 16 * (tid & 3), r = r0 + i;
+  constexpr int W = Piece<E>::n;
+  f32x4 v[4];
+#pragma unroll
+  for (int h = 0; h < 16 / W; ++h) {
+    P<E> x{};
+    if (r < rows && c0 + c + W * h < cols) x = piece_at(p + (size_t)r * cols + c0 + c + W * h, cols - (c0 + c + W * h));
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[(W * h + e) / 4][e % 4] = (float)((double)value(x[e]) * f);  // (behind a row's values: zeros)
+  }
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
-    const int i = 16 * h + (tid >> 4), c = 4 * (tid & 15), r = r0 + i;
-    f32x4 v{0.f, 0.f, 0.f, 0.f};
-    if (r < rows) {
+    if (r < rows && c0 + c + 4 * h < values_of<SP>(lda)) put4<SP>(as + (size_t)r * lda, c0 + c + 4 * h, v[h]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c0 + c + e < cols) v[e] = (float)((double)value(p[(size_t)r * cols + c0 + c + e]) * f);
-      if (c0 + c < values_of<SP>(lda)) put4<SP>(as + (size_t)r * lda, c0 + c, v);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[i][c + e] = v[e];
+    for (int e = 0; e < 4; ++e) s[i][c + 4 * h + e] = v[h][e];
   }
   __syncthreads();
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
-    const int i = 16 * h + (tid >> 4), c = 4 * (tid & 15);
-    if (c0 + i < cols && r0 + c < values_of<SP>(ldc))
-      put4<SP>(across + (size_t)(c0 + i) * ldc, r0 + c, f32x4{s[c][i], s[c + 1][i], s[c + 2][i], s[c + 3][i]});
+    const int k = c + 4 * h;
+    if (c0 + i < cols && r0 + k < values_of<SP>(ldc))
+      put4<SP>(across + (size_t)(c0 + i) * ldc, r0 + k, f32x4{s[k][i], s[k + 1][i], s[k + 2][i], s[k + 3][i]});
   }
 }
 
@@ -158,14 +172,32 @@ __global__ __launch_bounds__(256) void pack(const Group g, double eps) {
 // ------------------------------------------------------------------------------------------------
 enum Phase { kGram, kPoly, kStep, kLast };
 
-// rows[b][a] and cols[a][b] = alpha (sum) + beta with[b][a], in the units of their operands.
+// The sums' first values: ratio from[b][a], or 0.  (Read while the first chunks are under way, not behind the last.)
+template <class T, bool SP>
+__device__ __forceinline__ void start_with(f32x4 (&acc)[T::NA][T::NB], const Place& pl, const u16* from, float ratio, int B, int ld) {
+#pragma unroll
+  for (int j = 0; j < T::NB; ++j) {
+    const int b = pl.b0 + 16 * j + pl.n;
+#pragma unroll
+    for (int i = 0; i < T::NA; ++i) {
+      const int a = pl.a0 + 16 * i + 4 * pl.quad;
+      acc[i][j] = from && b < B && a < values_of<SP>(ld) ? get4<SP>(from + (size_t)b * ld, a) * ratio : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+}
+
+// rows[b][a] and cols[a][b] = alpha (ratio from[b][a] + sum) + beta with[b][a], in the units of their operands.
 template <bool SP>
 struct Keep {
-  static constexpr bool kScaledByTile = false;
-  float alpha, beta;
-  const u16* with;  // [B][ldr], or null
-  u16 *rows, *cols;  // cols: null on the diagonal of a symmetric product
+  static constexpr bool kScaledByTile = false, kStarts = true;
+  float alpha, beta, ratio;
+  const u16 *with, *from;  // [B][ldr], or null
+  u16 *rows, *cols;        // cols: null on the diagonal of a symmetric product
   int A, B, ldr, ldc;
+  template <class T>
+  __device__ __forceinline__ void start(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
+    start_with<T, SP>(acc, pl, from, ratio, B, ldr);
+  }
   template <class T>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
     constexpr int RA = 16 * T::NA, kPer = SP ? 2 : T::NB;  // the wave's a; tiles of b that go through LDS together
@@ -227,14 +259,18 @@ struct Keep {
   }
 };
 
-// out[b][a] = alpha (sum) + beta with[b][a].
+// out[b][a] = alpha (ratio from[b][a] + sum).
 template <class E>
 struct Result {
-  static constexpr bool kScaledByTile = false;
-  float alpha, beta;
-  const u16* with;  // [B][ldw]
+  static constexpr bool kScaledByTile = false, kStarts = true;
+  float alpha, ratio;
+  const u16* from;  // [B][ld]
   E* out;           // [B][A]
-  int A, B, ldw;
+  int A, B, ld;
+  template <class T>
+  __device__ __forceinline__ void start(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
+    start_with<T, sizeof(E) == 4>(acc, pl, from, ratio, B, ld);
+  }
   template <class T>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char*) const {
 #pragma unroll
@@ -245,7 +281,7 @@ struct Result {
       for (int i = 0; i < T::NA; ++i) {
         const int a = pl.a0 + 16 * i + 4 * pl.quad;
         if (a >= A) continue;
-        const f32x4 v = acc[i][j] * alpha + get4<sizeof(E) == 4>(with + (size_t)b * ldw, a) * beta;
+        const f32x4 v = acc[i][j] * alpha;
         E* d = out + (size_t)b * A + a;
         if (a + 3 < A) {
           if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(d) = f32x4u{v[0], v[1], v[2], v[3]};
@@ -265,14 +301,42 @@ struct Step {
   int phase, now;  // now: which of xt is this step's
 };
 
-// Blocks of all matrices of a group.  Each XCD takes a run of them (block b runs on XCD b mod 8), so that the tiles it works
-// on at a time share the operands' rows in its L2.
+// The order of a launch's tiles: classes of matrices alike, those with the longest tiles first.  Each XCD (block b runs on XCD b
+// mod 8) takes an eighth of every class, one run of it: so the tiles it works on at a time share their operands' rows in its
+// L2, all XCDs have as much to do, and the last tiles are short.
+constexpr int kClasses = 16;
+struct Order {
+  int n;
+  int start[kClasses + 1];
+  __host__ __device__ static int share(int all, int xcd) { return (all >> 3) * xcd + ((all & 7) * xcd >> 3); }  // all * xcd / 8
+  // The tile of a block, or -1.
+  __device__ __forceinline__ int tile() const {
+    const int xcd = blockIdx.x & 7;
+    int k = blockIdx.x >> 3;
+    for (int c = 0; c < n; ++c) {
+      const int all = start[c + 1] - start[c], lo = share(all, xcd), many = share(all, xcd + 1) - lo;
+      if (k < many) return start[c] + lo + k;
+      k -= many;
+    }
+    return -1;
+  }
+  unsigned blocks() const {
+    int most = 0;
+    for (int x = 0; x < 8; ++x) {
+      int many = 0;
+      for (int c = 0; c < n; ++c) many += share(start[c + 1] - start[c], x + 1) - share(start[c + 1] - start[c], x);
+      most = std::max(most, many);
+    }
+    return 8u * most;
+  }
+};
+
 template <class T, class E>
-__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group g, const Step s) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group g, const Step s, const Order order) {
   constexpr bool SP = sizeof(E) == 4;
   extern __shared__ __align__(16) char lds[];
-  const int blocks = gridDim.x, xcd = blockIdx.x & 7, per = blocks >> 3, rem = blocks & 7;
-  const int block = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
+  const int block = order.tile();
+  if (block < 0) return;
   const bool sym = s.phase <= kPoly;
   const Matrix& m = g.matrices[(sym ? g.of_sym : g.of_step)[block]];
   Place pl;
@@ -303,7 +367,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group
   f32x4 acc[T::NA][T::NB];
   auto exp2i = [](int e) { return __uint_as_float((unsigned)(127 + e) << 23); };
   if (s.phase == kLast) {
-    const Result<E> end{m.scale * exp2i(-kB - kX), s.a * m.scale * exp2i(-kX), m.tall ? m.xt[s.now] : m.x, static_cast<E*>(m.out),
+    const Result<E> end{m.scale * exp2i(-kB - kX), s.a * exp2i(kB), m.tall ? m.xt[s.now] : m.x, static_cast<E*>(m.out),
                         (int)oa.rows, (int)ob.rows, m.tall ? m.ldm : m.ldn};
     tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
     end.template operator()<T>(acc, pl, lds);
@@ -324,8 +388,8 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group
     end.ldr = end.ldc = m.ldm;
   } else {
     end.alpha = exp2i(-kB);
-    end.beta = s.a;
-    end.with = m.x;
+    end.ratio = s.a * exp2i(kB);
+    end.from = m.x;
     end.rows = m.x;
     end.cols = m.xt[s.now ^ 1];
     end.ldr = m.ldn;
@@ -377,9 +441,10 @@ inline double side_tiles(int v, int k) { return (double)ceil_div(v, kTileSides[k
 
 // The arrays of one dtype that go together: from `at` on, until their buffers fill kGroupBytes.
 struct GroupPlan {
-  std::vector<int> arrays;
+  std::vector<int> arrays;  // those with the longest tiles first
   int sym = 0, step = 0;  // tiles
   long long chunks = 0, packs = 0, syms = 0, steps = 0;
+  Order sym_order{}, step_order{};
   size_t buffers = 0;
   // Bytes of all: descriptors, indexes, sums and buffers.
   size_t total() const {
@@ -409,22 +474,35 @@ GroupPlan next_group(int n_arrays, const wn_ortho_array* arrays, int dtype, int&
   }
   p.sym = sym.best();
   p.step = step.best();
+  std::sort(p.arrays.begin(), p.arrays.end(), [&](int i, int k) {
+    const Sides a(arrays[i]), b(arrays[k]);
+    return a.ldn + a.ldm != b.ldn + b.ldm ? a.ldn + a.ldm > b.ldn + b.ldm : a.ldn != b.ldn ? a.ldn > b.ldn : i < k;
+  });
+  int ldn = -1, ldm = -1;
   for (int i : p.arrays) {
     const Sides s(arrays[i]);
+    if ((s.ldn != ldn || s.ldm != ldm) && p.sym_order.n < kClasses) {
+      p.sym_order.start[p.sym_order.n++] = (int)p.syms;
+      p.step_order.start[p.step_order.n++] = (int)p.steps;
+      ldn = s.ldn;
+      ldm = s.ldm;
+    }
     const long long tm = (long long)side_tiles(s.m, p.sym);
     p.chunks += (long long)ceil_div((size_t)s.m * s.n, (size_t)chunk_of((long long)s.m * s.n));
     p.packs += (long long)(ceil_div(s.m, 64) * ceil_div(s.n, 64));
     p.syms += tm * (tm + 1) / 2;
     p.steps += (long long)(side_tiles(s.m, p.step) * side_tiles(s.n, p.step));
   }
+  p.sym_order.start[p.sym_order.n] = (int)p.syms;
+  p.step_order.start[p.step_order.n] = (int)p.steps;
   return p;
 }
 
 template <class T, class E>
-hipError_t launch_newton(const Group& g, const Step& s, long long blocks, hipStream_t st) {
+hipError_t launch_newton(const Group& g, const Step& s, const Order& order, hipStream_t st) {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(newton<T, E>), hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((newton<T, E>), dim3((unsigned)blocks), dim3(T::kThreads), T::kLds, st, g, s);
+  hipLaunchKernelGGL((newton<T, E>), dim3(order.blocks()), dim3(T::kThreads), T::kLds, st, g, s, order);
   return hipGetLastError();
 }
 
@@ -473,17 +551,17 @@ hipError_t run_group(const GroupPlan& p, const wn_ortho_array* arrays, int steps
   hipLaunchKernelGGL(squares<E>, dim3(chunks), dim3(256), 0, st, g);
   hipLaunchKernelGGL(pack<E>, dim3(packs), dim3(256), 0, st, g, (double)eps);
   hipError_t e = hipGetLastError();
-  auto launch = [&](int tile, const Step& s, long long blocks) {
+  auto launch = [&](int tile, const Step& s, const Order& o) {
     if (e != hipSuccess) return;
-    e = tile == 0 ? launch_newton<Big, E>(g, s, blocks, st) : tile == 1 ? launch_newton<Small, E>(g, s, blocks, st) : launch_newton<Tiny, E>(g, s, blocks, st);
+    e = tile == 0 ? launch_newton<Big, E>(g, s, o, st) : tile == 1 ? launch_newton<Small, E>(g, s, o, st) : launch_newton<Tiny, E>(g, s, o, st);
   };
   for (int k = 0; k < steps; ++k) {
     Step s{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], kGram, k & 1};
-    launch(p.sym, s, p.syms);
+    launch(p.sym, s, p.sym_order);
     s.phase = kPoly;
-    launch(p.sym, s, p.syms);
+    launch(p.sym, s, p.sym_order);
     s.phase = k + 1 < steps ? kStep : kLast;
-    launch(p.step, s, p.steps);
+    launch(p.step, s, p.step_order);
   }
   return e;
 }

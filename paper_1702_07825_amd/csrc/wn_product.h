@@ -34,14 +34,14 @@ struct Product {
 typedef __amdgpu_buffer_rsrc_t rsrc;
 typedef __attribute__((address_space(3))) void lds_void;
 
-// Tiles of TA x TB outputs by WA x WB waves.
-template <int TA_, int TB_, int WA_, int WB_>
+// Tiles of TA x TB outputs by WA x WB waves, with room in LDS for kStages chunks of both operands (a power of two).
+template <int TA_, int TB_, int WA_, int WB_, int kStages_ = 2>
 struct Tile {
-  static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_;
+  static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_, kStages = kStages_;
   static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves;
   static constexpr int NA = TA / WA / 16, NB = TB / WB / 16;  // 16 x 16 outputs of a wave
   static constexpr int kStage = (TA + TB) * kChunk * 2;        // bytes of a chunk of both operands
-  static constexpr int kLds = 2 * kStage;
+  static constexpr int kLds = kStages * kStage;
   static constexpr int IA = TA * 8 / kThreads, IB = TB * 8 / kThreads;  // 16-byte pieces of a chunk per thread
   static constexpr int kOccupancy = 2;  // waves of a SIMD
   static_assert(NB <= NA, "the order of the reads in product");
@@ -76,8 +76,9 @@ typedef u16 u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// The sums of chunks c0 .. c1 - 1 of a tile, in V8's type of 16-bit values (SP: hi and lo parts).  Operands go from memory
-// straight to LDS (two chunks of each), from there to registers half a chunk ahead of their products.
+// The sums of chunks c0 .. c1 - 1 of a tile, in V8's type of 16-bit values (SP: hi and lo parts), added to what `end` starts
+// with (kStarts) or to 0.  Operands go from memory straight to LDS (kStages chunks of each), from there to registers half a
+// chunk ahead of their products.
 template <class T, bool SP, class V8, class End>
 __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Operand& a, const Operand& b, const Place& pl, int c0, int c1,
                                           char* lds, const End& end) {
@@ -112,24 +113,35 @@ __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Oper
     for (int k = 0; k < kPieces; ++k)
       if (k * T::NA / kPieces == i) stage_piece(c, to, k);
   };
+  constexpr int S = T::kStages;
+  if (S > 2 || End::kStarts)
 #pragma unroll
-  for (int i = 0; i < T::NA; ++i)
+    for (int k = 0; k < S; ++k)
+      if (c0 + k < c1) stage(c0 + k, lds + k * T::kStage);
+  if constexpr (End::kStarts) {
+    end.template start<T>(acc, pl);
+  } else {
 #pragma unroll
-    for (int j = 0; j < T::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   const int ra = pl.wa * (T::TA / T::WA), rb = pl.wb * (T::TB / T::WB);
   const int sw = pl.n >> 1;
   const int fa = (ra + pl.n) * kChunk * 2, fb = (T::TA + rb + pl.n) * kChunk * 2;
   const int s0 = (pl.quad ^ sw) * 16, s1 = ((4 + pl.quad) ^ sw) * 16;
-  auto buffer = [&](int c) { return lds + ((c - c0) & 1) * T::kStage; };
+  auto buffer = [&](int c) { return lds + ((c - c0) & (S - 1)) * T::kStage; };
   auto get = [&](const char* at, int row, int s) { return *reinterpret_cast<const V8*>(at + row + s); };
   constexpr int kRow = 16 * kChunk * 2;
   // a chunk's first and second half of each operand's values (SP: hi and lo parts)
   V8 a0[T::NA], a1[T::NA], b0[T::NB], b1[T::NB];
   if (c0 < c1) {
-    stage(c0, buffer(c0));
-    if (c0 + 1 < c1) {
-      stage(c0 + 1, buffer(c0 + 1));
-      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(T::IA + T::IB) : "memory");
+    if (S == 2 && !End::kStarts) {
+      stage(c0, buffer(c0));
+      if (c0 + 1 < c1) stage(c0 + 1, buffer(c0 + 1));
+    }
+    if (c0 + S - 1 < c1) {
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"((S - 1) * kPieces) : "memory");
     } else {
       asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     }
@@ -157,12 +169,14 @@ __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Oper
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const bool more = c + 2 < c1;
+    // (of what is under way only the next chunk is waited for, while all buffers are in use)
+    if (S == 2 || c + S - 1 >= c1) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"((S - 2) * kPieces) : "memory");
+    const bool more = c + S < c1;
     at = buffer(c + 1);
     __builtin_amdgcn_s_setprio(1);
     if constexpr (SP) {
-      if (more) stage(c + 2, to);  // (spread over the products they spill)
+      if (more) stage(c + S, to);  // (spread over the products they spill)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
 #pragma unroll
@@ -180,7 +194,7 @@ __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Oper
     } else {
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
-        if (more) stage_part(c + 2, to, i);
+        if (more) stage_part(c + S, to, i);
         a0[i] = get(at, fa + i * kRow, s0);
         if (i < T::NB) b0[i] = get(at, fb + i * kRow, s0);
 #pragma unroll
