@@ -185,13 +185,13 @@ typedef struct {
  * Updates orthogonalised by Newton-Schulz products, as the Muon optimizer takes them: every matrix G of `arrays` (a HOST
  * array, read before the call returns) by itself
  *   X = G / (norm + eps), norm its Frobenius norm (summed in fp64), transposed if rows > cols;
- *   `steps` times, with (a, b, c) = coefficients[0], [1], [2] of the step:  A = X X',  X <- a X + (b A + c A A) X
+ *   `steps` times, with (a, b, c) = coefficients[0], [1], [2] of the step:  A = X X',  X <- (a I + b A + c A A) X
  *   out = scale X, transposed back
  * coefficients is a HOST array [steps][3].  With (3.4445, -4.7750, 2.0315) five times the singular values of out / scale
  * lie about 1 (0.7 to 1.2) where those of X were above 0.003 or so; any others may be given as long as no entry of a step's X, A or
- * b A + c A A reaches 16, 16 or 64 in size (a matrix where one does ends up not finite).
+ * a I + b A + c A A reaches 16, 16 or 64 in size (a matrix where one does ends up not finite).
  * A zero matrix gives zeros; an infinity or NaN in a matrix makes its update NaN, and no other's.
- * Products are summed in fp32: of WN_BF16 matrices X, A and b A + c A A are rounded to fp16 between products (2^-11 of a value, and
+ * Products are summed in fp32: of WN_BF16 matrices X, A and a I + b A + c A A are rounded to fp16 between products (2^-11 of a value, and
  * 2^-37 to 2^-35), of WN_F32 ones held in two fp16 parts (2^-22) and three products of them taken for one.
  * n_arrays 0 .. 2^16, steps 1 .. 64, eps finite and >= 0.
  * Errors as wn_loss (of the arrays only the first one's memory is looked at), WN_EINVAL for arrays that overlap, and WN_ENOMEM.

@@ -24,7 +24,7 @@ __host__ __device__ constexpr int kept(int top) { return top + 2 + top / 8; }
 static_assert(kept(kMostTop) <= 64, "a lane for each");
 
 struct ProbeEnd {
-  static constexpr bool kScaledByTile = false, kStarts = false;
+  static constexpr bool kScaledByTile = false;
   Logits l;
   float2* part;    // [tiles of all pieces][N]: m and s
   float* spread;   // t
@@ -313,7 +313,7 @@ __device__ __forceinline__ S class_logits(const Alternatives& a, int n, const in
 // compute the logits of these groups' classes in 32 bits, of which the largest, as many as groups, are computed in 64 and
 // ranked by counting.  For few rows the block joins its row's statistics first.
 template <class E, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
+__global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
   constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
   __shared__ Group found[(kWaves + 1) * kMostKept], best[kMostKept], room[kWaves][64];
   __shared__ Group near[kMostKept * 8], pick[kMostKept];  // classes by their logits in 32 bits

@@ -25,7 +25,7 @@ using namespace wnt;
 // logits lie and no loss is negative.  (fma(l, log2 e, -largest log2 e) is one operation shorter, but the rounding of
 // its last term moves every exponential of the row: by 1e-6 at logits of 20, a factor of 3e5 at -1e9.)
 struct StatsEnd {
-  static constexpr bool kScaledByTile = false, kStarts = false;
+  static constexpr bool kScaledByTile = false;
   Logits l;
   float2* part;   // [tiles of all pieces][N]
   int tile0;      // the piece's first
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void row_terms(const float* g, const float* h,
 // hi and lo parts) at a time, so that its stores are runs of 128 bytes.
 template <bool SP, bool ENT>
 struct GradEnd {
-  static constexpr bool kScaledByTile = false, kStarts = false;
+  static constexpr bool kScaledByTile = false;
   Logits l;
   const float *lse, *g;
   const float* gmax;  // bf16: parts of max |g| (largest_g); null without qt
@@ -311,7 +311,7 @@ struct GradEnd {
 // dx and dw: out[b][a] (rows of D).  DW in fp32: operand B's scales change from tile to tile of k.
 template <class E, bool DW>
 struct OutEnd {
-  static constexpr bool kScaledByTile = sizeof(E) == 4 && DW, kStarts = false;
+  static constexpr bool kScaledByTile = sizeof(E) == 4 && DW;
   int A, B;           // D, rows
   const int* ea;      // fp32: scales of operand A's rows; the product is acc 2^-(ea[a] + eb)
   const int* eq;      // fp32 dw: eb of each tile of k, [tiles][B]

@@ -1,7 +1,7 @@
 // Updates orthogonalised by Newton-Schulz products (gfx950).  Declarations and contracts are in include/wn_train.h.
 //
 // Each matrix is X [m][n] with m <= n (a taller one transposed), its Frobenius norm at most 1.  A step is
-//   A = X X',  B = b A + c A A,  X <- a X + B X
+//   A = X X',  B = a I + b A + c A A,  X <- B X
 // three products of 16-bit operands on wn_product.h's tiles, all matrices of a call in one launch each.  A and B are symmetric:
 // their tiles on one side of the diagonal are computed and stored twice.  Both operands of a product lie along its sum, so
 // X is kept in both orders (the end of a step writes both).
@@ -26,10 +26,17 @@ constexpr size_t kGroupBytes = (size_t)4 << 30;  // of the matrices that go thro
 // (small products are a chain of a few chunks' loads: room for four)
 using Tiny = Tile<64, 64, 2, 2, 4>;
 
+// Addresses that kernels read from memory, as pointers that are known to lie in memory and not in LDS: through a pointer that
+// could be either, accesses are slower and the waits for LDS wait for them too.
+typedef unsigned long long Address;
+template <class T>
+__device__ __forceinline__ T* in_memory(Address p) {
+  return (T*)(__attribute__((address_space(1))) T*)p;
+}
+
 struct Matrix {
-  const void* g;
-  void* out;
-  u16 *x, *xt[2], *a, *b;  // X [m][ldn], its transpose [n][ldm] of this step and the next, A and B [m][ldm]
+  Address g, out;
+  Address x, xt[2], a, b;  // X [m][ldn], its transpose [n][ldm] of this step and the next, A and B [m][ldm]
   int m, n, ldm, ldn;      // m <= n; units from row to row
   int tall;                // g is X transposed
   float scale;
@@ -76,7 +83,7 @@ __global__ __launch_bounds__(256) void squares(const Group g) {
   const Matrix& m = g.matrices[g.of_chunk[blockIdx.x]];
   const long long all = (long long)m.m * m.n, at = (blockIdx.x - m.chunk0) * m.chunk, end = at + m.chunk < all ? at + m.chunk : all;
   constexpr int W = Piece<E>::n;
-  const E* p = static_cast<const E*>(m.g);
+  const E* p = in_memory<const E>(m.g);
   double sum[2] = {0.0, 0.0};
   auto add = [&](const P<E>& v) {
 #pragma unroll
@@ -97,6 +104,14 @@ __global__ __launch_bounds__(256) void squares(const Group g) {
   for (; i < end; i += 256 * W) add(piece_at(p + i, (int)(end - i < W ? end - i : W)));
   const double s = block_sum(sum[0] + sum[1]);
   if (threadIdx.x == 0) g.squares[blockIdx.x] = s;
+}
+
+// (Value by value: the compiler makes one wide load of a factor and what lies beside it where it is multiplied with a vector,
+// and then keeps the structure that both are members of in private memory.)
+__device__ __forceinline__ f32x4 times(f32x4 v, float f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= f;
+  return v;
 }
 
 // Four values to place k of a row (a multiple of 4), times 2^kX where they are of X.
@@ -137,9 +152,9 @@ __global__ __launch_bounds__(256) void pack(const Group g, double eps) {
   const double norm = sqrt(block_sum(sum)) + eps, f = norm != 0.0 ? (1 << kX) / norm : 0.0;
   const int rows = m.tall ? m.n : m.m, cols = m.tall ? m.m : m.n, wide = (cols + 63) / 64, t = blockIdx.x - m.pack0;
   const int r0 = t / wide * 64, c0 = t % wide * 64, tid = threadIdx.x;
-  const E* p = static_cast<const E*>(m.g);
-  u16* const as = m.tall ? m.xt[0] : m.x;
-  u16* const across = m.tall ? m.x : m.xt[0];
+  const E* p = in_memory<const E>(m.g);
+  u16* const as = in_memory<u16>(m.tall ? m.xt[0] : m.x);
+  u16* const across = in_memory<u16>(m.tall ? m.x : m.xt[0]);
   const int lda = m.tall ? m.ldm : m.ldn, ldc = m.tall ? m.ldn : m.ldm;
   // a thread has 16 values of a row, then of a column
   const int i = tid >> 2, c = 16 * (tid & 3), r = r0 + i;
@@ -172,32 +187,15 @@ __global__ __launch_bounds__(256) void pack(const Group g, double eps) {
 // ------------------------------------------------------------------------------------------------
 enum Phase { kGram, kPoly, kStep, kLast };
 
-// The sums' first values: ratio from[b][a], or 0.  (Read while the first chunks are under way, not behind the last.)
-template <class T, bool SP>
-__device__ __forceinline__ void start_with(f32x4 (&acc)[T::NA][T::NB], const Place& pl, const u16* from, float ratio, int B, int ld) {
-#pragma unroll
-  for (int j = 0; j < T::NB; ++j) {
-    const int b = pl.b0 + 16 * j + pl.n;
-#pragma unroll
-    for (int i = 0; i < T::NA; ++i) {
-      const int a = pl.a0 + 16 * i + 4 * pl.quad;
-      acc[i][j] = from && b < B && a < values_of<SP>(ld) ? get4<SP>(from + (size_t)b * ld, a) * ratio : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-  }
-}
-
-// rows[b][a] and cols[a][b] = alpha (ratio from[b][a] + sum) + beta with[b][a], in the units of their operands.
-template <bool SP>
+// rows[b][a] and cols[a][b] = alpha (sum), and of kPoly + beta with[b][a] + unit [a = b], in the units of their operands.  (Phases are
+// parameters of the templates: an end that is put together at run time would be kept in private memory.)
+template <bool SP, int kPhase>
 struct Keep {
-  static constexpr bool kScaledByTile = false, kStarts = true;
-  float alpha, beta, ratio;
-  const u16 *with, *from;  // [B][ldr], or null
-  u16 *rows, *cols;        // cols: null on the diagonal of a symmetric product
+  static constexpr bool kScaledByTile = false;
+  float alpha, beta, unit;
+  const u16* with;   // [B][ldr]
+  u16 *rows, *cols;
   int A, B, ldr, ldc;
-  template <class T>
-  __device__ __forceinline__ void start(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
-    start_with<T, SP>(acc, pl, from, ratio, B, ldr);
-  }
   template <class T>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
     constexpr int RA = 16 * T::NA, kPer = SP ? 2 : T::NB;  // the wave's a; tiles of b that go through LDS together
@@ -206,6 +204,7 @@ struct Keep {
     char* const tr = lds + (pl.wa * T::WB + pl.wb) * RA * kBytes;
     const int lane = threadIdx.x & 63;
     const bool odd = lane & 1;
+    const bool across = kPhase == kStep || pl.ta != pl.tb;  // (a tile on the diagonal of a symmetric product holds both)
     auto place = [](int v, int piece) { return v * kBytes + ((piece ^ (v >> 1 & (kPieces - 1))) << 4); };
     // Two lanes that hold neighbouring rows of b (n even, n + 1) swap two of their four values: the even lane then holds
     // values 0 and 1 of both, the odd one 2 and 3, and each writes pairs.
@@ -221,12 +220,27 @@ struct Keep {
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
       const int b = pl.b0 + 16 * j + pl.n;
+      if constexpr (kPhase == kPoly) {  // (all of a row's reads before its stores, which could be to the same place for all that is known)
+        f32x4 more[T::NA];
+#pragma unroll
+        for (int i = 0; i < T::NA; ++i) {
+          const int a = pl.a0 + 16 * i + 4 * pl.quad;
+          more[i] = b < B && a < values_of<SP>(ldr) ? get4<SP>(with + (size_t)b * ldr, a) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int i = 0; i < T::NA; ++i) {
+          const int a = pl.a0 + 16 * i + 4 * pl.quad;
+          acc[i][j] = times(acc[i][j], alpha) + times(more[i], beta);
+          if (pl.ta == pl.tb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] += a + e == b ? unit : 0.f;
+        }
+      }
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) {
         const int a = pl.a0 + 16 * i + 4 * pl.quad;
         const bool in = b < B && a < values_of<SP>(ldr);
-        f32x4 v = acc[i][j] * alpha;
-        if (with && in) v += get4<SP>(with + (size_t)b * ldr, a) * beta;
+        const f32x4 v = kPhase == kPoly ? acc[i][j] : times(acc[i][j], alpha);
         u16 hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -239,12 +253,12 @@ struct Keep {
           if constexpr (SP)
             *reinterpret_cast<u32x2*>(d + 32) = u32x2{(unsigned)lo[0] | (unsigned)lo[1] << 16, (unsigned)lo[2] | (unsigned)lo[3] << 16};
         }
-        if (cols) {
+        if (across) {
           put_pair(i, 16 * (j % kPer) + (pl.n & ~1), hi);
           if constexpr (SP) put_pair(i, 32 + 16 * (j % kPer) + (pl.n & ~1), lo);
         }
       }
-      if (j % kPer != kPer - 1 || !cols) continue;
+      if (j % kPer != kPer - 1 || !across) continue;
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own part of LDS)
       const int unit0 = SP ? (pl.b0 + 16 * (j - 1)) * 2 : pl.b0;
       constexpr int kRows = 64 / kPieces;
@@ -259,18 +273,13 @@ struct Keep {
   }
 };
 
-// out[b][a] = alpha (ratio from[b][a] + sum).
+// out[b][a] = alpha (sum).
 template <class E>
 struct Result {
-  static constexpr bool kScaledByTile = false, kStarts = true;
-  float alpha, ratio;
-  const u16* from;  // [B][ld]
-  E* out;           // [B][A]
-  int A, B, ld;
-  template <class T>
-  __device__ __forceinline__ void start(f32x4 (&acc)[T::NA][T::NB], const Place& pl) const {
-    start_with<T, sizeof(E) == 4>(acc, pl, from, ratio, B, ld);
-  }
+  static constexpr bool kScaledByTile = false;
+  float alpha;
+  E* out;  // [B][A]
+  int A, B;
   template <class T>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char*) const {
 #pragma unroll
@@ -281,7 +290,7 @@ struct Result {
       for (int i = 0; i < T::NA; ++i) {
         const int a = pl.a0 + 16 * i + 4 * pl.quad;
         if (a >= A) continue;
-        const f32x4 v = acc[i][j] * alpha;
+        const f32x4 v = times(acc[i][j], alpha);
         E* d = out + (size_t)b * A + a;
         if (a + 3 < A) {
           if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(d) = f32x4u{v[0], v[1], v[2], v[3]};
@@ -298,7 +307,7 @@ struct Result {
 
 struct Step {
   float a, b, c;
-  int phase, now;  // now: which of xt is this step's
+  int now;  // which of xt is this step's
 };
 
 // The order of a launch's tiles: classes of matrices alike, those with the longest tiles first.  Each XCD (block b runs on XCD b
@@ -331,33 +340,30 @@ struct Order {
   }
 };
 
-template <class T, class E>
+template <class T, class E, int kPhase>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group g, const Step s, const Order order) {
-  constexpr bool SP = sizeof(E) == 4;
+  constexpr bool SP = sizeof(E) == 4, kSym = kPhase <= kPoly;
   extern __shared__ __align__(16) char lds[];
   const int block = order.tile();
   if (block < 0) return;
-  const bool sym = s.phase <= kPoly;
-  const Matrix& m = g.matrices[(sym ? g.of_sym : g.of_step)[block]];
+  const Matrix& m = g.matrices[(kSym ? g.of_sym : g.of_step)[block]];
   Place pl;
   Operand oa, ob;
-  if (sym) {
+  if constexpr (kSym) {
     const int t = block - m.sym0;
     int i = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
     while (i * (i + 1) / 2 > t) --i;
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     pl.tb = i;
     pl.ta = t - i * (i + 1) / 2;
-    oa = s.phase == kGram ? Operand{m.x, m.m, m.ldn, m.ldn} : Operand{m.a, m.m, m.ldm, m.ldm};
+    const int ld = kPhase == kGram ? m.ldn : m.ldm;
+    oa = {in_memory<u16>(kPhase == kGram ? m.x : m.a), m.m, ld, ld};
     ob = oa;
   } else {
-    oa = {m.xt[s.now], m.n, m.ldm, m.ldm};
-    ob = {m.b, m.m, m.ldm, m.ldm};
-    if (s.phase == kLast && m.tall) {
-      const Operand o = oa;
-      oa = ob;
-      ob = o;
-    }
+    const bool turned = kPhase == kLast && m.tall;
+    const Address xt = s.now ? m.xt[1] : m.xt[0];
+    oa = {in_memory<u16>(turned ? m.b : xt), turned ? m.m : m.n, m.ldm, m.ldm};
+    ob = {in_memory<u16>(turned ? xt : m.b), turned ? m.n : m.m, m.ldm, m.ldm};
     const int ta = (int)((oa.rows + T::TA - 1) / T::TA), tb = (int)((ob.rows + T::TB - 1) / T::TB), t = block - m.step0;
     const int band = t / (kBand * ta), in = t - band * kBand * ta, wide = min(kBand, tb - band * kBand);
     pl.ta = in / wide;
@@ -366,38 +372,25 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group
   pl.in_tile<T>();
   f32x4 acc[T::NA][T::NB];
   auto exp2i = [](int e) { return __uint_as_float((unsigned)(127 + e) << 23); };
-  if (s.phase == kLast) {
-    const Result<E> end{m.scale * exp2i(-kB - kX), s.a * exp2i(kB), m.tall ? m.xt[s.now] : m.x, static_cast<E*>(m.out),
-                        (int)oa.rows, (int)ob.rows, m.tall ? m.ldm : m.ldn};
+  if constexpr (kPhase == kLast) {
+    const Result<E> end{m.scale * exp2i(-kB - kX), in_memory<E>(m.out), (int)oa.rows, (int)ob.rows};
     tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
     end.template operator()<T>(acc, pl, lds);
-    return;
-  }
-  Keep<SP> end{};
-  end.A = (int)oa.rows;
-  end.B = (int)ob.rows;
-  if (s.phase == kGram) {
-    end.alpha = exp2i(kA - 2 * kX);
-    end.rows = m.a;
-    end.ldr = end.ldc = m.ldm;
-  } else if (s.phase == kPoly) {
-    end.alpha = s.c * exp2i(kB - 2 * kA);
-    end.beta = s.b * exp2i(kB - kA);
-    end.with = m.a;
-    end.rows = m.b;
-    end.ldr = end.ldc = m.ldm;
   } else {
-    end.alpha = exp2i(-kB);
-    end.ratio = s.a * exp2i(kB);
-    end.from = m.x;
-    end.rows = m.x;
-    end.cols = m.xt[s.now ^ 1];
-    end.ldr = m.ldn;
-    end.ldc = m.ldm;
+    u16* const rows = in_memory<u16>(kPhase == kGram ? m.a : kPhase == kPoly ? m.b : m.x);
+    const Keep<SP, kPhase> end{kPhase == kGram ? exp2i(kA - 2 * kX) : kPhase == kPoly ? s.c * exp2i(kB - 2 * kA) : exp2i(-kB),
+                               s.b * exp2i(kB - kA),
+                               s.a * exp2i(kB),
+                               in_memory<const u16>(m.a),
+                               rows,
+                               kSym ? rows : in_memory<u16>(s.now ? m.xt[0] : m.xt[1]),
+                               (int)oa.rows,
+                               (int)ob.rows,
+                               kPhase == kStep ? m.ldn : m.ldm,
+                               m.ldm};
+    tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
+    end.template operator()<T>(acc, pl, lds);
   }
-  if (sym && pl.ta != pl.tb) end.cols = end.rows;
-  tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
-  end.template operator()<T>(acc, pl, lds);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -498,12 +491,17 @@ GroupPlan next_group(int n_arrays, const wn_ortho_array* arrays, int dtype, int&
   return p;
 }
 
-template <class T, class E>
+template <class T, class E, int kPhase>
 hipError_t launch_newton(const Group& g, const Step& s, const Order& order, hipStream_t st) {
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(newton<T, E>), hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(newton<T, E, kPhase>), hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((newton<T, E>), dim3(order.blocks()), dim3(T::kThreads), T::kLds, st, g, s, order);
+  hipLaunchKernelGGL((newton<T, E, kPhase>), dim3(order.blocks()), dim3(T::kThreads), T::kLds, st, g, s, order);
   return hipGetLastError();
+}
+template <class E, int kPhase>
+hipError_t launch_tiles(int tile, const Group& g, const Step& s, const Order& order, hipStream_t st) {
+  return tile == 0 ? launch_newton<Big, E, kPhase>(g, s, order, st)
+                   : tile == 1 ? launch_newton<Small, E, kPhase>(g, s, order, st) : launch_newton<Tiny, E, kPhase>(g, s, order, st);
 }
 
 template <class E>
@@ -526,9 +524,9 @@ hipError_t run_group(const GroupPlan& p, const wn_ortho_array* arrays, int steps
       const wn_ortho_array& a = arrays[p.arrays[at]];
       const Sides s(a);
       Matrix& m = batch.m[n];
-      auto units = [&](int rows, int ld) { return reinterpret_cast<u16*>(ws + c.take((size_t)rows * ld * 2)); };
-      m.g = a.g;
-      m.out = a.out;
+      auto units = [&](int rows, int ld) { return reinterpret_cast<Address>(ws + c.take((size_t)rows * ld * 2)); };
+      m.g = reinterpret_cast<Address>(a.g);
+      m.out = reinterpret_cast<Address>(a.out);
       m.x = units(s.m, s.ldn);
       m.xt[0] = units(s.n, s.ldm);
       m.xt[1] = units(s.n, s.ldm);
@@ -551,17 +549,11 @@ hipError_t run_group(const GroupPlan& p, const wn_ortho_array* arrays, int steps
   hipLaunchKernelGGL(squares<E>, dim3(chunks), dim3(256), 0, st, g);
   hipLaunchKernelGGL(pack<E>, dim3(packs), dim3(256), 0, st, g, (double)eps);
   hipError_t e = hipGetLastError();
-  auto launch = [&](int tile, const Step& s, const Order& o) {
-    if (e != hipSuccess) return;
-    e = tile == 0 ? launch_newton<Big, E>(g, s, o, st) : tile == 1 ? launch_newton<Small, E>(g, s, o, st) : launch_newton<Tiny, E>(g, s, o, st);
-  };
-  for (int k = 0; k < steps; ++k) {
-    Step s{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], kGram, k & 1};
-    launch(p.sym, s, p.sym_order);
-    s.phase = kPoly;
-    launch(p.sym, s, p.sym_order);
-    s.phase = k + 1 < steps ? kStep : kLast;
-    launch(p.step, s, p.step_order);
+  for (int k = 0; k < steps && e == hipSuccess; ++k) {
+    const Step s{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], k & 1};
+    e = launch_tiles<E, kGram>(p.sym, g, s, p.sym_order, st);
+    if (e == hipSuccess) e = launch_tiles<E, kPoly>(p.sym, g, s, p.sym_order, st);
+    if (e == hipSuccess) e = k + 1 < steps ? launch_tiles<E, kStep>(p.step, g, s, p.step_order, st) : launch_tiles<E, kLast>(p.step, g, s, p.step_order, st);
   }
   return e;
 }

@@ -76,9 +76,8 @@ typedef u16 u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// The sums of chunks c0 .. c1 - 1 of a tile, in V8's type of 16-bit values (SP: hi and lo parts), added to what `end` starts
-// with (kStarts) or to 0.  Operands go from memory straight to LDS (kStages chunks of each), from there to registers half a
-// chunk ahead of their products.
+// The sums of chunks c0 .. c1 - 1 of a tile, in V8's type of 16-bit values (SP: hi and lo parts).  Operands go from memory
+// straight to LDS (kStages chunks of each), from there to registers half a chunk ahead of their products.
 template <class T, bool SP, class V8, class End>
 __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Operand& a, const Operand& b, const Place& pl, int c0, int c1,
                                           char* lds, const End& end) {
@@ -113,19 +112,11 @@ __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Oper
     for (int k = 0; k < kPieces; ++k)
       if (k * T::NA / kPieces == i) stage_piece(c, to, k);
   };
+#pragma unroll
+  for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   constexpr int S = T::kStages;
-  if (S > 2 || End::kStarts)
-#pragma unroll
-    for (int k = 0; k < S; ++k)
-      if (c0 + k < c1) stage(c0 + k, lds + k * T::kStage);
-  if constexpr (End::kStarts) {
-    end.template start<T>(acc, pl);
-  } else {
-#pragma unroll
-    for (int i = 0; i < T::NA; ++i)
-#pragma unroll
-      for (int j = 0; j < T::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
   const int ra = pl.wa * (T::TA / T::WA), rb = pl.wb * (T::TB / T::WB);
   const int sw = pl.n >> 1;
   const int fa = (ra + pl.n) * kChunk * 2, fb = (T::TA + rb + pl.n) * kChunk * 2;
@@ -136,10 +127,9 @@ __device__ __forceinline__ void tile_sums(f32x4 (&acc)[T::NA][T::NB], const Oper
   // a chunk's first and second half of each operand's values (SP: hi and lo parts)
   V8 a0[T::NA], a1[T::NA], b0[T::NB], b1[T::NB];
   if (c0 < c1) {
-    if (S == 2 && !End::kStarts) {
-      stage(c0, buffer(c0));
-      if (c0 + 1 < c1) stage(c0 + 1, buffer(c0 + 1));
-    }
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+      if (c0 + k < c1) stage(c0 + k, lds + k * T::kStage);
     if (c0 + S - 1 < c1) {
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"((S - 1) * kPieces) : "memory");
     } else {

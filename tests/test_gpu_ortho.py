@@ -4,7 +4,7 @@ Tolerances, in the Frobenius norm |.|.  A step takes X to f(X), whose singular v
 X's.  An error of X grows by at most L, the largest of |phi'| and |phi(s) / s| on [0, |X|_2] (the derivative of f has
 the divided differences of phi and (phi(s) + phi(t)) / (s + t) as factors), and a step adds its own:
   A = X X':       h |A| + K(n) | |X| |X|' |          h: what a value is held to, fp16 2^-11 or two fp16 parts 2^-22
-  B = b A + c A A: (|b| + 2 |c| |A|_2) err(A) + h |B| + |c| K(m) | |A| |A| |
+  B = a I + b A + c A A: (|b| + 2 |c| |A|_2) err(A) + h |B| + |c| K(m) | |A| |A| |
   X:              |X|_2 err(B) + h |X| + K(m) | |B| |X| |
 with K(k) = k u of fp32 sums (u = 2^-24), of two parts 3 k u and 3 2^-22 for the product of the low parts and the
 parts' rounding, and 2^-37, 2^-37 and 2^-35 for each value of X, A and B that fp16's smallest step cuts off.  A tenth is
@@ -53,14 +53,14 @@ def _formula(g, scale=1.0, steps=MUON, eps=1e-7):
     err = h * float(x.norm()) + 2.0 ** -37 * (m * n) ** 0.5
     for a, b, c in steps:
         A = x @ x.t().contiguous()
-        B = b * A + c * A @ A
+        B = a * torch.eye(m, dtype=torch.float64, device=A.device) + b * A + c * A @ A
         s2 = _largest(A)
         top = s2 ** 0.5
         s = np.linspace(0, top * 1.01, 2001)
         L = max(np.abs(a + 3 * b * s ** 2 + 5 * c * s ** 4).max(), np.abs(a + b * s ** 2 + c * s ** 4).max())
         eA = h * float(A.norm()) + K(n) * float((x.abs() @ x.abs().t().contiguous()).norm()) + 2.0 ** -37 * m
         eB = (abs(b) + 2 * abs(c) * s2) * eA + h * float(B.norm()) + abs(c) * K(m) * float((A.abs() @ A.abs()).norm()) + 2.0 ** -35 * m
-        new = a * x + B @ x
+        new = B @ x
         eX = top * eB + h * float(new.norm()) + K(m) * float((B.abs() @ x.abs()).norm()) + 2.0 ** -37 * (m * n) ** 0.5
         err = 1.1 * (L * err + eX)
         x = new
