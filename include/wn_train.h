@@ -93,9 +93,10 @@ size_t wn_loss_backward_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int
  *   top_logprobs  fp32 [N][top] out, their log probabilities.  Both may be NULL where top is 0.
  * The alternatives' logits are summed in 64 bits, so classes closer to each other than the other logits' rounding are in
  * order; one that that rounding moves behind more than two others (and one more for each 8 of top) in other groups of 8
- * classes may be missed.  A class of bias -inf is masked: it adds nothing to the entropy and is an alternative (of log
- * probability -inf) only where fewer than top are left.  If every class is masked, or a logit is NaN or +inf, the row's logprob,
- * entropy, lse and top_logprobs are NaN or infinite and its top_ids any classes.
+ * classes may be missed (more than 64 rows of up to 1024 classes: in any groups).  A class of bias -inf is masked: it adds
+ * nothing to the entropy and is an alternative (of log probability -inf) only where fewer than top are left.  If every class
+ * is masked, or a logit is NaN or +inf, the row's logprob, entropy, lse and top_logprobs are NaN or infinite and its top_ids
+ * any classes.
  * Sizes and errors as wn_loss; top 0 .. 32 and at most V.
  */
 int wn_logprobs(int32_t dtype, int32_t N, int32_t D, int32_t V, int32_t top, const void* x, const void* w, const float* b,

@@ -8,9 +8,10 @@
 //
 // Alternatives: the end also leaves the largest logit of every 8 classes.  The K likeliest classes lie in the K groups of
 // 8 whose largest logits are largest (any K classes from K other groups would be less likely), so a row's groups are
-// searched for a few more than K (kept()), and their classes' logits are computed anew, in 64 bits.  So the logits
-// are neither kept nor sorted, classes next to each other are in order although the product's sums are of 32 bits, and
-// equal ones (copies of a row of w) are equal: the lowest index comes first.
+// searched for a few more than K (kept()), and their classes' logits are computed anew, in 64 bits.  (Of up to 1024 classes
+// each is a group by itself, see group_of.)  So the logits of many classes are neither kept nor sorted, classes next to
+// each other are in order although the product's sums are of 32 bits, and equal ones (copies of a row of w) are equal: the
+// lowest index comes first.
 #include "wn_product.h"
 
 namespace {
@@ -30,7 +31,8 @@ struct ProbeEnd {
   float* spread;   // t
   int tile0;       // the piece's first
   float* target;   // [N]
-  float* groups;   // [N][ceil(l.V / 8)], or null
+  float* groups;   // [N][ceil(l.V / 8)] or [N][l.V], or null
+  int per;         // classes of a group: 8 or 1
   template <class T>
   __device__ void operator()(f32x4 (&acc)[T::NA][T::NB], const Place& pl, char* lds) const {
     l.take<T>(acc, pl);
@@ -49,7 +51,20 @@ struct ProbeEnd {
       }
       o.m = quads_max(o.m);
       Logits::at_target<T>(pl, t < l.V ? t : -1, [&](int i, int e) { target[n] = acc[i][j][e]; });
-      if (groups) {
+      if (groups && per == 1) {
+#pragma unroll
+        for (int i = 0; i < T::NA; ++i) {
+          const int v = pl.a0 + 16 * i + 4 * pl.quad;
+          float* const at = groups + (size_t)n * l.V + v;
+          if (n < l.N && v + 3 < l.V) {
+            *reinterpret_cast<f32x4u*>(at) = f32x4u{acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+          } else if (n < l.N) {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (v + e < l.V) at[e] = acc[i][j][e];
+          }
+        }
+      } else if (groups) {
         // an even quad and the odd one behind it hold 8 classes of a row: the even one stores those of even i
 #pragma unroll
         for (int i = 0; i < T::NA; i += 2) {
@@ -176,6 +191,7 @@ __device__ __forceinline__ Group largest_of(Group (&e)[R], int want) {
 
 struct Alternatives {
   const float* groups;  // [N][count] of this piece
+  int per;              // classes of a group: 8 or 1
   int count, first;     // its groups, the number of the first
   int N, D, V, top;
   const void *x, *w;
@@ -309,9 +325,11 @@ __device__ __forceinline__ S class_logits(const Alternatives& a, int n, const in
   return s;
 }
 
-// A block per row.  The waves find the largest groups of their segments, which are then joined; in the last piece they
-// compute the logits of these groups' classes in 32 bits, of which the largest, as many as groups, are computed in 64 and
-// ranked by counting.  For few rows the block joins its row's statistics first.
+// A block per row.  The waves find the largest groups of their segments, which are then joined; in the last piece, unless
+// the groups are single classes, they compute the logits of these groups' classes in 32 bits.  The largest, as many as
+// groups, are computed in 64 and ranked by counting.  (All of the groups' classes in 64 at once, a round of loads less, takes
+// few rows longer: 1 row x 32000 classes x 2048, 5 alternatives 51 us and not 48, 100 x 16000 x 4096, 32 of them 216 and not
+// 178.)  For few rows the block joins its row's statistics first.
 template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
   constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
@@ -355,50 +373,54 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
     if (tid < want) a.list[(size_t)n * want + tid] = best[tid];
     return;
   }
-  for (int k = wave; k < want; k += kWaves) {
-    const int g = best[k].g, c = lane >> 3;
-    Group e{-INFINITY, kNone};
-    if (g != kNone) {
-      int v[8];
+  const bool single = a.per == 1;  // (then the groups are the classes themselves)
+  const Group* const chosen = single ? best : pick;
+  int picked = min(a.V, want);
+  if (!single) {
+    for (int k = wave; k < want; k += kWaves) {
+      const int g = best[k].g, c = lane >> 3;
+      Group e{-INFINITY, kNone};
+      if (g != kNone) {
+        int v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = min(g * 8 + i, a.V - 1);
-      const float l = class_logits<E, float, 8, kAhead>(a, n, v);
-      if (g * 8 + c < a.V) e = {fmaxf(l, -INFINITY), g * 8 + c};
+        for (int i = 0; i < 8; ++i) v[i] = min(g * 8 + i, a.V - 1);
+        const float l = class_logits<E, float, 8, kAhead>(a, n, v);
+        if (g * 8 + c < a.V) e = {fmaxf(l, -INFINITY), g * 8 + c};
+      }
+      if ((lane & 7) == 0) near[k * 8 + c] = e;
+      const float m = wnk::wave_max(e.v);
+      if (lane == 0) top_of[k] = m;
     }
-    if ((lane & 7) == 0) near[k * 8 + c] = e;
-    const float m = wnk::wave_max(e.v);
-    if (lane == 0) top_of[k] = m;
+    __syncthreads();
+    // the want largest of them reach the least of the groups' largest
+    if (wave == 0) {
+      const float t = -wnk::wave_max(lane < want ? -top_of[lane] : -INFINITY);
+      int m = 0;
+      for (int i = 0; i < want * 8; i += 64) {
+        const Group e = i + lane < want * 8 ? near[i + lane] : Group{-INFINITY, kNone};
+        const bool in = e.g != kNone && e.v >= t;
+        const unsigned long long all = __ballot(in);
+        asm volatile("" ::: "memory");
+        if (in) near[m + __popcll(all & ((1ull << lane) - 1))] = e;  // (never behind what is still to be read)
+        m += __popcll(all);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int i = lane; i < m; i += 64) {
+        const Group e = near[i];
+        int rank = 0;
+        for (int k = 0; k < m; ++k) rank += before(near[k], e);
+        if (rank < want) pick[rank] = e;
+      }
+      picked = min(m, want);
+      if (lane == 0) top_of[0] = __int_as_float(picked);
+    }
+    __syncthreads();
+    picked = __float_as_int(top_of[0]);
   }
-  __syncthreads();
-  // the want largest of them reach the least of the groups' largest
-  int picked = 0;
-  if (wave == 0) {
-    const float t = -wnk::wave_max(lane < want ? -top_of[lane] : -INFINITY);
-    int m = 0;
-    for (int i = 0; i < want * 8; i += 64) {
-      const Group e = i + lane < want * 8 ? near[i + lane] : Group{-INFINITY, kNone};
-      const bool in = e.g != kNone && e.v >= t;
-      const unsigned long long all = __ballot(in);
-      asm volatile("" ::: "memory");
-      if (in) near[m + __popcll(all & ((1ull << lane) - 1))] = e;  // (never behind what is still to be read)
-      m += __popcll(all);
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    for (int i = lane; i < m; i += 64) {
-      const Group e = near[i];
-      int rank = 0;
-      for (int k = 0; k < m; ++k) rank += before(near[k], e);
-      if (rank < want) pick[rank] = e;
-    }
-    picked = min(m, want);
-    if (lane == 0) top_of[0] = __int_as_float(picked);
-  }
-  __syncthreads();
-  picked = __float_as_int(top_of[0]);
   for (int k = wave * 4; k < picked; k += kWaves * 4) {
     int v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pick[min(k + i, picked - 1)].g;
+    for (int i = 0; i < 4; ++i) v[i] = chosen[min(k + i, picked - 1)].g;
     const double l = class_logits<E, double, 4, kAhead>(a, n, v);
     if ((lane & 15) == 0 && k + (lane >> 4) < picked)
       logit[k + (lane >> 4)] = l == l ? l : -INFINITY;  // (where a logit is a NaN, log s is, and so is what comes out)
@@ -406,12 +428,12 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
   __syncthreads();
   if (tid >= picked) return;  // (of the first wave: it has a lane for each)
   if (!a.part) z = a.log_s[n];
-  const int v = pick[tid].g;
+  const int v = chosen[tid].g;
   const double l = logit[tid];
   int rank = 0;
   double most = -INFINITY;
   for (int k = 0; k < picked; ++k) {
-    const int o = pick[k].g;
+    const int o = chosen[k].g;
     const double ol = logit[k];
     rank += ol > l || (ol == l && o < v);
     most = fmax(most, ol);
@@ -425,11 +447,18 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
 // ------------------------------------------------------------------------------------------------
 // Host
 // ------------------------------------------------------------------------------------------------
+// Classes of a group.  Where one segment holds a row's logits, they are kept and searched themselves, which costs less than
+// the logits of eight classes for each one wanted.  Groups of 8 and of 1 (us a call): 16000 rows x 256 classes x 256 in fp32, 3
+// alternatives 86 and 60, in bf16 20 of them 274 and 107; 16000 x 1024 x 256, 5: 118 and 93; 300 x 1000 x 1024, 20: 47 and 36;
+// 2000 x 1024 x 64, 5: 35 and 36; but 16000 x 1030 x 256, 5: 139 and 229, and few rows gain nothing (64 x 1000 x 1024, 5: 25
+// and 25; 1 x 2048 x 2048: 20 and 27).
+int group_of(int N, int V) { return N > kFewRows && V <= 64 * kSegment && (size_t)N * V * 4 <= kGroupsBytes ? 1 : 8; }
+
 // Classes of a piece; `each` as for forward_piece.
 int probe_piece(int N, int V, size_t each, int top) {
   const int most = forward_piece(N, V, each);
   if (!top) return most;
-  const size_t fit = std::max<size_t>(256, kGroupsBytes / 4 * 8 / N / 256 * 256);
+  const size_t fit = std::max<size_t>(256, kGroupsBytes / 4 * group_of(N, V) / N / 256 * 256);
   return (int)std::min<size_t>(most, fit);
 }
 
@@ -445,7 +474,7 @@ struct Probe {
     spread = c.take(tiles * N * 4);
     target = c.take((size_t)N * 4);
     log_s = c.take((size_t)N * 4);
-    groups = c.take(top ? (size_t)N * ceil_div(few ? V : probe_piece(N, V, 0, top), 8) * 4 : 0);
+    groups = c.take(top ? (size_t)N * ceil_div(few ? V : probe_piece(N, V, 0, top), group_of(N, V)) * 4 : 0);
     list = c.take(top ? (size_t)N * kept(top) * sizeof(Group) : 0);
     if (!few) {
       x = c.take((size_t)N * units * 2);
@@ -489,7 +518,8 @@ int run_probe(const ProbeCall& c, const E* x, const E* w, char* ws, hipStream_t 
   float* const log_s = reinterpret_cast<float*>(ws + f.log_s);
   float* const groups = c.top ? reinterpret_cast<float*>(ws + f.groups) : nullptr;
   const RowOut rows{target, c.y, N, V, c.logprob, c.entropy, c.lse, log_s};
-  Alternatives alt{groups, 0, 0, N, D, V, c.top, x, w, c.b, log_s, reinterpret_cast<Group*>(ws + f.list), 0, 0, nullptr, nullptr, 0, rows,
+  const int per = group_of(N, V);
+  Alternatives alt{groups, per, 0, 0, N, D, V, c.top, x, w, c.b, log_s, reinterpret_cast<Group*>(ws + f.list), 0, 0, nullptr, nullptr, 0, rows,
                    c.ids, c.top_logprobs};
   if (N <= kFewRows) {
     hipError_t e = wn_few_probe<E>({N, D, V, x, w, c.b, c.y}, part, spread, target, groups, st);
@@ -499,7 +529,7 @@ int run_probe(const ProbeCall& c, const E* x, const E* w, char* ws, hipStream_t 
       e = hipGetLastError();
     }
     if (e == hipSuccess && c.top) {
-      alt.count = (int)ceil_div(V, 8);
+      alt.count = (int)ceil_div(V, per);
       alt.last = 1;
       alt.part = part;
       alt.spread = spread;
@@ -521,11 +551,11 @@ int run_probe(const ProbeCall& c, const E* x, const E* w, char* ws, hipStream_t 
     const Operand ow = pack.add(w + (size_t)v0 * D, n, D, reinterpret_cast<u16*>(ws + f.w), ew);
     pack.launch(st);
     const bool big = shape_for(n, N, ox.k, sp, false).big;
-    const ProbeEnd end{{sp ? ex : nullptr, sp ? ew : nullptr, c.b ? c.b + v0 : nullptr, c.y, N, n, v0, V}, part, spread, tiles, target, groups};
+    const ProbeEnd end{{sp ? ex : nullptr, sp ? ew : nullptr, c.b ? c.b + v0 : nullptr, c.y, N, n, v0, V}, part, spread, tiles, target, groups, per};
     e = run_product<sp>({ow, ox, 0, 0, 1, 0}, big, end, st);
     tiles += (int)ceil_div(n, big ? 256 : 128);
-    alt.count = (int)ceil_div(n, 8);
-    alt.first = v0 / 8;
+    alt.count = (int)ceil_div(n, per);
+    alt.first = v0 / per;
     alt.last = v0 + n == V;
     if (e == hipSuccess && alt.last) {
       hipLaunchKernelGGL(join_probe, dim3((unsigned)ceil_div(N, 16)), dim3(256), 0, st, part, spread, tiles, rows);

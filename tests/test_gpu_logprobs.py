@@ -230,6 +230,42 @@ def test_several_pieces_of_the_vocabulary(dtype):
 
 
 @DTYPES
+@pytest.mark.parametrize("N", [64, 65, 1100, 2049])
+@pytest.mark.parametrize("V", [6, 33, 255, 1023, 1024, 1025])
+def test_alternatives_of_few_classes(N, V, dtype):
+    """On both sides of where a row's logits are searched themselves; masked classes, copies and alike ones among them."""
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 30, V, dtype, seed=44))
+    g = torch.Generator().manual_seed(6)
+    w[V // 2:] = w[torch.randint(0, max(1, V // 4), (V - V // 2,), generator=g).cuda()]
+    b[V // 2:] = b[0]
+    b[::3] = -float("inf")
+    x[2] = 0
+    print("few classes", N, V, dtype, flush=True)
+    for top in {1, min(5, V), min(20, V), min(32, V)}:
+        _probe(x, w, b, y, top)
+
+
+def test_few_classes_in_several_pieces():
+    """fp32 rows so long that a piece of the packed vocabulary holds a part of the classes only."""
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(66, 50000, 800, torch.float32, seed=45))
+    print("few classes in pieces", flush=True)
+    _probe(x, w, b, y, 32)
+
+
+@pytest.mark.parametrize("N", [223696, 223697])
+def test_few_classes_of_many_rows(N):
+    """On both sides of where the logits of 300 classes would take more than their part of the workspace."""
+    import paper_1702_07825_amd as wn
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 8, 300, torch.float32, seed=46))
+    print("few classes of many rows", N, flush=True)
+    got = wn.head_logprobs(x, w, y, b=b, top=4)
+    for n in range(0, N, 60000):
+        want, _ = _rows(x[n:n + 60000], w, b, y[n:n + 60000], 4)
+        assert torch.equal(got[3][n:n + 60000], want["top_ids"])
+        _near(got[4][n:n + 60000], want["top_logprobs"], "top_logprobs")
+
+
+@DTYPES
 def test_each_gradient_and_each_upstream_alone(dtype):
     args = _inputs(70, 48, 300, dtype, seed=5, bias=False)
     _, all_ = _check(*args)
