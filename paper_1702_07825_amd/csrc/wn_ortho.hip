@@ -45,28 +45,79 @@ struct Matrix {
   int pack0, sym0, step0;  // first blocks of the packing, of the products that give A and B, and of the one that gives X
   int packs, syms, steps;
 };
-// Matrices of a group, in the workspace; of[block] says which matrix a block of a phase works on.
+// Matrices of a group, in the workspace.  of[block] says which matrix a block works on; each tile of a product has its matrix by
+// itself, as one load less stands before the operands' then (six small matrices 102.8 us and 101.9, 14 of width 333 156.3 and 155.0).
 struct Group {
   Matrix* matrices;
   double* squares;
-  int *of_chunk, *of_pack, *of_sym, *of_step;
+  int *of_chunk, *of_pack;
+  Matrix *of_sym, *of_step;
 };
-constexpr int kBatch = 20;
+
+// What a matrix is put together from: as many of a list as a launch's arguments hold (82 small ones in two
+// launches 158 us a call; whole descriptors took five, 172).
+struct Given {
+  Address g, out, buffers;
+  int rows, cols;
+  float scale;
+  int chunk0, pack0, sym0, step0;
+};
+constexpr int kBatch = 68;
 struct Batch {
-  Matrix m[kBatch];
-  int first;
+  Given given[kBatch];
+  int first, sym_side, step_side;  // sides of the products' tiles
 };
 static_assert(sizeof(Batch) < 3900, "kernel arguments");
 
+__host__ __device__ constexpr int tiles_of(int v, int side) { return (v + side - 1) / side; }
+__host__ __device__ constexpr size_t bytes_of(int rows, int ld) { return ((size_t)rows * ld * 2 + 255) / 256 * 256; }
+__host__ __device__ constexpr long long chunk_of(long long n) {
+  const long long c = (n + 1024 * 8 - 1) / (1024 * 8) * 8;
+  return c < 16384 ? 16384 : c;
+}
+
+__host__ __device__ inline Matrix matrix_of(const Given& v, bool sp, int sym_side, int step_side) {
+  Matrix m;
+  m.g = v.g, m.out = v.out, m.scale = v.scale;
+  m.tall = v.rows > v.cols;
+  m.m = m.tall ? v.cols : v.rows;
+  m.n = m.tall ? v.rows : v.cols;
+  const int values = chunk_values(sp);
+  m.ldm = tiles_of(m.m, values) * kChunk;
+  m.ldn = tiles_of(m.n, values) * kChunk;
+  m.x = v.buffers;
+  m.xt[0] = m.x + bytes_of(m.m, m.ldn);
+  m.xt[1] = m.xt[0] + bytes_of(m.n, m.ldm);
+  m.a = m.xt[1] + bytes_of(m.n, m.ldm);
+  m.b = m.a + bytes_of(m.m, m.ldm);
+  const long long all = (long long)m.m * m.n;
+  m.chunk = chunk_of(all);
+  m.chunk0 = v.chunk0, m.pack0 = v.pack0, m.sym0 = v.sym0, m.step0 = v.step0;
+  m.chunks = (int)((all + m.chunk - 1) / m.chunk);
+  m.packs = tiles_of(m.m, 64) * tiles_of(m.n, 64);
+  const int t = tiles_of(m.m, sym_side);
+  m.syms = t * (t + 1) / 2;
+  m.steps = tiles_of(m.m, step_side) * tiles_of(m.n, step_side);
+  return m;
+}
+
 // A block for each matrix of a batch.
+template <class E>
 __global__ __launch_bounds__(256) void put_matrices(const Batch batch, const Group g) {
-  const Matrix& m = batch.m[blockIdx.x];
+  constexpr int kWords = sizeof(Matrix) / 8;
+  static_assert(sizeof(Matrix) % 8 == 0, "words");
+  __shared__ union { Matrix m; Address words[kWords]; } s;
   const int at = batch.first + blockIdx.x;
-  if (threadIdx.x == 0) g.matrices[at] = m;
-  for (int k = threadIdx.x; k < m.chunks; k += 256) g.of_chunk[m.chunk0 + k] = at;
-  for (int k = threadIdx.x; k < m.packs; k += 256) g.of_pack[m.pack0 + k] = at;
-  for (int k = threadIdx.x; k < m.syms; k += 256) g.of_sym[m.sym0 + k] = at;
-  for (int k = threadIdx.x; k < m.steps; k += 256) g.of_step[m.step0 + k] = at;
+  if (threadIdx.x == 0) s.m = matrix_of(batch.given[blockIdx.x], sizeof(E) == 4, batch.sym_side, batch.step_side);
+  __syncthreads();
+  auto copies = [&](Matrix* to, int n) {
+    for (int k = threadIdx.x; k < n * kWords; k += 256) reinterpret_cast<Address*>(to)[k] = s.words[k % kWords];
+  };
+  copies(g.matrices + at, 1);
+  copies(g.of_sym + s.m.sym0, s.m.syms);
+  copies(g.of_step + s.m.step0, s.m.steps);
+  for (int k = threadIdx.x; k < s.m.chunks; k += 256) g.of_chunk[s.m.chunk0 + k] = at;
+  for (int k = threadIdx.x; k < s.m.packs; k += 256) g.of_pack[s.m.pack0 + k] = at;
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -346,7 +397,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group
   extern __shared__ __align__(16) char lds[];
   const int block = order.tile();
   if (block < 0) return;
-  const Matrix& m = g.matrices[(kSym ? g.of_sym : g.of_step)[block]];
+  const Matrix& m = (kSym ? g.of_sym : g.of_step)[block];
   Place pl;
   Operand oa, ob;
   if constexpr (kSym) {
@@ -403,7 +454,7 @@ struct Sides {
     ldm = padded_units(m, a.dtype == WN_F32);
     ldn = padded_units(n, a.dtype == WN_F32);
   }
-  size_t bytes() const { return up256((size_t)m * ldn * 2) + 2 * up256((size_t)n * ldm * 2) + 2 * up256((size_t)m * ldm * 2); }
+  size_t bytes() const { return bytes_of(m, ldn) + 2 * bytes_of(n, ldm) + 2 * bytes_of(m, ldm); }  // (as matrix_of lays them out)
 };
 inline bool empty(const wn_ortho_array& a) { return a.rows == 0 || a.cols == 0; }
 
@@ -441,11 +492,10 @@ struct GroupPlan {
   size_t buffers = 0;
   // Bytes of all: descriptors, indexes, sums and buffers.
   size_t total() const {
-    return up256(arrays.size() * sizeof(Matrix)) + up256(chunks * 8) + up256(chunks * 4) + up256(packs * 4) + up256(syms * 4) +
-           up256(steps * 4) + buffers;
+    return up256(arrays.size() * sizeof(Matrix)) + up256(chunks * 8) + up256(chunks * 4) + up256(packs * 4) +
+           up256(syms * sizeof(Matrix)) + up256(steps * sizeof(Matrix)) + buffers;
   }
 };
-inline long long chunk_of(long long n) { return std::max<long long>(16384, (long long)ceil_div((size_t)n, 1024 * 8) * 8); }
 
 GroupPlan next_group(int n_arrays, const wn_ortho_array* arrays, int dtype, int& at) {
   GroupPlan p;
@@ -513,38 +563,23 @@ hipError_t run_group(const GroupPlan& p, const wn_ortho_array* arrays, int steps
   g.squares = reinterpret_cast<double*>(ws + c.take(p.chunks * 8));
   g.of_chunk = reinterpret_cast<int*>(ws + c.take(p.chunks * 4));
   g.of_pack = reinterpret_cast<int*>(ws + c.take(p.packs * 4));
-  g.of_sym = reinterpret_cast<int*>(ws + c.take(p.syms * 4));
-  g.of_step = reinterpret_cast<int*>(ws + c.take(p.steps * 4));
+  g.of_sym = reinterpret_cast<Matrix*>(ws + c.take(p.syms * sizeof(Matrix)));
+  g.of_step = reinterpret_cast<Matrix*>(ws + c.take(p.steps * sizeof(Matrix)));
   int chunks = 0, packs = 0, syms = 0, products = 0;
   Batch batch;
+  batch.sym_side = kTileSides[p.sym];
+  batch.step_side = kTileSides[p.step];
   for (size_t at = 0; at < p.arrays.size();) {
     batch.first = (int)at;
     int n = 0;
     for (; n < kBatch && at < p.arrays.size(); ++n, ++at) {
       const wn_ortho_array& a = arrays[p.arrays[at]];
-      const Sides s(a);
-      Matrix& m = batch.m[n];
-      auto units = [&](int rows, int ld) { return reinterpret_cast<Address>(ws + c.take((size_t)rows * ld * 2)); };
-      m.g = reinterpret_cast<Address>(a.g);
-      m.out = reinterpret_cast<Address>(a.out);
-      m.x = units(s.m, s.ldn);
-      m.xt[0] = units(s.n, s.ldm);
-      m.xt[1] = units(s.n, s.ldm);
-      m.a = units(s.m, s.ldm);
-      m.b = units(s.m, s.ldm);
-      m.m = s.m, m.n = s.n, m.ldm = s.ldm, m.ldn = s.ldn, m.tall = s.tall;
-      m.scale = a.scale;
-      const long long all = (long long)s.m * s.n;
-      m.chunk = chunk_of(all);
-      m.chunk0 = chunks, m.pack0 = packs, m.sym0 = syms, m.step0 = products;
-      m.chunks = (int)ceil_div((size_t)all, (size_t)m.chunk);
-      m.packs = (int)(ceil_div(s.m, 64) * ceil_div(s.n, 64));
-      const int tm = (int)side_tiles(s.m, p.sym);
-      m.syms = tm * (tm + 1) / 2;
-      m.steps = (int)(side_tiles(s.m, p.step) * side_tiles(s.n, p.step));
+      const Address buffers = reinterpret_cast<Address>(ws + c.take(Sides(a).bytes()));
+      batch.given[n] = {reinterpret_cast<Address>(a.g), reinterpret_cast<Address>(a.out), buffers, a.rows, a.cols, a.scale, chunks, packs, syms, products};
+      const Matrix m = matrix_of(batch.given[n], sizeof(E) == 4, batch.sym_side, batch.step_side);
       chunks += m.chunks, packs += m.packs, syms += m.syms, products += m.steps;
     }
-    hipLaunchKernelGGL(put_matrices, dim3(n), dim3(256), 0, st, batch, g);
+    hipLaunchKernelGGL(put_matrices<E>, dim3(n), dim3(256), 0, st, batch, g);
   }
   hipLaunchKernelGGL(squares<E>, dim3(chunks), dim3(256), 0, st, g);
   hipLaunchKernelGGL(pack<E>, dim3(packs), dim3(256), 0, st, g, (double)eps);
