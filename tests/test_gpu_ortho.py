@@ -117,6 +117,54 @@ def test_a_list_of_many():
 
 
 @DTYPES
+def test_a_list_described_by_several_launches(dtype):
+    """150 matrices of one dtype, wide and tall, each with a scale of its own."""
+    import paper_1702_07825_amd as wn
+    gs = [_matrix(1 + i % 71, 1 + (7 * i) % 67, dtype, seed=300 + i) for i in range(150)]
+    scales = [0.01 * (i + 1) * (-1) ** i for i in range(150)]
+    got = wn.orthogonalize(gs, scales=scales)
+    for g, s, o in zip(gs, scales, got):
+        _near(o, g, scale=s)
+
+
+@pytest.mark.parametrize("tall", [True, False])
+def test_offsets_beyond_32_bits(tall):
+    """More than 2^31 elements, one step: some of the outputs, on both sides of element 2^31, against 64 bits.  Columns X_c of X [m][n] come
+    out as B X_c, so they are off by |err B| |X_c| + |B|_2 h |X_c| + h |new| + K(m) | |B| |X_c| | with err B as above."""
+    import paper_1702_07825_amd as wn
+    m, n, (a, b, c), h = 8193, 1 << 18, (3.0, -2.0, 0.5), 2.0 ** -11
+    gen = torch.Generator(device="cuda").manual_seed(70)
+    g = torch.empty((n, m) if tall else (m, n), dtype=torch.bfloat16, device="cuda")
+    for k in range(0, g.shape[0], 4096):
+        g[k:k + 4096] = torch.randn(g[k:k + 4096].shape, generator=gen, device="cuda").bfloat16()
+    print("offsets", tuple(g.shape), flush=True)
+    got = wn.orthogonalize([g], coefficients=[(a, b, c)])[0]
+
+    def columns(t, k0, k1):
+        return (t[k0:k1].t() if tall else t[:, k0:k1]).double().contiguous()
+
+    A, A1 = (torch.zeros((m, m), dtype=torch.float64, device="cuda") for _ in range(2))
+    for k in range(0, n, 1 << 15):
+        x = columns(g, k, k + (1 << 15))
+        A += x @ x.t().contiguous()
+        A1 += x.abs() @ x.abs().t().contiguous()
+    norm = float(A.diagonal().sum()) ** 0.5 + 1e-7
+    A, A1 = A / norm ** 2, A1 / norm ** 2
+    s2 = _largest(A)
+    B = a * torch.eye(m, dtype=torch.float64, device="cuda") + b * A + c * A @ A
+    eA = 2 * h * s2 ** 0.5 + h * float(A.norm()) + n * U * float(A1.norm()) + 2.0 ** -37 * m
+    eB = (abs(b) + 2 * abs(c) * s2) * eA + h * float(B.norm()) + c * m * U * float((A.abs() @ A.abs()).norm()) + 2.0 ** -35 * m
+    top = abs(a) + abs(b) * s2 + abs(c) * s2 ** 2
+    for k in (0, (1 << 31) // m - 30, n // 2, n - 64):
+        x = columns(g, k, k + 64) / norm
+        want = B @ x
+        e = eB * float(x.norm()) + top * h * float(x.norm()) + h * float(want.norm()) + m * U * float((B.abs() @ x.abs()).norm())
+        tol = 1.1 * (e + 2.0 ** -37 * (64 * m) ** 0.5) + 2.0 ** -8 * float(want.norm())
+        assert float((columns(got, k, k + 64) - want).norm()) <= tol, (k, tol, float(want.norm()))
+        assert float(want.norm()) > 5 * tol, (k, tol)
+
+
+@DTYPES
 def test_several_groups(dtype):
     """More than 4 GiB of buffers: the matrices go through in groups that share the workspace."""
     import paper_1702_07825_amd as wn
