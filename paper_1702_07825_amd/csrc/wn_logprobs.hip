@@ -24,6 +24,8 @@ constexpr size_t kGroupsBytes = (size_t)256 << 20;  // of the groups' largest lo
 __host__ __device__ constexpr int kept(int top) { return top + 2 + top / 8; }
 static_assert(kept(kMostTop) <= 64, "a lane for each");
 
+// Bound: the product, as in the loss.  Measured: 8192 rows x 65536 classes x 2048 in bf16 1.72 to 1.78 ms (the loss's end 1.69
+// to 1.78), 4096 x 65536 x 1024 with alternatives 546 to 595 us, 16000 x 256 x 256 in fp32 17 (without 14.5).
 struct ProbeEnd {
   static constexpr bool kScaledByTile = false;
   Logits l;
@@ -330,6 +332,9 @@ __device__ __forceinline__ S class_logits(const Alternatives& a, int n, const in
 // groups, are computed in 64 and ranked by counting.  (All of the groups' classes in 64 at once, a round of loads less, takes
 // few rows longer: 1 row x 32000 classes x 2048, 5 alternatives 51 us and not 48, 100 x 16000 x 4096, 32 of them 216 and not
 // 178.)  For few rows the block joins its row's statistics first.
+// Bound: many rows by reading the groups and the classes' rows of w (4096 rows x 65536 classes x 1024, bf16, 8 alternatives: 134 MB
+// and 0.74 GB, most of it from the caches, 199 us; 16000 x 256 x 256 in fp32, 3: 37); few rows by a chain of some ten reads and
+// reductions (1 x 32000 x 2048, bf16, 5: 26 us).
 template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
   constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
@@ -360,11 +365,27 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
       best[tid] = {-INFINITY, kNone};
     }
     __syncthreads();
+    // An entry's rank: how many of each list, all sorted, are before it.  (Compared with every entry, one after the other in
+    // LDS, 1 row x 32000 classes x 2048 with 20 alternatives took 77 us and not 58, 37 x 50021 x 777 with 20 127 and not 109.)
     const int all = (kWaves + 1) * want;
     for (int i = tid; i < all; i += kThreads) {
       const Group e = found[i];
+      int ahead[kWaves + 1];
+#pragma unroll
+      for (int l = 0; l <= kWaves; ++l) ahead[l] = 0;
+#pragma unroll 1
+      for (int h = 32; h; h >>= 1)
+#pragma unroll
+        for (int l = 0; l <= kWaves; ++l) {
+          // (without a branch: hipcc 7.2 made wrong code of one, entries of equal values had the same rank)
+          const int k = ahead[l] + h;
+          const Group o = found[l * want + min(k, want) - 1];
+          const int in = (int)(k <= want) & ((int)(o.v > e.v) | ((int)(o.v == e.v) & (int)(o.g < e.g)));
+          ahead[l] += in * h;
+        }
       int rank = 0;
-      for (int k = 0; k < all; ++k) rank += before(found[k], e);
+#pragma unroll
+      for (int l = 0; l <= kWaves; ++l) rank += ahead[l];
       if (e.g != kNone && rank < want) best[rank] = e;
     }
   }
@@ -408,6 +429,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
       for (int i = lane; i < m; i += 64) {
         const Group e = near[i];
         int rank = 0;
+#pragma unroll 8
         for (int k = 0; k < m; ++k) rank += before(near[k], e);
         if (rank < want) pick[rank] = e;
       }
@@ -432,6 +454,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
   const double l = logit[tid];
   int rank = 0;
   double most = -INFINITY;
+#pragma unroll 4
   for (int k = 0; k < picked; ++k) {
     const int o = chosen[k].g;
     const double ol = logit[k];
@@ -488,8 +511,9 @@ struct Probe {
 
 // Waves of a row.  Few rows leave the chip empty, so a row takes many; many rows of few groups take one each, which has no
 // other to wait for.  Measured with 1, 4 and 8 waves (us beside the call without alternatives): 1 row x 32000 classes x
-// 2048, 5 alternatives 53, 22, 22 and 20 of them 124, 50, 51; 37 x 50021 x 777 in fp32, 20: 142, 59, 49; 300 x 32000 x 1024, 5: 49,
-// 25, 46; 1000 x 32000 x 1024, 20: 117, 95, 205; 4096 x 65536 x 1024, 8: 226, 184, 469; 16000 x 256 x 256 in fp32, 3: 56, 108, 455.
+// 2048, 5 alternatives 55, 20, 19 and 20 of them 124, 41, 34; 37 x 50021 x 777 in fp32, 20: 138, 51, 36; 128 x 32000 x 1024 in
+// fp32, 5: 59, 34, 34; 300 x 32000 x 1024, 5: 51, 23, 39; 1000 x 32000 x 1024, 20: 113, 82, 132; 4096 x 65536 x 1024, 8: 225,
+// 203, 410; 2000 x 256 x 256 in fp32, 3: 10, 15, 47; 16000 of them 31, 72, 364.
 template <class E>
 hipError_t launch_alternatives(const Alternatives& a, hipStream_t st) {
   if (a.N <= 128) hipLaunchKernelGGL((alternatives<E, 8>), dim3(a.N), dim3(512), 0, st, a);

@@ -128,7 +128,8 @@ __device__ __forceinline__ double block_sum(double v) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Squares in 64 bits: fp32 values neither overflow nor vanish.  A block for each chunk of a matrix.
+// Squares in 64 bits: fp32 values neither overflow nor vanish.  A block for each chunk of a matrix.  Bound: reading them
+// (26 bf16 matrices, 457 MB: 89 us, 5.1 TB/s).
 template <class E>
 __global__ __launch_bounds__(256) void squares(const Group g) {
   const Matrix& m = g.matrices[g.of_chunk[blockIdx.x]];
@@ -192,7 +193,8 @@ __device__ __forceinline__ f32x4 get4(const u16* row, int k) {
 template <bool SP>
 __device__ __forceinline__ int values_of(int units) { return SP ? units / 2 : units; }
 
-// X = G / (|G| + eps) in both orders, 64 x 64 values per block; zeros behind a row's values.
+// X = G / (|G| + eps) in both orders, 64 x 64 values per block; zeros behind a row's values.  Bound: reading G and writing
+// twice as much (26 bf16 matrices, 1.37 GB in all: 356 us, 3.9 TB/s).
 template <class E>
 __global__ __launch_bounds__(256) void pack(const Group g, double eps) {
   constexpr bool SP = sizeof(E) == 4;
@@ -391,6 +393,10 @@ struct Order {
   }
 };
 
+// A phase of all matrices.  Bound: large matrices by the matrix units (busy 51 % of the cycles), small ones by the chain of a
+// launch's loads and stores.  Measured: 26 matrices of widths 2048 and 8192 in bf16, a step: X X' 461 us and B X 947, 1.0
+// PFLOP/s (of the triangle with its diagonal tiles; a plain library product of 16384^3 1.6), the polynomial 283; the smallest lists
+// 6 to 7 us a phase.
 template <class T, class E, int kPhase>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group g, const Step s, const Order order) {
   constexpr bool SP = sizeof(E) == 4, kSym = kPhase <= kPoly;

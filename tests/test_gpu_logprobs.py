@@ -201,6 +201,17 @@ def test_equal_classes_come_in_order(N, V, dtype):
 
 
 @DTYPES
+@pytest.mark.parametrize("N", [9, 128, 129, 2050])
+def test_equal_classes_of_several_segments(N, dtype):
+    """Copies all over a vocabulary whose groups several waves search, for each number of waves."""
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 16, 20000, dtype, seed=47))
+    w = w[:300].repeat(67, 1)[:20000].contiguous()
+    b[:] = -1.5
+    for top in (1, 2, 8, 32):
+        _probe(x, w, b, y, top)
+
+
+@DTYPES
 @pytest.mark.parametrize("rising", [True, False])
 @pytest.mark.parametrize("N,V", [(2, 40000), (80, 40000)])
 def test_classes_in_order_of_their_logits(N, V, rising, dtype):
