@@ -333,8 +333,8 @@ __device__ __forceinline__ S class_logits(const Alternatives& a, int n, const in
 // few rows longer: 1 row x 32000 classes x 2048, 5 alternatives 51 us and not 48, 100 x 16000 x 4096, 32 of them 216 and not
 // 178.)  For few rows the block joins its row's statistics first.
 // Bound: many rows by reading the groups and the classes' rows of w (4096 rows x 65536 classes x 1024, bf16, 8 alternatives: 134 MB
-// and 0.74 GB, most of it from the caches, 199 us; 16000 x 256 x 256 in fp32, 3: 37); few rows by a chain of some ten reads and
-// reductions (1 x 32000 x 2048, bf16, 5: 26 us).
+// and 0.74 GB, most of it from the caches, 177 us; 16000 x 256 x 256 in fp32, 3: 37); few rows by a chain of some ten reads and
+// reductions (1 x 32000 x 2048, bf16, 5: 22 us).
 template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
   constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
