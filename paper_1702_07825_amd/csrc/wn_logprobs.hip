@@ -513,11 +513,13 @@ struct Probe {
 // other to wait for.  Measured with 1, 4 and 8 waves (us beside the call without alternatives): 1 row x 32000 classes x
 // 2048, 5 alternatives 55, 20, 19 and 20 of them 124, 41, 34; 37 x 50021 x 777 in fp32, 20: 138, 51, 36; 128 x 32000 x 1024 in
 // fp32, 5: 59, 34, 34; 300 x 32000 x 1024, 5: 51, 23, 39; 1000 x 32000 x 1024, 20: 113, 82, 132; 4096 x 65536 x 1024, 8: 225,
-// 203, 410; 2000 x 256 x 256 in fp32, 3: 10, 15, 47; 16000 of them 31, 72, 364.
+// 203, 410; 16000 x 256 x 256 in fp32, 3: 31, 72, 364.  The chip holds 1536 blocks of 4 waves at a time, and rows of one segment
+// beyond that take one wave (1 and 4): 1536 x 1000 x 1024, 20 31 and 28, 1537 of them 31 and 37; 1536 x 8000 x 1024, 5 38 and 37,
+// 1537 38 and 44.
 template <class E>
 hipError_t launch_alternatives(const Alternatives& a, hipStream_t st) {
   if (a.N <= 128) hipLaunchKernelGGL((alternatives<E, 8>), dim3(a.N), dim3(512), 0, st, a);
-  else if (a.N <= 2048 || a.count > 64 * kSegment) hipLaunchKernelGGL((alternatives<E, 4>), dim3(a.N), dim3(256), 0, st, a);
+  else if (a.N <= 1536 || a.count > 64 * kSegment) hipLaunchKernelGGL((alternatives<E, 4>), dim3(a.N), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((alternatives<E, 1>), dim3(a.N), dim3(64), 0, st, a);
   return hipGetLastError();
 }

@@ -256,6 +256,15 @@ def test_alternatives_of_few_classes(N, V, dtype):
         _probe(x, w, b, y, top)
 
 
+@DTYPES
+@pytest.mark.parametrize("V", [300, 8000])
+@pytest.mark.parametrize("N", [1536, 1537])
+def test_alternatives_where_a_row_takes_one_wave(N, V, dtype):
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 40, V, dtype, seed=48))
+    for top in (1, 32):
+        _probe(x, w, b, y, top)
+
+
 def test_few_classes_in_several_pieces():
     """fp32 rows so long that a piece of the packed vocabulary holds a part of the classes only."""
     x, w, b, y, _, _ = (t.cuda() for t in _inputs(66, 50000, 800, torch.float32, seed=45))
