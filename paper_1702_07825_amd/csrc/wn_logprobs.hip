@@ -8,10 +8,10 @@
 //
 // Alternatives: the end also leaves the largest logit of every 8 classes.  The K likeliest classes lie in the K groups of
 // 8 whose largest logits are largest (any K classes from K other groups would be less likely), so a row's groups are
-// searched for a few more than K (kept()), and their classes' logits are computed anew, in 64 bits.  (Of up to 1024 classes
-// each is a group by itself, see group_of.)  So the logits of many classes are neither kept nor sorted, classes next to
-// each other are in order although the product's sums are of 32 bits, and equal ones (copies of a row of w) are equal: the
-// lowest index comes first.
+// searched for a few more than K (kept()), and their classes' logits are computed anew: in 32 bits with a bound of their
+// rounding, and those in 64 that may be among the K by it.  (Of up to 1024 classes each is a group by itself, see group_of.)
+// So the logits of many classes are neither kept nor sorted, classes next to each other are in order although the product's
+// sums are of 32 bits, and equal ones (copies of a row of w) are equal: the lowest index comes first.
 #include "wn_product.h"
 
 namespace {
@@ -20,7 +20,8 @@ constexpr int kMostTop = 32;
 constexpr size_t kGroupsBytes = (size_t)256 << 20;  // of the groups' largest logits of a piece: they stay in the last-level cache
 
 // Groups of 8 classes kept for `top` alternatives: more than `top`, since a group's largest logit is off by the product's
-// rounding.  Classes are missed only if more groups than the surplus lie within that rounding of the last one wanted.
+// rounding.  Classes are missed only if more groups than the surplus lie within that rounding of the last one wanted.  (Of a
+// group that is kept every class may be an alternative.)
 __host__ __device__ constexpr int kept(int top) { return top + 2 + top / 8; }
 static_assert(kept(kMostTop) <= 64, "a lane for each");
 
@@ -270,14 +271,16 @@ __device__ __forceinline__ Group join_segment(const float (&v)[kSegment], int fi
   return lane < want && lane < n ? room[lane] : Group{-INFINITY, kNone};
 }
 
-// C classes' logits, summed in S by a wave: lanes 64 / C c .. of it end with class v[c]'s.
+// C classes' logits, summed in S by a wave: lanes 64 / C c .. of it end with class v[c]'s.  `size`, in 32 bits: sum |x w| over all
+// C, of which each class's is a part.
 template <class E, class S, int C, int kAhead>
-__device__ __forceinline__ S class_logits(const Alternatives& a, int n, const int (&v)[C]) {
+__device__ __forceinline__ S class_logits(const Alternatives& a, int n, const int (&v)[C], float* size = nullptr) {
   constexpr int W = Piece<E>::n;
   const int lane = threadIdx.x & 63;
   const E* x = static_cast<const E*>(a.x) + (size_t)n * a.D;
   const E* w[C];
   S sum[C];
+  float all[2] = {0.f, 0.f};
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     sum[c] = 0;
@@ -288,7 +291,10 @@ __device__ __forceinline__ S class_logits(const Alternatives& a, int n, const in
     for (int k = 0; k < W; ++k) {
       const S xs = value(xv[k]);
 #pragma unroll
-      for (int c = 0; c < C; ++c) sum[c] += xs * (S)value(wv[c][k]);
+      for (int c = 0; c < C; ++c) {
+        sum[c] += xs * (S)value(wv[c][k]);
+        if (size) all[c & 1] = fmaf(fabsf(value(xv[k])), fabsf(value(wv[c][k])), all[c & 1]);
+      }
     }
   };
   const int whole = a.D / (64 * W) * (64 * W);
@@ -324,14 +330,19 @@ __device__ __forceinline__ S class_logits(const Alternatives& a, int n, const in
 #pragma unroll
   for (int c = 1; c < C; ++c) mine = lane / (64 / C) == c ? v[c] : mine;
   if (a.b) s += (S)a.b[mine];
+  if (size) *size = wnk::wave_sum(all[0] + all[1]);
   return s;
 }
+// A class's logit of 32 bits is off by `off`, in its sum, and by the roundings of the bias's addition and of what is computed
+// here, 2^-22 of itself: it lies between these two.  (An infinity stays one.)
+__device__ __forceinline__ float at_least(float l, float off) { return fminf(l * (1.f - 0x1p-22f), l * (1.f + 0x1p-22f)) - off; }
+__device__ __forceinline__ float at_most(float l, float off) { return fmaxf(l * (1.f - 0x1p-22f), l * (1.f + 0x1p-22f)) + off; }
 
 // A block per row.  The waves find the largest groups of their segments, which are then joined; in the last piece, unless
-// the groups are single classes, they compute the logits of these groups' classes in 32 bits.  The largest, as many as
-// groups, are computed in 64 and ranked by counting.  (All of the groups' classes in 64 at once, a round of loads less, takes
-// few rows longer: 1 row x 32000 classes x 2048, 5 alternatives 51 us and not 48, 100 x 16000 x 4096, 32 of them 216 and not
-// 178.)  For few rows the block joins its row's statistics first.
+// the groups are single classes, they compute the logits of these groups' classes in 32 bits.  At least `top` of them are at
+// least at_least() of the top-th largest, so a class that is less at most is none of the alternatives; the others, hardly more than
+// `top` unless classes are nearly alike, are computed in 64 and ranked by counting.  For few rows the block joins its row's
+// statistics first.
 // Bound: many rows by reading the groups and the classes' rows of w (4096 rows x 65536 classes x 1024, bf16, 8 alternatives: 134 MB
 // and 0.74 GB, most of it from the caches, 177 us; 16000 x 256 x 256 in fp32, 3: 37); few rows by a chain of some ten reads and
 // reductions (1 x 32000 x 2048, bf16, 5: 22 us).
@@ -339,22 +350,23 @@ template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
   constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
   __shared__ Group found[(kWaves + 1) * kMostKept], best[kMostKept], room[kWaves][64];
-  __shared__ Group near[kMostKept * 8], pick[kMostKept];  // classes by their logits in 32 bits
-  __shared__ float top_of[kMostKept];
-  __shared__ double logit[kMostKept];
+  __shared__ union { Group near[kMostKept * 8]; double logit[kMostKept * 8]; } s;  // (near is done with before the first logit)
+  __shared__ Group pick[kMostKept * 8];  // classes by their logits in 32 bits, the largest first
+  __shared__ float top_of[kMostKept], size_of[kMostKept];
+  __shared__ int many;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x, want = kept(a.top);
   float z = 0.f;
   if (a.part) z = a.rows.put(n, join_tiles<kThreads>(a.part, a.spread, a.tiles, a.N, n));
   const float* groups = a.groups + (size_t)n * a.count;
   Group mine{-INFINITY, kNone};
-  for (int s = wave * 64 * kSegment; s < a.count; s += kThreads * kSegment) {
+  for (int at = wave * 64 * kSegment; at < a.count; at += kThreads * kSegment) {
     float v[kSegment];
 #pragma unroll
     for (int k = 0; k < kSegment; ++k) {
-      const int i = s + k * 64 + lane;
+      const int i = at + k * 64 + lane;
       v[k] = fmaxf(i < a.count ? groups[i] : -INFINITY, -INFINITY);  // (a NaN would be neither before nor behind another)
     }
-    mine = join_segment(v, a.first + s, a.count - s, mine, want, room[wave]);
+    mine = join_segment(v, a.first + at, a.count - at, mine, want, room[wave]);
   }
   if (a.count <= 64 * kSegment && !a.seen) {
     if (tid < want) best[tid] = mine;
@@ -401,43 +413,49 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
     for (int k = wave; k < want; k += kWaves) {
       const int g = best[k].g, c = lane >> 3;
       Group e{-INFINITY, kNone};
+      float size = 0.f;
       if (g != kNone) {
         int v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = min(g * 8 + i, a.V - 1);
-        const float l = class_logits<E, float, 8, kAhead>(a, n, v);
+        const float l = class_logits<E, float, 8, kAhead>(a, n, v, &size);
         if (g * 8 + c < a.V) e = {fmaxf(l, -INFINITY), g * 8 + c};
       }
-      if ((lane & 7) == 0) near[k * 8 + c] = e;
+      if ((lane & 7) == 0) s.near[k * 8 + c] = e;
       const float m = wnk::wave_max(e.v);
-      if (lane == 0) top_of[k] = m;
+      if (lane == 0) top_of[k] = m, size_of[k] = size;
     }
     __syncthreads();
-    // the want largest of them reach the least of the groups' largest
     if (wave == 0) {
-      const float t = -wnk::wave_max(lane < want ? -top_of[lane] : -INFINITY);
+      // A lane adds up D / 64 terms and a piece at most, then come 6 sums of lanes.  (Where it overflows every class stays in.)
+      const float off = (float)(a.D / 64 + 16) * 0x1.04p-24f * wnk::wave_max(lane < want ? size_of[lane] : 0.f);
+      // as many classes as groups reach the least of the groups' largest
+      const float t = -wnk::wave_max(lane < want ? -top_of[lane] : -INFINITY), low = at_least(t, off);
       int m = 0;
       for (int i = 0; i < want * 8; i += 64) {
-        const Group e = i + lane < want * 8 ? near[i + lane] : Group{-INFINITY, kNone};
-        const bool in = e.g != kNone && e.v >= t;
+        const Group e = i + lane < want * 8 ? s.near[i + lane] : Group{-INFINITY, kNone};
+        const bool in = e.g != kNone && !(at_most(e.v, off) < low);
         const unsigned long long all = __ballot(in);
         asm volatile("" ::: "memory");
-        if (in) near[m + __popcll(all & ((1ull << lane) - 1))] = e;  // (never behind what is still to be read)
+        if (in) s.near[m + __popcll(all & ((1ull << lane) - 1))] = e;  // (never behind what is still to be read)
         m += __popcll(all);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       for (int i = lane; i < m; i += 64) {
-        const Group e = near[i];
+        const Group e = s.near[i];
         int rank = 0;
 #pragma unroll 8
-        for (int k = 0; k < m; ++k) rank += before(near[k], e);
-        if (rank < want) pick[rank] = e;
+        for (int k = 0; k < m; ++k) rank += before(s.near[k], e);
+        pick[rank] = e;
       }
-      picked = min(m, want);
-      if (lane == 0) top_of[0] = __int_as_float(picked);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const float last = at_least(pick[a.top - 1].v, off);
+      int c = 0;
+      for (int i = 0; i < m; i += 64) c += __popcll(__ballot(i + lane < m && !(at_most(pick[min(i + lane, m - 1)].v, off) < last)));
+      if (lane == 0) many = c;
     }
     __syncthreads();
-    picked = __float_as_int(top_of[0]);
+    picked = many;
   }
   for (int k = wave * 4; k < picked; k += kWaves * 4) {
     int v[4];
@@ -445,26 +463,27 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
     for (int i = 0; i < 4; ++i) v[i] = chosen[min(k + i, picked - 1)].g;
     const double l = class_logits<E, double, 4, kAhead>(a, n, v);
     if ((lane & 15) == 0 && k + (lane >> 4) < picked)
-      logit[k + (lane >> 4)] = l == l ? l : -INFINITY;  // (where a logit is a NaN, log s is, and so is what comes out)
+      s.logit[k + (lane >> 4)] = l == l ? l : -INFINITY;  // (where a logit is a NaN, log s is, and so is what comes out)
   }
   __syncthreads();
-  if (tid >= picked) return;  // (of the first wave: it has a lane for each)
   if (!a.part) z = a.log_s[n];
-  const int v = chosen[tid].g;
-  const double l = logit[tid];
-  int rank = 0;
-  double most = -INFINITY;
+  for (int i = tid; i < picked; i += kThreads) {
+    const int v = chosen[i].g;
+    const double l = s.logit[i];
+    int rank = 0;
+    double most = -INFINITY;
 #pragma unroll 4
-  for (int k = 0; k < picked; ++k) {
-    const int o = chosen[k].g;
-    const double ol = logit[k];
-    rank += ol > l || (ol == l && o < v);
-    most = fmax(most, ol);
+    for (int k = 0; k < picked; ++k) {
+      const int o = chosen[k].g;
+      const double ol = s.logit[k];
+      rank += ol > l || (ol == l && o < v);
+      most = fmax(most, ol);
+    }
+    if (rank >= a.top) continue;
+    a.ids[(size_t)n * a.top + rank] = v;
+    // (the row's largest logit is taken off as it is here, not as the product rounded it: no log probability is above 0)
+    a.logprobs[(size_t)n * a.top + rank] = (float)((l - most) - (double)z);
   }
-  if (rank >= a.top) return;
-  a.ids[(size_t)n * a.top + rank] = v;
-  // (the row's largest logit is taken off as it is here, not as the product rounded it: no log probability is above 0)
-  a.logprobs[(size_t)n * a.top + rank] = (float)((l - most) - (double)z);
 }
 
 // ------------------------------------------------------------------------------------------------

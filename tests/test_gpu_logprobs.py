@@ -265,6 +265,43 @@ def test_alternatives_where_a_row_takes_one_wave(N, V, dtype):
         _probe(x, w, b, y, top)
 
 
+@DTYPES
+@pytest.mark.parametrize("N,V", [(1, 3000), (64, 300), (65, 1030), (200, 3000), (1600, 3000)])
+def test_classes_of_a_group_closer_than_fp32_rounds(N, V, dtype):
+    """Eight classes beside each other, far above the others, whose rows differ where x is tiny: their logits of about 16, whose
+    sums in 32 bits are off by some 2^-20, lie 2^-22 apart."""
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 2048, V, dtype, seed=49))
+    at = 8 * (V // 16)
+    w[at:at + 8] = w[at]
+    x.copy_((x.float() + 7 * w[at].float()).to(dtype))
+    b[at:at + 8] = 1.0
+    x[:, 5::400] = (x[:, 5::400].float() * 2.0 ** -21).to(dtype)
+    w[at:at + 8, 5::400] = torch.randn(w[at:at + 8, 5::400].shape, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    l = x.double() @ w[at:at + 8].double().t().contiguous()
+    l = l.sort(dim=1).values
+    gap = l[:, 1:] - l[:, :-1]
+    assert float(gap.min()) > 1e-12 and float(gap.median()) < 2.0 ** -20 and float(l.min()) > 8
+    for top in (1, 5, 8, 12):
+        got, _ = _probe(x, w, b, y, top)
+        n = min(top, 8)
+        assert bool(((got[3][:, :n] >= at) & (got[3][:, :n] < at + 8)).all())
+
+
+@DTYPES
+@pytest.mark.parametrize("N,V", [(20, 300), (64, 2000), (100, 2000), (300, 2000), (1600, 2000)])
+def test_candidates_by_the_hundred(N, V, dtype):
+    """Terms of 2^17 that cancel exactly, in 32 columns of their own: the logits are as exact as without, but no bound of
+    their rounding can tell so, and most of the groups' classes are candidates."""
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 160, V, dtype, seed=53))
+    x[:, :32] = 0
+    w[:, :32] = 0
+    x[:, :2] = 2.0 ** 17
+    w[:, 0] = 1
+    w[:, 1] = -1
+    for top in (1, 5, 32):
+        _probe(x, w, b, y, top)
+
+
 def test_few_classes_in_several_pieces():
     """fp32 rows so long that a piece of the packed vocabulary holds a part of the classes only."""
     x, w, b, y, _, _ = (t.cuda() for t in _inputs(66, 50000, 800, torch.float32, seed=45))
