@@ -707,7 +707,9 @@ def orthogonalize(updates, scales=None, coefficients=MUON_COEFFICIENTS, eps: flo
     if not dense:
         raise ValueError("updates must be contiguous")
     arrays = np.zeros(n, dtype=_ORTHO_ARRAY)
-    arrays["scale"] = 1.0 if scales is None else scales  # (numpy refuses a list of another length)
+    if np.ndim(scales) and np.shape(scales) != (n,):  # (numpy would take one of a single number for all)
+        raise ValueError("scales must be a number or one for each of the %d updates" % n)
+    arrays["scale"] = 1.0 if scales is None else scales
     if outs is None:
         outs = [on.empty(s, d) for s, d in zip(shapes, dtypes)]
     else:

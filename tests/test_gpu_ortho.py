@@ -357,3 +357,16 @@ def test_refusals():
         with pytest.raises((ValueError, TypeError, wn.WnError)):
             f()
             raise AssertionError(k)
+
+
+def test_scales_are_one_for_each_matrix_or_a_number():
+    import paper_1702_07825_amd as wn
+    gs = [_matrix(8, 6, torch.float32, seed=k) for k in range(3)]
+    for scales in ([0.5], (0.5,), np.array([0.5]), torch.tensor([0.5]), [], [1.0, 2.0], [1.0] * 4, [[1.0], [2.0], [3.0]], [[1.0, 2.0, 3.0]]):
+        with pytest.raises((ValueError, TypeError)):
+            wn.orthogonalize(gs, scales=scales)
+    want = wn.orthogonalize(gs)
+    for scales in (0.5, np.float32(0.5), torch.tensor(0.5), [0.5] * 3, (0.5,) * 3, np.full(3, 0.5), torch.full((3,), 0.5)):
+        for a, b in zip(wn.orthogonalize(gs, scales=scales), want):
+            assert torch.equal(a, 0.5 * b)
+    assert torch.equal(wn.orthogonalize(gs[:1], scales=[0.5])[0], 0.5 * want[0])
