@@ -326,11 +326,11 @@ struct Keep {
   }
 };
 
-// out[b][a] = alpha (sum).
+// out[b][a] = scale (alpha sum), alpha a power of two (alpha scale may lie below fp32's smallest normal value).
 template <class E>
 struct Result {
   static constexpr bool kScaledByTile = false;
-  float alpha;
+  float alpha, scale;
   E* out;  // [B][A]
   int A, B;
   template <class T>
@@ -343,7 +343,7 @@ struct Result {
       for (int i = 0; i < T::NA; ++i) {
         const int a = pl.a0 + 16 * i + 4 * pl.quad;
         if (a >= A) continue;
-        const f32x4 v = times(acc[i][j], alpha);
+        const f32x4 v = times(times(acc[i][j], alpha), scale);
         E* d = out + (size_t)b * A + a;
         if (a + 3 < A) {
           if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4u*>(d) = f32x4u{v[0], v[1], v[2], v[3]};
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group
   f32x4 acc[T::NA][T::NB];
   auto exp2i = [](int e) { return __uint_as_float((unsigned)(127 + e) << 23); };
   if constexpr (kPhase == kLast) {
-    const Result<E> end{m.scale * exp2i(-kB - kX), in_memory<E>(m.out), (int)oa.rows, (int)ob.rows};
+    const Result<E> end{exp2i(-kB - kX), m.scale, in_memory<E>(m.out), (int)oa.rows, (int)ob.rows};
     tile_sums<T, SP, f16x8>(acc, oa, ob, pl, 0, oa.k / kChunk, lds, end);
     end.template operator()<T>(acc, pl, lds);
   } else {

@@ -370,3 +370,18 @@ def test_scales_are_one_for_each_matrix_or_a_number():
         for a, b in zip(wn.orthogonalize(gs, scales=scales), want):
             assert torch.equal(a, 0.5 * b)
     assert torch.equal(wn.orthogonalize(gs[:1], scales=[0.5])[0], 0.5 * want[0])
+
+
+@DTYPES
+@pytest.mark.parametrize("scale", [1e-30, -1e-34, 1e-36, 1e-38, 1e37])
+def test_scales_at_the_ends_of_fp32(scale, dtype):
+    """Their product with the sums' own power of two lies below fp32's smallest normal value.  A result there is off by half
+    of the smallest step of its type: 2^-150, bf16 2^-134."""
+    import paper_1702_07825_amd as wn
+    for m, n in ((70, 90), (130, 60), (300, 200)):
+        g = _matrix(m, n, dtype, seed=m)
+        got = wn.orthogonalize([g], scales=scale)[0]
+        want, t = _formula(g, scale=float(np.float32(scale)))
+        off = float((got.double() - want).norm())
+        t += 2.0 ** (-150 if dtype == torch.float32 else -134) * (m * n) ** 0.5
+        assert off <= t, (m, n, scale, off, t, float(want.norm()))
