@@ -707,9 +707,10 @@ def orthogonalize(updates, scales=None, coefficients=MUON_COEFFICIENTS, eps: flo
     if not dense:
         raise ValueError("updates must be contiguous")
     arrays = np.zeros(n, dtype=_ORTHO_ARRAY)
-    if np.ndim(scales) and np.shape(scales) != (n,):  # (numpy would take one of a single number for all)
+    scales = np.asarray(1.0 if scales is None else scales, dtype=np.float32)
+    if scales.ndim and scales.shape != (n,):  # (numpy would take a list of one for all)
         raise ValueError("scales must be a number or one for each of the %d updates" % n)
-    arrays["scale"] = 1.0 if scales is None else scales
+    arrays["scale"] = scales
     if outs is None:
         outs = [on.empty(s, d) for s, d in zip(shapes, dtypes)]
     else:
