@@ -389,7 +389,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
       for (int h = 32; h; h >>= 1)
 #pragma unroll
         for (int l = 0; l <= kWaves; ++l) {
-          // (without a branch: hipcc 7.2 made wrong code of one, entries of equal values had the same rank)
+          // (Without a branch: given `if (k <= want && before(o, e)) ahead[l] = k` with nine lists, hipcc 7.2 keeps `ahead` in one run
+          // of registers and copies the old run on the path where the values are equal and o's number is lower, so equal entries
+          // got the same rank.  A kernel of this loop alone does so at -O1 to -O3, not at -O0, and not with two lists.)
           const int k = ahead[l] + h;
           const Group o = found[l * want + min(k, want) - 1];
           const int in = (int)(k <= want) & ((int)(o.v > e.v) | ((int)(o.v == e.v) & (int)(o.g < e.g)));
