@@ -385,3 +385,15 @@ def test_scales_at_the_ends_of_fp32(scale, dtype):
         off = float((got.double() - want).norm())
         t += 2.0 ** (-150 if dtype == torch.float32 else -134) * (m * n) ** 0.5
         assert off <= t, (m, n, scale, off, t, float(want.norm()))
+
+
+def test_a_list_of_both_dtypes_described_by_several_launches():
+    """More than 68 matrices, what a launch describes, of each dtype: the second dtype takes the workspace that the first had."""
+    import paper_1702_07825_amd as wn
+    gs = [_matrix(1 + i % 71, 1 + (7 * i) % 67, (torch.float32, torch.bfloat16)[i & 1], seed=500 + i) for i in range(290)]
+    scales = [0.01 * (i + 1) * (-1) ** i for i in range(len(gs))]
+    got = wn.orthogonalize(gs, scales=scales)
+    for g, s, o in zip(gs, scales, got):
+        _near(o, g, scale=s)
+    alone = wn.orthogonalize([g for g in gs if g.dtype == torch.bfloat16], scales=scales[1::2])
+    assert all(torch.equal(a, o) for a, o in zip(alone, got[1::2]))
