@@ -430,7 +430,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
     __syncthreads();
     if (wave == 0) {
       // A lane adds up D / 64 terms and a piece at most, then come 6 sums of lanes.  (Where it overflows every class stays in.)
-      const float off = (float)(a.D / 64 + 16) * 0x1.04p-24f * wnk::wave_max(lane < want ? size_of[lane] : 0.f);
+      const float size = wnk::wave_max(lane < want ? size_of[lane] : 0.f), off = (float)(a.D / 64 + 16) * 0x1.04p-24f * size;
       // as many classes as groups reach the least of the groups' largest
       const float t = -wnk::wave_max(lane < want ? -top_of[lane] : -INFINITY), low = at_least(t, off);
       int m = 0;
@@ -451,9 +451,13 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
         pick[rank] = e;
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      const float last = at_least(pick[a.top - 1].v, off);
+      // (Where fewer than top are left of a mask, the last one is the mask's value: if the products are nothing beside it in 64 bits
+      // either, 32 have the masked classes in order already.)
+      const float last = pick[a.top - 1].v, low_last = at_least(last, off);
       int c = 0;
-      for (int i = 0; i < m; i += 64) c += __popcll(__ballot(i + lane < m && !(at_most(pick[min(i + lane, m - 1)].v, off) < last)));
+      if (fabsf(last) >= size * 0x1p55f) c = a.top;
+      else
+        for (int i = 0; i < m; i += 64) c += __popcll(__ballot(i + lane < m && !(at_most(pick[min(i + lane, m - 1)].v, off) < low_last)));
       if (lane == 0) many = c;
     }
     __syncthreads();

@@ -302,6 +302,21 @@ def test_candidates_by_the_hundred(N, V, dtype):
         _probe(x, w, b, y, top)
 
 
+@DTYPES
+@pytest.mark.parametrize("N,V,mask", [(20, 300, m) for m in (-1e9, -1e17, -1e30, -3e38, 1e30)] +
+                         [(N, 2000, m) for N in (90, 1600) for m in (-1e30, -3e38, 1e30)])
+def test_fewer_classes_left_than_alternatives(N, V, mask, dtype):
+    """Alternatives among classes that a finite value masks: by their numbers where 64 bits hold nothing beside it, and by their
+    logits at -1e9 (at -1e17 where one reaches 8, half of the step there).  32 bits hold nothing there, so all groups' largest
+    logits are alike, which lets classes be missed unless all groups are searched: 38 groups of 8 with 32 alternatives."""
+    x, w, b, y, _, _ = (t.cuda() for t in _inputs(N, 100, V, dtype, seed=54))
+    x[1] = 0
+    b[:] = mask
+    b[[7, V // 2, V - 1]] = torch.tensor([0.5, -0.5, 1.5], device="cuda") if mask < 0 else 2 * mask
+    for top in (1, 3, 32) if -1e18 < mask < 0 else (1, 3, 4, 20, 32):
+        _probe(x, w, b, y, top)
+
+
 def test_few_classes_in_several_pieces():
     """fp32 rows so long that a piece of the packed vocabulary holds a part of the classes only."""
     x, w, b, y, _, _ = (t.cuda() for t in _inputs(66, 50000, 800, torch.float32, seed=45))
