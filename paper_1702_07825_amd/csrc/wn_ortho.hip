@@ -54,8 +54,8 @@ struct Group {
   Matrix *of_sym, *of_step;
 };
 
-// What a matrix is put together from: as many of a list as a launch's arguments hold (82 small ones in two
-// launches 158 us a call; whole descriptors took five, 172).
+// What a matrix is put together from: as many of a list as a launch's arguments hold (82 small ones take two launches of 4 us;
+// as whole descriptors five, and a call 14 us longer).
 struct Given {
   Address g, out, buffers;
   int rows, cols;
@@ -465,19 +465,28 @@ struct Sides {
 inline bool empty(const wn_ortho_array& a) { return a.rows == 0 || a.cols == 0; }
 
 // The tiles of a launch: by a model of its time.  A chunk of 256 x 256 outputs takes a CU 1.4 us (three products of fp16
-// parts: 2.1), of 128 x 128 two blocks on a CU 1.2 us, of 64 x 64 four 0.9 us; a tile's start and end 8, 6 and 5 us.
+// parts: 2.1), of 128 x 128 two blocks on a CU 1.2 us, of 64 x 64 two 0.45 us; a tile's start and end 8, 6 and 2.5 us.
+// Both sides of 64 and 128 (us a call of five steps, bf16 and fp32): B X of 576 tiles of 64 145 and 147, 227 and 228 (9 matrices of
+// 512 x 512), 768 193 and 200, 346 and 352 (3 of 1024 x 1024), 982 160 and 167, 248 and 264 (14 of width 333), 896 155 and 152, 263 and
+// 254 (14 of 512 x 512), 1024 241 and 237, 450 and 429 (1024 x 4096), 1536 324 and 300, 622 and 587 (6 of 1024 x 1024); X X' and the
+// polynomial of 816 193 and 253, 346 and 460 (3 of 1024 x 1024), 1056 423 and 432, 817 and 806 (2048 x 2048), 1200 153 and 157, 239 and 260
+// (60 of 256 x 256, where the model takes 128), 1632 324 and 314, 622 and 595 (6 of 1024 x 1024).
 constexpr int kTileSides[3] = {256, 128, 64};
+// What the LDS of 256 CUs holds.
+template <class T>
+constexpr int blocks_at_once() { return 256 * (160 * 1024 / T::kLds); }
+static_assert(blocks_at_once<Big>() == 256 && blocks_at_once<Small>() == 512 && blocks_at_once<Tiny>() == 512, "the model's figures");
 struct Plan {
   double sum[3] = {0, 0, 0}, longest[3] = {0, 0, 0}, blocks[3] = {0, 0, 0};
   void add(int k, double tiles, int units, bool sp) {
-    static const double kChunkUs[3] = {1.4, 1.2, 0.9}, kEnds[3] = {8.0, 6.0, 5.0};
+    static const double kChunkUs[3] = {1.4, 1.2, 0.45}, kEnds[3] = {8.0, 6.0, 2.5};
     const double us = units / kChunk * kChunkUs[k] * (sp ? 1.5 : 1.0) + kEnds[k];
     sum[k] += tiles * us;
     blocks[k] += tiles;
     longest[k] = std::max(longest[k], us);
   }
   int best() const {
-    static const double kRoom[3] = {256, 512, 1024};
+    static const double kRoom[3] = {blocks_at_once<Big>(), blocks_at_once<Small>(), blocks_at_once<Tiny>()};
     int at = 0;
     double least = 1e300;
     for (int k = 0; k < 3; ++k) {
