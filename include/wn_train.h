@@ -91,8 +91,8 @@ size_t wn_loss_backward_workspace_bytes(int32_t dtype, int32_t N, int32_t D, int
  *   logprob, entropy, lse   fp32 [N] out
  *   top_ids       int32 [N][top] out, the classes of the largest logits in falling order, of equal ones the lowest first;
  *   top_logprobs  fp32 [N][top] out, their log probabilities.  Both may be NULL where top is 0.
- * The alternatives' logits are summed in 64 bits, so classes closer to each other than the other logits' rounding are in
- * order; one that that rounding moves behind more than two others (and one more for each 8 of top) in other groups of 8
+ * The alternatives' logits are summed in 64 bits, so classes closer to each other than the other logits' rounding (their
+ * products' and their bias's addition's) are in order; one that that rounding moves behind more than two others (and one more for each 8 of top) in other groups of 8
  * classes may be missed (more than 64 rows of up to 1024 classes: in any groups).  A class of bias -inf is masked: it adds
  * nothing to the entropy and is an alternative (of log probability -inf) only where fewer than top are left.  If every class
  * is masked, or a logit is NaN or +inf, the row's logprob, entropy, lse and top_logprobs are NaN or infinite and its top_ids
@@ -189,7 +189,7 @@ typedef struct {
  *   `steps` times, with (a, b, c) = coefficients[0], [1], [2] of the step:  A = X X',  X <- (a I + b A + c A A) X
  *   out = scale X, transposed back
  * coefficients is a HOST array [steps][3].  With (3.4445, -4.7750, 2.0315) five times the singular values of out / scale
- * lie about 1 (0.7 to 1.2) where those of X were above 0.003 or so; any others may be given as long as no entry of a step's X, A or
+ * lie about 1 (0.68 to 1.21, and the roundings) where those of X were above 0.002; any others may be given as long as no entry of a step's X, A or
  * a I + b A + c A A reaches 16, 16 or 64 in size (a matrix where one does ends up not finite).
  * A zero matrix gives zeros; an infinity or NaN in a matrix makes its update NaN, and no other's.
  * Products are summed in fp32: of WN_BF16 matrices X, A and a I + b A + c A A are rounded to fp16 between products (2^-11 of a value, and
@@ -201,7 +201,7 @@ int wn_orthogonalize(int32_t n_arrays, const wn_ortho_array* arrays, int32_t ste
                      void* workspace, size_t ws_bytes, void* stream);
 
 /* Bytes of workspace wn_orthogonalize needs for arrays of these sizes and dtypes (0 for sizes out of range): about six times
- * the arrays in 16 bits (fp32: twelve), of about 4 GiB of buffers at a time. */
+ * the arrays in 16 bits (fp32: twelve) with sides rounded up to 64 (fp32: 32), of about 4 GiB of buffers at a time. */
 size_t wn_orthogonalize_workspace_bytes(int32_t n_arrays, const wn_ortho_array* arrays);
 
 #ifdef __cplusplus

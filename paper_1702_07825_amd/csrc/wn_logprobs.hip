@@ -344,8 +344,8 @@ __device__ __forceinline__ float at_most(float l, float off) { return fmaxf(l * 
 // `top` unless classes are nearly alike, are computed in 64 and ranked by counting.  For few rows the block joins its row's
 // statistics first.
 // Bound: many rows by reading the groups and the classes' rows of w (4096 rows x 65536 classes x 1024, bf16, 8 alternatives: 134 MB
-// and 0.74 GB, most of it from the caches, 177 us; 16000 x 256 x 256 in fp32, 3: 37); few rows by a chain of some ten reads and
-// reductions (1 x 32000 x 2048, bf16, 5: 22 us).
+// and 0.74 GB, most of it from the caches, 177 us; 16000 x 256 x 256 in fp32, 3: 38); few rows by a chain of some ten reads and
+// reductions (1 x 32000 x 2048, bf16, 5: 23 us).
 template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2) void alternatives(const Alternatives a) {
   constexpr int kThreads = 64 * kWaves, kAhead = kWaves <= 4 ? 1 : 2;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
     }
     __syncthreads();
     // An entry's rank: how many of each list, all sorted, are before it.  (Compared with every entry, one after the other in
-    // LDS, 1 row x 32000 classes x 2048 with 20 alternatives took 77 us and not 58, 37 x 50021 x 777 with 20 127 and not 109.)
+    // LDS, 1 row x 32000 classes x 2048 with 20 alternatives took 19 us longer, 37 x 50021 x 777 with 20 18.)
     const int all = (kWaves + 1) * want;
     for (int i = tid; i < all; i += kThreads) {
       const Group e = found[i];
@@ -497,8 +497,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 1 ? 5 : kWaves <= 4 ? 6 : 2)
 // ------------------------------------------------------------------------------------------------
 // Classes of a group.  Where one segment holds a row's logits, they are kept and searched themselves, which costs less than
 // the logits of eight classes for each one wanted.  Groups of 8 and of 1 (us a call): 16000 rows x 256 classes x 256 in fp32, 3
-// alternatives 86 and 60, in bf16 20 of them 274 and 107; 16000 x 1024 x 256, 5: 118 and 93; 300 x 1000 x 1024, 20: 47 and 36;
-// 2000 x 1024 x 64, 5: 35 and 36; but 16000 x 1030 x 256, 5: 139 and 229, and few rows gain nothing (64 x 1000 x 1024, 5: 25
+// alternatives 84 and 59, in bf16 20 of them 294 and 107; 16000 x 1024 x 256, 5: 121 and 78; 300 x 1000 x 1024, 20: 48 and 36;
+// 2000 x 1024 x 64, 5: 34 and 28; but 16000 x 1030 x 256, 5: 139 and 229, and few rows gain nothing (64 x 1000 x 1024, 5: 25
 // and 25; 1 x 2048 x 2048: 20 and 27).
 int group_of(int N, int V) { return N > kFewRows && V <= 64 * kSegment && (size_t)N * V * 4 <= kGroupsBytes ? 1 : 8; }
 
@@ -536,11 +536,11 @@ struct Probe {
 
 // Waves of a row.  Few rows leave the chip empty, so a row takes many; many rows of few groups take one each, which has no
 // other to wait for.  Measured with 1, 4 and 8 waves (us beside the call without alternatives): 1 row x 32000 classes x
-// 2048, 5 alternatives 55, 20, 19 and 20 of them 124, 41, 34; 37 x 50021 x 777 in fp32, 20: 138, 51, 36; 128 x 32000 x 1024 in
-// fp32, 5: 59, 34, 34; 300 x 32000 x 1024, 5: 51, 23, 39; 1000 x 32000 x 1024, 20: 113, 82, 132; 4096 x 65536 x 1024, 8: 225,
-// 203, 410; 16000 x 256 x 256 in fp32, 3: 31, 72, 364.  The chip holds 1536 blocks of 4 waves at a time, and rows of one segment
-// beyond that take one wave (1 and 4): 1536 x 1000 x 1024, 20 31 and 28, 1537 of them 31 and 37; 1536 x 8000 x 1024, 5 38 and 37,
-// 1537 38 and 44.
+// 2048, 5 alternatives 58, 22, 19 and 20 of them 133, 44, 35; 37 x 50021 x 777 in fp32, 20: 144, 54, 37; 128 x 32000 x 1024 in
+// fp32, 5: 61, 34, 35; 300 x 32000 x 1024, 5: 51, 24, 39; 1000 x 32000 x 1024, 20: 118, 83, 135; 4096 x 65536 x 1024, 8: 220,
+// 191, 394; 16000 x 256 x 256 in fp32, 3: 31, 74, 364.  The chip holds 1536 blocks of 4 waves at a time, and rows of one segment
+// beyond that take one wave (1 and 4): 1536 x 1000 x 1024, 20 31 and 28, 1537 of them 31 and 36; 1536 x 8000 x 1024, 5 38 and 37,
+// 1537 39 and 45.
 template <class E>
 hipError_t launch_alternatives(const Alternatives& a, hipStream_t st) {
   if (a.N <= 128) hipLaunchKernelGGL((alternatives<E, 8>), dim3(a.N), dim3(512), 0, st, a);

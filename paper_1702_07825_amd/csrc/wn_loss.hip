@@ -90,7 +90,8 @@ __device__ __forceinline__ float join_largest(const float* parts, int n) {
 // 1 - p, so what 2^-39 cuts off is not seen.  As dw's operand a row is a class, which no row may target and whose
 // probabilities may all be small: there e is the class's own within a tile of rows, so that the tile's
 // largest p (1 if a row targets the class) lies in [2^14, 2^15), up to kQMost (a tile all below 2^-66 is held to 2^-105).  dw's sums change from one tile's
-// scale to the next by at most 2^66: below 2^116 with 2^20 rows of products below 2^30.
+// scale to the next by at most 2^66, those of log probabilities and entropies (whose |q| is below 8, e from 12) by 2^68: below 2^118
+// with 2^20 rows of products below 2^30.  (A tile whose q is not finite takes e = 0; the class's sums are not finite then.)
 constexpr int kQScale = 14, kQMost = 80;
 // With upstream gradients g of a row's log probability and h of its entropy the logits' gradient is
 //   g ([v = y] - p) - h p (log p + H) = c q,   q = a [v = y] - p (a + e (log p + H)),   c = max(|g|, |h|), a = g / c, e = h / c:
@@ -333,7 +334,7 @@ struct OutEnd {
 #pragma unroll
     for (int j = 0; j < T::NB; ++j) {
       const int b = min(pl.b0 + 16 * j + pl.n, B - 1);
-      const float f = __uint_as_float((unsigned)(127 + now[b] - (now - B)[b]) << 23);  // (at most 2^66 either way)
+      const float f = __uint_as_float((unsigned)(127 + now[b] - (now - B)[b]) << 23);  // (at most 2^68 either way where q is finite)
 #pragma unroll
       for (int i = 0; i < T::NA; ++i) acc[i][j] *= f;
     }

@@ -394,8 +394,8 @@ struct Order {
 };
 
 // A phase of all matrices.  Bound: large matrices by the matrix units (busy 51 % of the cycles), small ones by the chain of a
-// launch's loads and stores.  Measured: 26 matrices of widths 2048 and 8192 in bf16, a step: X X' 461 us and B X 947, 1.0
-// PFLOP/s (of the triangle with its diagonal tiles; a plain library product of 16384^3 1.6), the polynomial 283; the smallest lists
+// launch's loads and stores.  Measured: 26 matrices of widths 2048 and 8192 in bf16, a step: X X' 451 us and B X 948, 1.0
+// PFLOP/s (of the triangle with its diagonal tiles; a plain library product of 16384^3 1.6), the polynomial 280; the smallest lists
 // 6 to 7 us a phase.
 template <class T, class E, int kPhase>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void newton(const Group g, const Step s, const Order order) {
